@@ -270,6 +270,99 @@ strp_status strp_refit(strp_ctx* ctx, strp_side side, const float* Gram, int32_t
                        const void* Rhs, strp_dtype rhs_dtype, int64_t ld_rhs, int64_t T, const int32_t* idx,
                        int32_t s, float* W, int32_t out, int32_t in);
 
+/* ---- a decoder layer's forward operators, and what its model answers -----------------------
+ *
+ * What carries calibration tokens from one module to the next, in the layout of the module path: activations are
+ * [channels x ld] with the tokens contiguous, ld a multiple of 8 and not below T, bases 16-byte aligned; columns from T on
+ * are neither data nor written.  They are stateless, need no module and do not touch the status word: what is not finite
+ * passes through the arithmetic.  Sums, softmax statistics and norms are held in fp32; an output of bf16 is rounded once.
+ * Results do not depend on the workspace's size, and a call repeated on the same inputs gives the same bits.  They may be
+ * captured; they run on the context's device whatever device is current.  Inputs must not overlap outputs except where said.
+ */
+
+/* activation of strp_linear: none, max(x, 0), x Phi(x) (the error-function form) */
+typedef enum { STRP_ACT_NONE = 0, STRP_ACT_RELU = 1, STRP_ACT_GELU = 2 } strp_activation;
+
+/*
+ * strp_linear -- Y = act(W X + bias) + R over T tokens: a projection with its bias, activation and residual in one pass
+ * (z = W a of the module path with what the paper's modules leave out).
+ *   W [M x ldw] w_dtype, ldw >= K a multiple of 8, entries from column K on are not read as data;  X [K x ldx] x_dtype;
+ *   bias [M] fp32 or NULL;  R [M x ldr] y_dtype or NULL;  Y [M x ldy] y_dtype.  R may be Y itself (same ld).
+ * bf16 W and X are multiplied in bf16 with fp32 sums; with an fp32 operand the products are those of fp32.
+ * Errors: STRP_EINVAL (null W, X or Y, sizes not positive, ld below its width or no multiple of 8, misaligned, unknown
+ * dtype or activation), STRP_ENOMEM (strp_linear_workspace_bytes).
+ */
+typedef struct {
+  const void* W;
+  const void* X;
+  const float* bias;
+  const void* R;
+  void* Y;
+  int32_t w_dtype, x_dtype, y_dtype;
+  int32_t M, K;
+  int32_t act;         /* strp_activation */
+  int64_t T, ldw, ldx, ldr, ldy;
+} strp_linear_in;
+strp_status strp_linear(strp_ctx* ctx, const strp_linear_in* in);
+/* Workspace (bytes, device) that strp_linear needs at these sizes and types, 0 where it needs none; pure function. */
+size_t strp_linear_workspace_bytes(int32_t M, int32_t K, int64_t T, strp_dtype w_dtype, strp_dtype x_dtype);
+
+/*
+ * strp_layer_norm -- Y[:, t] = (X[:, t] - mean_t) / sqrt(var_t + eps) * gain + bias over the d channels of every token
+ * (population variance, the deviations taken from the mean).
+ *   X [d x ldx], Y [d x ldy] of dtype;  gain, bias [d] fp32, either may be NULL (1 and 0).  Y may be X (same ld).
+ * Errors: STRP_EINVAL (null X or Y, d or T not positive, eps negative or not a number, bad ld, misaligned, unknown dtype).
+ */
+strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype dtype, int32_t d, int64_t T, int64_t ldx, const float* gain,
+                            const float* bias, double eps, void* Y, int64_t ldy);
+
+/*
+ * strp_attention -- causal attention over whole prompts that lie one after the other along the tokens; what it returns are
+ * the head outputs C that a head module's scores, Gram matrix and refit read.
+ *   Sequence i is tokens [seq_start[i], seq_start[i + 1]); its token t sees the keys of [seq_start[i], t].
+ *   head h, key-value head g(h):  c_t = sum_j softmax_j(scale q_t . k_j) v_j
+ *   Q [heads*d_head x ldq], K, V [kv_heads*d_head x ldk / ldv], C [heads*d_head x ldc], all of dtype;
+ *   seq_start: n_seq + 1 ascending offsets in [0, T] (device), or NULL for one sequence of all T tokens (n_seq = 0).
+ *   kv_of_head: heads entries in [0, kv_heads) (device), for heads that pruning has left in groups of different sizes;
+ *   NULL: g(h) = h / (heads / kv_heads), kv_heads divides heads.
+ * Sequences may be empty or of one token.  Tokens outside every sequence keep what C holds.  What a token does not see
+ * (other sequences, later tokens, padding) has no part in its result, whatever it holds, infinities and NaN included.
+ * Entries of seq_start or kv_of_head outside their ranges give wrong results, no access out of bounds.
+ * bf16: the probabilities are rounded to bf16 before they meet V (fp32 sums).  fp32: products of fp32.
+ * Errors: STRP_EINVAL (null pointer, sizes not positive, d_head above 128, kv_heads that does not divide heads without
+ * kv_of_head, scale not positive and finite, bad ld, misaligned, unknown dtype, more heads than 65535).
+ */
+typedef struct {
+  const void* Q;
+  const void* K;
+  const void* V;
+  void* C;
+  const int32_t* seq_start;
+  const int32_t* kv_of_head;
+  int32_t dtype, heads, kv_heads, d_head, n_seq;
+  float scale;
+  int64_t T, ldq, ldk, ldv, ldc;
+} strp_attention_in;
+strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in);
+
+/*
+ * strp_token_logprobs -- what a model answers at every token: log probability of a given token, entropy of the distribution,
+ * and the best alternatives.  logits [V x ldl] of dtype, one row per vocabulary entry.  With p = softmax(logits[:, t]):
+ *   logp[t] = log p[target[t]] (0 where target[t] is outside [0, V): not scored)   target [T] int32; both NULL: not wanted
+ *   entropy[t] = -sum p log p (an entry of -inf counts as 0)                        NULL: not wanted
+ *   top_id[i ldt + t], top_logp[i ldt + t], i < n_top: the entries of highest logit in descending order, equal ones by the
+ *   lower index, and their log p.  A token with a NaN among its logits has id -1 and NaN there.
+ * Errors: STRP_EINVAL (null logits, V or T not positive, n_top outside [0, min(V, STRP_TOP_MAX)], target without logp or the
+ * reverse, top_id or top_logp missing with n_top > 0, ldt < T, nothing asked for, bad ld, misaligned, unknown dtype),
+ * STRP_ENOMEM (strp_token_logprobs_workspace_bytes).
+ */
+#define STRP_TOP_MAX 16
+strp_status strp_token_logprobs(strp_ctx* ctx, const void* logits, strp_dtype dtype, int32_t V, int64_t T, int64_t ldl,
+                                const int32_t* target, float* logp, float* entropy, int32_t n_top, int32_t* top_id, float* top_logp,
+                                int64_t ldt);
+/* Workspace (bytes, device) that strp_token_logprobs needs; pure function. */
+size_t strp_token_logprobs_workspace_bytes(int32_t V, int64_t T, int32_t n_top);
+
 /* ---- stateful per-module path ---------------------------------------------------------- */
 typedef struct {
   const void* X;       /* [d x ldx]   x_dtype                                               */

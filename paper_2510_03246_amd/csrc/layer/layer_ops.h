@@ -1,0 +1,61 @@
+// Shared by the forward operators of a decoder layer (linear, layer norm, attention, token log probabilities).
+#pragma once
+
+#include "../strp_internal.h"
+
+namespace strp {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// The stream of a context may be the null stream, which is that of the current device: an operator makes its context's
+// device current while it enqueues and leaves the caller's as it was.
+class OnDevice {
+  int was_ = -1;
+  bool ok_ = false;
+
+ public:
+  explicit OnDevice(const strp_ctx* ctx) {
+    int now = -1;
+    if (hipGetDevice(&now) != hipSuccess) return;
+    if (now != ctx->device) {
+      if (hipSetDevice(ctx->device) != hipSuccess) return;
+      was_ = now;
+    }
+    ok_ = true;
+  }
+  ~OnDevice() {
+    if (was_ >= 0) (void)hipSetDevice(was_);
+  }
+  bool ok() const { return ok_; }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+};
+
+static inline bool known_dtype(int dt) { return dt == STRP_BF16 || dt == STRP_F32; }
+static inline size_t bytes_of(int dt) { return dt == STRP_BF16 ? 2 : 4; }
+static inline bool ptr16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+static inline bool token_ld(int64_t ld, int64_t T) { return ld >= T && ld % 8 == 0; }
+
+// N consecutive values as floats; N * sizeof(T) bytes aligned to themselves or to 16
+template <int N, typename T>
+__device__ __forceinline__ void load_floats(const T* p, float (&v)[N]) {
+  typedef T vec __attribute__((ext_vector_type(N)));
+  const vec x = *(const vec*)p;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (float)x[i];
+}
+// values rounded once, to the nearest
+template <int N, typename T>
+__device__ __forceinline__ void store_floats(T* p, const float (&v)[N]) {
+  typedef T vec __attribute__((ext_vector_type(N)));
+  vec x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = (T)v[i];
+  *(vec*)p = x;
+}
+
+}  // namespace strp

@@ -23,11 +23,14 @@ PREC_FAST, PREC_SPLIT = 0, 1
 PROD_GRAM, PROD_RHS2, PROD_RHS1, PROD_RESID, PROD_AUPD, PROD_ZUPD = range(6)
 STAGE_SELECT, STAGE_REFIT2, STAGE_REFIT1, STAGE_AUPD, STAGE_ZUPD, STAGE_OBJ = 1, 2, 4, 8, 16, 32
 STAGE_ALL = 63
+ACT_NONE, ACT_RELU, ACT_GELU = range(3)
+TOP_MAX = 16
 
 EXPORTS = [
     "strp_create", "strp_destroy", "strp_last_error", "strp_set_precision", "strp_set_product_planes", "strp_set_workspace",
     "strp_poll", "strp_workspace_bytes", "strp_module_cache_bytes", "strp_profile_enable", "strp_profile_read", "strp_profile_launches", "strp_gram", "strp_score_alloc", "strp_mask_topk", "strp_mask_topk_static", "strp_topk_workspace_bytes", "strp_weight_energy", "strp_alloc_inverse", "strp_alloc_softmax",
     "strp_refit", "strp_module_init", "strp_admm_step",
+    "strp_linear", "strp_linear_workspace_bytes", "strp_layer_norm", "strp_attention", "strp_token_logprobs", "strp_token_logprobs_workspace_bytes",
 ]
 
 
@@ -69,6 +72,19 @@ class Report(C.Structure):
 
 class WeightRef(C.Structure):
     _fields_ = [("W", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("ld", C.c_int64)]
+
+
+class LinearIn(C.Structure):
+    _fields_ = [("W", C.c_void_p), ("X", C.c_void_p), ("bias", C.c_void_p), ("R", C.c_void_p), ("Y", C.c_void_p),
+                ("w_dtype", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("M", C.c_int32), ("K", C.c_int32),
+                ("act", C.c_int32), ("T", C.c_int64), ("ldw", C.c_int64), ("ldx", C.c_int64), ("ldr", C.c_int64), ("ldy", C.c_int64)]
+
+
+class AttentionIn(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("C", C.c_void_p), ("seq_start", C.c_void_p),
+                ("kv_of_head", C.c_void_p), ("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("d_head", C.c_int32),
+                ("n_seq", C.c_int32), ("scale", C.c_float), ("T", C.c_int64), ("ldq", C.c_int64), ("ldk", C.c_int64),
+                ("ldv", C.c_int64), ("ldc", C.c_int64)]
 
 
 _packers = {}
@@ -131,8 +147,16 @@ def load_library():
     lib.strp_module_init.argtypes = [vp, C.POINTER(ModuleDesc), C.POINTER(ModuleState), C.POINTER(Params)]
     lib.strp_admm_step.argtypes = [vp, C.POINTER(ModuleDesc), C.POINTER(ModuleState), C.POINTER(Params),
                                    C.POINTER(Report)]
+    lib.strp_linear.argtypes = [vp, C.POINTER(LinearIn)]
+    lib.strp_layer_norm.argtypes = [vp, vp, C.c_int, i32, i64, i64, vp, vp, dbl, vp, i64]
+    lib.strp_attention.argtypes = [vp, C.POINTER(AttentionIn)]
+    lib.strp_token_logprobs.argtypes = [vp, vp, C.c_int, i32, i64, i64, vp, vp, vp, i32, vp, vp, i64]
+    lib.strp_linear_workspace_bytes.argtypes = [i32, i32, i64, C.c_int, C.c_int]
+    lib.strp_linear_workspace_bytes.restype = C.c_size_t
+    lib.strp_token_logprobs_workspace_bytes.argtypes = [i32, i64, i32]
+    lib.strp_token_logprobs_workspace_bytes.restype = C.c_size_t
     for name in EXPORTS:
-        if name not in ("strp_last_error", "strp_workspace_bytes", "strp_module_cache_bytes", "strp_topk_workspace_bytes"):
+        if not name.endswith("_bytes") and name != "strp_last_error":
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -298,6 +322,105 @@ class Context:
                                        _ptr(Rhs), dtype_code(Rhs), Rhs.stride(0), T, _ptr(idx), idx.numel(), _ptr(W),
                                        out, inn))
         return W
+
+    # ---- a decoder layer's forward operators ----------------------------------------------
+    # Activations are [channels x ld] tensors with the tokens contiguous, T of the ld columns valid; what the library cannot see
+    # (shapes, strides, types and devices of the tensors) is checked here, the rest there.
+    def _operand(self, name, t, shape, dtypes):
+        """t as an operand of `shape` (None: any; the last is the least) and one of the dtypes, on this context's device."""
+        if t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, the context on {self.device}")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+        if t.dim() != len(shape) or t.shape[-1] < shape[-1] or (len(shape) == 2 and shape[0] is not None and t.shape[0] != shape[0]):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, needs {tuple(shape)}")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: its last dimension is not contiguous")
+        return t
+
+    def _rows(self, t):
+        # one row of any length: its stride is not used, and torch may report anything
+        return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+
+    def _result(self, name, out, rows, T, dtype):
+        if out is None:
+            return torch.empty((rows, (T + 7) // 8 * 8), dtype=dtype, device=self.device)
+        return self._operand(name, out, (rows, T), (dtype,) if dtype is not None else tuple(_CODES))
+
+    def strp_linear(self, W, X, T, bias=None, act=ACT_NONE, residual=None, out=None):
+        """act(W X + bias) + residual: W [M x K], X [K x ld], bias [M] fp32, residual [M x ld] of out's dtype (out itself is
+        allowed).  Returns out, made in X's dtype where none is given."""
+        M, K = W.shape
+        self._operand("W", W, (M, K), _CODES)
+        self._operand("X", X, (K, T), _CODES)
+        out = self._result("out", out, M, T, X.dtype if out is None else None)
+        if bias is not None:
+            self._operand("bias", bias, (M,), (torch.float32,))
+        if residual is not None:
+            self._operand("residual", residual, (M, T), (out.dtype,))
+        need = int(self.lib.strp_linear_workspace_bytes(M, K, T, dtype_code(W), dtype_code(X)))
+        if need:
+            self.ensure_workspace(need)
+        a = LinearIn(_ptr(W), _ptr(X), _ptr(bias), _ptr(residual), _ptr(out), dtype_code(W), dtype_code(X), dtype_code(out), M, K, act, T,
+                     self._rows(W), self._rows(X), self._rows(residual) if residual is not None else 0, self._rows(out))
+        self.check(self.lib.strp_linear(self.h, C.byref(a)))
+        return out
+
+    def strp_layer_norm(self, X, T, gain=None, bias=None, eps=1e-5, out=None):
+        """Normalisation of every token over the channels of X [d x ld]; gain, bias [d] fp32.  out may be X."""
+        d = X.shape[0]
+        self._operand("X", X, (d, T), _CODES)
+        out = self._result("out", out, d, T, X.dtype)
+        for name, t in (("gain", gain), ("bias", bias)):
+            if t is not None:
+                self._operand(name, t, (d,), (torch.float32,))
+        self.check(self.lib.strp_layer_norm(self.h, _ptr(X), dtype_code(X), d, T, self._rows(X), _ptr(gain), _ptr(bias), float(eps), _ptr(out),
+                                            self._rows(out)))
+        return out
+
+    def strp_attention(self, Q, K, V, T, heads, kv_heads=None, seq_start=None, kv_of_head=None, scale=None, out=None):
+        """Causal attention of T packed tokens: Q [heads*d_head x ld], K, V [kv_heads*d_head x ld], seq_start [n_seq + 1] int32 offsets
+        (None: one sequence), kv_of_head [heads] int32 (None: equal groups), scale 1 / sqrt(d_head) by default.  Returns
+        the head outputs, like Q."""
+        kv_heads = heads if kv_heads is None else kv_heads
+        if heads <= 0 or Q.dim() != 2 or Q.shape[0] % heads:
+            raise ValueError(f"Q: {tuple(Q.shape)} is not {heads} heads")
+        dh = Q.shape[0] // heads
+        self._operand("Q", Q, (None, T), _CODES)
+        self._operand("K", K, (kv_heads * dh, T), (Q.dtype,))
+        self._operand("V", V, (kv_heads * dh, T), (Q.dtype,))
+        out = self._result("out", out, heads * dh, T, Q.dtype)
+        if seq_start is not None:
+            self._operand("seq_start", seq_start, (2,), (torch.int32,))
+        if kv_of_head is not None:
+            self._operand("kv_of_head", kv_of_head, (heads,), (torch.int32,))
+        a = AttentionIn(_ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(seq_start), _ptr(kv_of_head), dtype_code(Q), heads, kv_heads, dh,
+                        seq_start.numel() - 1 if seq_start is not None else 0, dh ** -0.5 if scale is None else float(scale), T,
+                        self._rows(Q), self._rows(K), self._rows(V), self._rows(out))
+        self.check(self.lib.strp_attention(self.h, C.byref(a)))
+        return out
+
+    def strp_token_logprobs(self, logits, T, target=None, entropy=True, n_top=0):
+        """What a model answers at each of T tokens, from logits [V x ld]: dict of logp [T] (of target [T] int32, if given), entropy [T]
+        (if wanted), top_ids and top_logp [n_top x T]."""
+        V = logits.shape[0]
+        self._operand("logits", logits, (V, T), _CODES)
+        if target is not None:
+            self._operand("target", target, (T,), (torch.int32,))
+        if n_top < 0 or n_top > min(V, TOP_MAX):
+            raise ValueError(f"n_top outside [0, {min(V, TOP_MAX)}]")
+        e = lambda *shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=self.device)
+        res = {}
+        if target is not None:
+            res["logp"] = e(T)
+        if entropy:
+            res["entropy"] = e(T)
+        res["top_ids"], res["top_logp"] = e(n_top, T, dt=torch.int32), e(n_top, T)
+        self.ensure_workspace(int(self.lib.strp_token_logprobs_workspace_bytes(V, T, n_top)))
+        self.check(self.lib.strp_token_logprobs(self.h, _ptr(logits), dtype_code(logits), V, T, self._rows(logits), _ptr(target), _ptr(res.get("logp")),
+                                                _ptr(res.get("entropy")), n_top, _ptr(res["top_ids"]) if n_top else None,
+                                                _ptr(res["top_logp"]) if n_top else None, T))
+        return res
 
     def strp_module_init(self, desc, state, params):
         self.check(self.lib.strp_module_init(self.h, C.byref(desc), C.byref(state), C.byref(params)))

@@ -1,0 +1,170 @@
+"""Refusals and launches of the decoder layer's operators on a HIP runtime that launches nothing (fake_hip.c), without a GPU.
+Each check runs in a process of its own, where the stand-in is loaded before the library."""
+import ctypes as C
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+A = [(i + 1) << 44 for i in range(8)]          # addresses nothing reads
+
+
+def _library(ws_bytes=1 << 40):
+    sys.path.insert(0, HERE)
+    from test_host_side import Library
+    return Library(ws_bytes)
+
+
+def _linear(strp, **kw):
+    a = dict(W=A[0], X=A[1], bias=A[2], R=A[3], Y=A[4], w_dtype=strp.BF16, x_dtype=strp.BF16, y_dtype=strp.BF16, M=40, K=50, act=strp.ACT_RELU, T=60,
+             ldw=56, ldx=64, ldr=64, ldy=64)
+    a.update(kw)
+    return strp.LinearIn(**a)
+
+
+def check_linear_refusals():
+    lib = _library()
+    strp = lib.strp
+    call = lambda **kw: lib.launches(lambda: lib.lib.strp_linear(lib.h, C.byref(_linear(strp, **kw))))
+    for good in (dict(), dict(bias=None, R=None, ldr=0), dict(R=A[4]), dict(M=1, K=1, T=1, ldw=8, ldx=8, ldr=8, ldy=8), dict(y_dtype=strp.F32), dict(x_dtype=strp.F32)):
+        st, launches = call(**good)
+        assert st == strp.OK and launches, good
+    for bad in (dict(W=None), dict(X=None), dict(Y=None), dict(M=0), dict(K=0), dict(T=0), dict(M=-1), dict(T=-5), dict(w_dtype=2), dict(x_dtype=-1), dict(y_dtype=7),
+                dict(act=3), dict(act=-1), dict(ldw=48), dict(ldw=57), dict(ldx=56), dict(ldx=61), dict(ldy=59), dict(ldy=68), dict(ldr=56), dict(W=A[0] + 8), dict(X=A[1] + 2),
+                dict(Y=A[4] + 4), dict(R=A[3] + 8), dict(R=A[4], ldr=72)):
+        st, launches = call(**bad)
+        assert st == strp.EINVAL and not launches and lib.lib.strp_last_error(lib.h), bad
+    assert lib.lib.strp_linear(lib.h, None) == strp.EINVAL
+    assert lib.lib.strp_linear(None, C.byref(_linear(strp))) == strp.EINVAL
+
+
+def check_norm_refusals():
+    lib = _library()
+    strp = lib.strp
+
+    def call(X=A[0], dtype=strp.F32, d=10, T=20, ldx=24, gain=A[1], bias=A[2], eps=1e-5, Y=A[3], ldy=24):
+        return lib.launches(lambda: lib.lib.strp_layer_norm(lib.h, X, dtype, d, T, ldx, gain, bias, eps, Y, ldy))
+
+    for good in (dict(), dict(gain=None, bias=None), dict(Y=A[0]), dict(eps=0.0), dict(d=1, T=1, ldx=8, ldy=8), dict(dtype=strp.BF16)):
+        st, launches = call(**good)
+        assert st == strp.OK and launches, good
+    for bad in (dict(X=None), dict(Y=None), dict(dtype=5), dict(d=0), dict(T=0), dict(ldx=16), dict(ldx=23), dict(ldy=16), dict(eps=-1e-9), dict(eps=float("nan")), dict(X=A[0] + 4),
+                dict(Y=A[3] + 2), dict(Y=A[0], ldy=32)):
+        st, launches = call(**bad)
+        assert st == strp.EINVAL and not launches, bad
+    assert lib.lib.strp_layer_norm(None, A[0], 1, 1, 1, 8, None, None, 0.0, A[1], 8) == strp.EINVAL
+
+
+def check_attention_refusals():
+    lib = _library()
+    strp = lib.strp
+
+    def call(**kw):
+        a = dict(Q=A[0], K=A[1], V=A[2], C=A[3], seq_start=A[4], kv_of_head=None, dtype=strp.BF16, heads=8, kv_heads=2, d_head=64, n_seq=3, scale=0.125, T=100, ldq=104, ldk=104,
+                 ldv=104, ldc=104)
+        a.update(kw)
+        return lib.launches(lambda: lib.lib.strp_attention(lib.h, C.byref(strp.AttentionIn(**a))))
+
+    for good in (dict(), dict(seq_start=None, n_seq=0), dict(kv_of_head=A[5], kv_heads=3), dict(d_head=1), dict(d_head=128), dict(T=1, ldq=8, ldk=8, ldv=8, ldc=8), dict(dtype=strp.F32),
+                 dict(kv_of_head=A[5], heads=2, kv_heads=5)):
+        st, launches = call(**good)
+        assert st == strp.OK and launches, good
+    for bad in (dict(Q=None), dict(K=None), dict(V=None), dict(C=None), dict(dtype=2), dict(heads=0), dict(kv_heads=0), dict(d_head=0), dict(d_head=129), dict(T=0), dict(kv_heads=3),
+                dict(heads=65536), dict(heads=2, kv_heads=5), dict(n_seq=0), dict(n_seq=-1), dict(seq_start=None), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+                dict(scale=float("inf")), dict(ldq=96), dict(ldk=101), dict(ldv=103), dict(ldc=99), dict(Q=A[0] + 8), dict(K=A[1] + 2), dict(V=A[2] + 4), dict(C=A[3] + 8),
+                dict(T=1 << 31, ldq=1 << 31, ldk=1 << 31, ldv=1 << 31, ldc=1 << 31)):
+        st, launches = call(**bad)
+        assert st == strp.EINVAL and not launches, bad
+    assert lib.lib.strp_attention(lib.h, None) == strp.EINVAL
+
+
+def check_logprobs_refusals():
+    lib = _library()
+    strp = lib.strp
+
+    def call(logits=A[0], dtype=strp.F32, V=100, T=20, ldl=24, target=A[1], logp=A[2], entropy=A[3], n_top=5, top_id=A[4], top_logp=A[5], ldt=20):
+        return lib.launches(lambda: lib.lib.strp_token_logprobs(lib.h, logits, dtype, V, T, ldl, target, logp, entropy, n_top, top_id, top_logp, ldt))
+
+    for good in (dict(), dict(target=None, logp=None), dict(entropy=None), dict(n_top=0, top_id=None, top_logp=None, ldt=0), dict(n_top=16), dict(V=3, n_top=3), dict(V=1, T=1, ldl=8, n_top=1),
+                 dict(dtype=strp.BF16, V=130000, T=4000, ldl=4000, ldt=4000), dict(V=1 << 30, T=1, ldl=8)):
+        st, launches = call(**good)
+        assert st == strp.OK and len(launches) == 2, good
+        assert all(0 < g[0] and 0 < g[1] <= 65535 for _, g in launches), launches
+    for bad in (dict(logits=None), dict(dtype=9), dict(V=0), dict(T=0), dict(ldl=16), dict(ldl=25), dict(logits=A[0] + 4), dict(n_top=-1), dict(n_top=17), dict(V=4, n_top=5), dict(target=None),
+                dict(logp=None), dict(top_id=None), dict(top_logp=None), dict(ldt=19), dict(target=None, logp=None, entropy=None, n_top=0)):
+        st, launches = call(**bad)
+        assert st == strp.EINVAL and not launches, bad
+    need = lib.lib.strp_token_logprobs_workspace_bytes(100, 20, 5)
+    lib.workspace(need)
+    assert call()[0] == strp.OK
+    # every size's need is enough, and none is asked for beyond it
+    for V in (1, 7, 300, 50000, 130001):
+        for T in (1, 3, 64, 65, 513, 4096):
+            for n_top in (0, 1):
+                for dt in (strp.BF16, strp.F32):
+                    lib.workspace(lib.lib.strp_token_logprobs_workspace_bytes(V, T, n_top))
+                    assert call(V=V, T=T, ldl=(T + 7) // 8 * 8, ldt=T, n_top=n_top, dtype=dt)[0] == strp.OK, (V, T, n_top, dt)
+    lib.workspace(4096)
+    st, launches = call(V=50000)
+    assert st == strp.ENOMEM and not launches
+    bare = C.c_void_p()
+    assert lib.lib.strp_create(C.byref(bare), 0, None) == strp.OK
+    assert lib.lib.strp_token_logprobs(bare, A[0], strp.F32, 9, 9, 16, None, None, A[3], 0, None, None, 0) == strp.ENOMEM
+    assert lib.lib.strp_token_logprobs_workspace_bytes(0, 5, 1) == 0 and lib.lib.strp_token_logprobs_workspace_bytes(5, 0, 1) == 0
+
+
+def check_the_current_device_is_left_as_it_was():
+    lib = _library()
+    strp, fake = lib.strp, lib.fake
+    h = C.c_void_p()
+    assert lib.lib.strp_create(C.byref(h), 1, None) == strp.OK
+    assert lib.lib.strp_set_workspace(h, 1 << 40, 1 << 30) == strp.OK
+    for current in (0, 1):
+        fake.hipSetDevice(current)
+        assert lib.lib.strp_linear(h, C.byref(_linear(strp))) == strp.OK
+        assert lib.lib.strp_layer_norm(h, A[0], strp.F32, 8, 8, 8, None, None, 0.0, A[1], 8) == strp.OK
+        assert lib.lib.strp_token_logprobs(h, A[0], strp.F32, 9, 9, 16, None, None, A[3], 0, None, None, 0) == strp.OK
+        now = C.c_int(-1)
+        assert fake.hipGetDevice(C.byref(now)) == 0 and now.value == current
+
+
+CHECKS = [check_linear_refusals, check_norm_refusals, check_attention_refusals, check_logprobs_refusals, check_the_current_device_is_left_as_it_was]
+
+
+@pytest.fixture(scope="session")
+def fake_hip(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("fake") / "libfake_hip.so")
+    subprocess.run(["gcc", "-O1", "-Wall", "-shared", "-fPIC", "-o", so, os.path.join(HERE, "fake_hip.c")], check=True, timeout=120)
+    return so
+
+
+@pytest.mark.parametrize("check", [c.__name__ for c in CHECKS])
+def test_layer_ops_host(fake_hip, check):
+    from paper_2510_03246_amd import strp
+    if not os.path.exists(strp.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    out = subprocess.run([sys.executable, os.path.abspath(__file__), check], env=dict(os.environ, FAKE_HIP=fake_hip), capture_output=True, text=True,
+                         timeout=300)
+    assert out.returncode == 0, out.stdout + out.stderr
+
+
+def test_binding_structs_mirror_the_header(tmp_path):
+    from paper_2510_03246_amd import strp
+    pairs = [("strp_linear_in", "ldy", strp.LinearIn), ("strp_attention_in", "ldc", strp.AttentionIn), ("strp_attention_in", "scale", strp.AttentionIn)]
+    src = tmp_path / "layout.c"
+    body = "".join(f'  printf("%zu %zu\\n", sizeof({c}), offsetof({c}, {f}));\n' for c, f, _ in pairs)
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "strp.h"\nint main(void) {\n' + body + '  printf("%d\\n", STRP_TOP_MAX);\n  return 0;\n}\n')
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-I", os.path.join(os.path.dirname(HERE), "include"), "-o", str(exe), str(src)], check=True, timeout=120)
+    out = subprocess.run([str(exe)], check=True, capture_output=True, text=True, timeout=30).stdout.split("\n")
+    for (cname, field, cls), line in zip(pairs, out):
+        size, off = (int(x) for x in line.split())
+        assert C.sizeof(cls) == size and getattr(cls, field).offset == off, (cname, field)
+    assert int(out[len(pairs)]) == strp.TOP_MAX
+
+
+if __name__ == "__main__":
+    globals()[sys.argv[1]]()

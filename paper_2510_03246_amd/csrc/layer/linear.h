@@ -1,0 +1,42 @@
+// The products of strp_linear: what the entry point hands to the kernels.
+#pragma once
+
+#include "layer_ops.h"
+
+namespace strp {
+
+struct LinearP {
+  const void* W;
+  const void* X;
+  const float* bias;
+  const void* R;
+  void* Y;
+  int M, K, act;
+  long long T, ldw, ldx, ldr, ldy;
+  int tilesM, tilesN;
+  int splits, steps;     // parts of the contraction and steps of 32 (16) of each; more than one part: sums to part, [splits][M][tp]
+  float* part;
+  long long tp;
+};
+
+__device__ __forceinline__ float activate(float z, int act) {
+  if (act == STRP_ACT_RELU) return z > 0.0f ? z : (z == z ? 0.0f : z);
+  // z Phi(z) with Phi from the complementary error function: no cancellation where z is far below zero
+  if (act == STRP_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+  return z;
+}
+
+// How a product is cut: tile shape, parts of the contraction.  Of sizes and types only.
+enum { LINEAR_FEW = 0, LINEAR_TILE = 1, LINEAR_TILE_LARGE = 2 };
+struct LinearPlan {
+  int kind;
+  int bm, bn;
+  int splits, steps;
+  size_t part_bytes;
+};
+LinearPlan plan_linear_bf16(int M, int K, long long T);
+void launch_linear_bf16(strp_ctx* ctx, LinearP p, const LinearPlan& plan, int y_dtype);
+// sums of the parts, bias, activation, residual
+void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype);
+
+}  // namespace strp

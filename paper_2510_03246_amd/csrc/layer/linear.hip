@@ -1,25 +1,7 @@
 // Y = act(W X + bias) + R: projections of a decoder layer.
-#include "layer_ops.h"
+#include "linear.h"
 
 namespace strp {
-
-struct LinearP {
-  const void* W;
-  const void* X;
-  const float* bias;
-  const void* R;
-  void* Y;
-  int M, K, act;
-  long long T, ldw, ldx, ldr, ldy;
-  int tilesM;
-};
-
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == STRP_ACT_RELU) return z > 0.0f ? z : (z == z ? 0.0f : z);
-  // z Phi(z) with Phi from the complementary error function: no cancellation where z is far below zero
-  if (act == STRP_ACT_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-  return z;
-}
 
 // Products of fp32 (v_mfma_f32_32x32x2_f32: an operand of bf16 is widened, which is exact).  Tiles of 128 channels x 128 tokens,
 // four wavefronts of 64 x 64, 16 contraction steps in LDS while the next 16 are on their way to registers.  Rows of X and columns
@@ -112,8 +94,10 @@ using namespace strp;
 extern "C" {
 
 size_t strp_linear_workspace_bytes(int32_t M, int32_t K, int64_t T, strp_dtype w_dtype, strp_dtype x_dtype) {
-  (void)M; (void)K; (void)T; (void)w_dtype; (void)x_dtype;
-  return 0;
+  if (M <= 0 || K <= 0 || T <= 0) return 0;
+  if (w_dtype != STRP_BF16 || x_dtype != STRP_BF16) return 0;
+  const size_t part = plan_linear_bf16(M, K, T).part_bytes;
+  return part ? part + 4096 : 0;
 }
 
 strp_status strp_linear(strp_ctx* ctx, const strp_linear_in* in) {
@@ -127,13 +111,24 @@ strp_status strp_linear(strp_ctx* ctx, const strp_linear_in* in) {
   if (!ptr16(in->W) || !ptr16(in->X) || !ptr16(in->Y) || !ptr16(in->R)) return fail(ctx, STRP_EINVAL, "linear: W, X, R or Y not 16-byte aligned");
   if (in->R == in->Y && in->ldr != in->ldy) return fail(ctx, STRP_EINVAL, "linear: R is Y with another leading dimension");
   if ((in->M + 63) / 64 * ((in->T + 63) / 64) > 0x7fffffffLL) return fail(ctx, STRP_EINVAL, "linear: more than 2^31 tiles of 64 x 64");
+  LinearP p{in->W, in->X, in->bias, in->R, in->Y, in->M, in->K, in->act, in->T, in->ldw, in->ldx, in->ldr, in->ldy};
+  p.splits = 1;
+  LinearPlan plan{};
+  const int wb = in->w_dtype == STRP_BF16, xb = in->x_dtype == STRP_BF16;
+  if (wb && xb) {
+    plan = plan_linear_bf16(p.M, p.K, p.T);
+    if (plan.part_bytes) {
+      if (!ctx->ws) return fail(ctx, STRP_ENOMEM, "linear: no workspace set");
+      Arena arena(ctx);
+      STRP_TAKE(ctx, arena, part, float, plan.part_bytes / 4);
+      p.part = part;
+    }
+  }
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "linear: device %d cannot be made current", ctx->device);
-  LinearP p{in->W, in->X, in->bias, in->R, in->Y, in->M, in->K, in->act, in->T, in->ldw, in->ldx, in->ldr, in->ldy, 0};
   const double M = in->M, K = in->K, T = (double)in->T;
   ProfScope ps(ctx, "linear", 2.0 * M * K * T, bytes_of(in->w_dtype) * M * K + bytes_of(in->x_dtype) * K * T + bytes_of(in->y_dtype) * M * T * (in->R ? 2 : 1));
-  const int wb = in->w_dtype == STRP_BF16, xb = in->x_dtype == STRP_BF16;
-  if (wb && xb) launch_linear_f32<__bf16, __bf16>(ctx, p, in->y_dtype);
+  if (wb && xb) launch_linear_bf16(ctx, p, plan, in->y_dtype);
   else if (wb) launch_linear_f32<__bf16, float>(ctx, p, in->y_dtype);
   else if (xb) launch_linear_f32<float, __bf16>(ctx, p, in->y_dtype);
   else launch_linear_f32<float, float>(ctx, p, in->y_dtype);

@@ -1,0 +1,359 @@
+// act(W X + bias) + R with W and X in bf16: v_mfma_f32_16x16x32_bf16, fp32 sums.
+//
+// W has its contraction contiguous, X its tokens, so a fragment of W is 16 bytes of a row and a fragment of X is a column: it is
+// read from LDS by ds_read_b64_tr_b16, which hands the 16 lanes of a group the 16 columns of four rows.  The accumulator is that of
+// (tokens x channels): a lane has four consecutive tokens of one channel.
+#include "linear.h"
+
+namespace strp {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 16 bytes per lane from memory to LDS at lds_addr + 16 lane, without registers; completion by wait_loads
+__device__ __forceinline__ void copy_to_lds(const void* gptr, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(gptr) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// all but the last N loads have arrived
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads_and_lds() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ short4v read_turned(unsigned lds_addr) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(size_t)lds_addr);
+}
+
+// Which tile a workgroup has: workgroups go to the eight XCDs in turn, and the per that an XCD holds at a time are neighbours, eight
+// tiles of channels by per / 8 of tokens, so that its L2 serves them from 8 + per / 8 panels.
+__device__ __forceinline__ void tile_of(int b, int blocks, int per, int tilesM, int tilesN, int& tm, int& tn) {
+  const int round = 8 * per, full = blocks / round * round;
+  int q;
+  if (b < full) {
+    q = b / round * round + (b & 7) * per + b % round / 8;
+  } else {
+    const int x = b & 7, rem = blocks - full;
+    q = full + x * (rem >> 3) + min(x, rem & 7) + ((b - full) >> 3);
+  }
+  const int band = q / (8 * tilesN), r = q - band * 8 * tilesN, h = min(8, tilesM - 8 * band);
+  tn = r / h;
+  tm = 8 * band + r - tn * h;
+}
+
+// X of 32 steps lies in LDS as 32 rows of BN tokens, in blocks of 16 tokens whose order depends on the row so that the rows that a read
+// touches at once are in different banks.
+template <int BN>
+__device__ __forceinline__ constexpr int block_turn(int k) {
+  return BN >= 128 ? ((k & 3) | ((k >> 1) & 4)) : (((k >> 1) & 1) | ((k >> 2) & 2));
+}
+
+// What becomes of a wavefront's sums: acc[i][j] has tokens 16 j + 4 (lane / 16) .. + 3 of channel m + 16 i, tokens from t on.  bf16: four lanes
+// exchange their quads so that each has two runs of eight tokens, and every row is written in 64 contiguous bytes an instruction.
+template <typename YT, int NI>
+__device__ __forceinline__ void finish_tile(const LinearP& p, const floatx4 (&acc)[NI][4], int m, long long t, YT* out, long long ldo, const float* bias,
+                                            const YT* res, int act) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int mi = m + 16 * i;
+    const bool row = mi < p.M;
+    const int mc = row ? mi : p.M - 1;
+    const float b = bias ? bias[mc] : 0.0f;
+    const YT* R = res ? res + (long long)mc * p.ldr : nullptr;
+    YT* Y = out + (long long)mc * ldo;
+    if constexpr (sizeof(YT) == 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long long tj = t + 16 * j + 4 * g;
+        floatx4 v = acc[i][j], r = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        const bool ok = row && tj < p.T;
+        if (R && ok) r = *(const floatx4*)(R + tj);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = activate(v[e] + b, act) + r[e];
+        if (!ok) continue;
+        if (tj + 4 <= p.T) *(floatx4*)(Y + tj) = v;
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (tj + e < p.T) Y[tj + e] = v[e];
+      }
+    } else {
+      floatx4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[j][e] = activate(acc[i][j][e] + b, act);
+      // slots (j1 j0) x lanes (g1 g0) of quads 8 j1 + 4 j0 + 2 g1 + g0  ->  lanes (j0 g1), slots (j1 g0); in fp32 where the residual is to be added before
+      // the one rounding, else in bf16
+      const auto swap32 = [](unsigned& a, unsigned& b2) { const auto s = __builtin_amdgcn_permlane32_swap(a, b2, false, false); a = s[0]; b2 = s[1]; };
+      const auto swap16 = [](unsigned& a, unsigned& b2) { const auto s = __builtin_amdgcn_permlane16_swap(a, b2, false, false); a = s[0]; b2 = s[1]; };
+      if (R) {
+        const auto turn = [&](int j1) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v0 = v[2 * j1][e], v1 = v[2 * j1 + 1][e];       // not bit_cast of an element of a vector: that takes the first
+            unsigned a = __builtin_bit_cast(unsigned, v0), c = __builtin_bit_cast(unsigned, v1);
+            swap32(a, c);
+            swap16(a, c);
+            v[2 * j1][e] = __builtin_bit_cast(float, a);
+            v[2 * j1 + 1][e] = __builtin_bit_cast(float, c);
+          }
+        };
+        turn(0);
+        turn(1);
+      }
+#pragma unroll
+      for (int j1 = 0; j1 < 2; ++j1) {
+        const long long tj = t + 32 * j1 + 8 * g;
+        const bool ok = row && tj < p.T;
+        uint4 out;
+        if (R) {
+          bf16x8 r;
+          if (ok) r = *(const bf16x8*)(R + tj);
+          bf16x8 y;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = (__bf16)(v[2 * j1 + (e >> 2)][e & 3] + (ok ? (float)r[e] : 0.0f));
+          out = __builtin_bit_cast(uint4, y);
+        } else {
+          unsigned q[4];
+#pragma unroll
+          for (int j0 = 0; j0 < 2; ++j0)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              q[2 * j0 + e] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)v[2 * j1 + j0][2 * e], (__bf16)v[2 * j1 + j0][2 * e + 1]});
+          swap32(q[0], q[2]);
+          swap32(q[1], q[3]);
+          swap16(q[0], q[2]);
+          swap16(q[1], q[3]);
+          out = make_uint4(q[0], q[1], q[2], q[3]);
+        }
+        if (!ok) continue;
+        if (tj + 8 <= p.T) *(uint4*)(Y + tj) = out;
+        else {
+          const bf16x8 y = __builtin_bit_cast(bf16x8, out);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (tj + e < p.T) Y[tj + e] = y[e];
+        }
+      }
+    }
+  }
+}
+
+// Tiles of (WM 16 NI) channels x (64 WN) tokens, a wavefront 16 NI x 64; NP steps of 32 in LDS or on their way there.  While a step is
+// multiplied the next NP - 1 are in flight; its slot is asked for again as soon as every wavefront has its last fragments of it in registers.
+// A remainder of the contraction is the first step and goes through registers, zeros from K on.
+template <int WM, int WN, int NI, int NP, typename YT>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_tile_kernel(const LinearP p) {
+  constexpr int NW = WM * WN, BM = WM * 16 * NI, BN = WN * 64, STAGE = 64 * (BM + BN), XAT = 64 * BM;
+  constexpr int PIECES = (BM + BN) / 16, LPW = PIECES / NW, RPI = 512 / BN;     // 1 KB pieces of a step; rows of X in one
+  static_assert(PIECES % NW == 0 && RPI >= 1, "pieces of a step");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NP * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  const int tiles = p.tilesM * p.tilesN, split = (int)blockIdx.x / tiles;
+  int tm, tn;
+  tile_of((int)blockIdx.x - split * tiles, tiles, NW >= 8 ? 32 : 64, p.tilesM, p.tilesN, tm, tn);
+  const int m0 = tm * BM;
+  const long long n0 = (long long)tn * BN;
+  const __bf16* W = (const __bf16*)p.W;
+  const __bf16* X = (const __bf16*)p.X;
+  const int all = (p.K + 31) / 32, s0 = split * p.steps, s1 = min(all, s0 + p.steps);
+  const int rest = s1 == all ? p.K & 31 : 0;               // this part has the remainder
+  const int whole = s1 - s0 - (rest ? 1 : 0), n = s1 - s0;
+
+  // this wavefront's pieces: 16 rows of W (four chunks of 16 bytes each, in an order that depends on the row) or RPI rows of X
+  const __bf16* src[LPW];
+  long long stride[LPW];
+  int piece_row[LPW], piece_col[LPW];
+  unsigned dst[LPW];
+  const long long t_last = (p.T - 1) / 8 * 8;
+  const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int q = wave + NW * i;
+    dst[i] = (unsigned)q * 1024;
+    if (q < BM / 16) {
+      const int row = min(m0 + 16 * q + (lane >> 2), p.M - 1), chunk = (lane & 3) ^ (lane >> 4);
+      piece_row[i] = row;
+      piece_col[i] = 8 * chunk;
+      src[i] = W + (long long)row * p.ldw + (long long)s0 * 32 + 8 * chunk;
+      stride[i] = 32;
+    } else {
+      const int k = (q - BM / 16) * RPI + lane / (64 / RPI), c = lane % (64 / RPI);
+      const long long t = n0 + 16 * ((c >> 1) ^ block_turn<BN>(k)) + 8 * (c & 1);
+      piece_row[i] = k;
+      piece_col[i] = 0;
+      src[i] = X + (t < p.T ? t : t_last) + (long long)(s0 * 32 + k) * p.ldx;
+      stride[i] = 32 * p.ldx;
+    }
+  }
+  const int first = rest ? 1 : 0;
+  auto issue = [&](int s) {                                // steps past the last re-read it and are never multiplied
+    if (whole == 0) return;
+    const long long at = min(s - first, whole - 1);
+    const unsigned slot = base + (unsigned)(s % NP) * STAGE;
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) copy_to_lds(src[i] + at * stride[i], slot + dst[i]);
+  };
+  if (rest) {
+    const int k0 = p.K - rest;
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+      const int q = wave + NW * i;
+      bf16x8 v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (__bf16)0.0f;
+      if (q < BM / 16) {
+        const int k = k0 + piece_col[i];
+        if (k < p.K) {
+          v = *(const bf16x8*)(W + (long long)piece_row[i] * p.ldw + k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = k + e < p.K ? v[e] : (__bf16)0.0f;
+        }
+      } else if (piece_row[i] < rest) {
+        v = *(const bf16x8*)(src[i] + (long long)(k0 - s0 * 32) * p.ldx);
+      }
+      *(bf16x8*)(smem + dst[i] + 16 * lane) = v;
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < NP; ++s)
+    if (s >= first) issue(s);
+
+  floatx4 acc[NI][4];
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int kg = lane >> 4, l16 = lane & 15;
+  const unsigned offW = base + (unsigned)((wm * NI * 16 + l16) * 64 + ((kg ^ (l16 >> 2)) * 16));
+  unsigned offX[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int k = 8 * kg + (l16 >> 2);
+    offX[j] = base + XAT + (unsigned)(k * (BN * 2) + ((wn * 4 + j) ^ block_turn<BN>(k)) * 32 + (l16 & 3) * 8);
+  }
+  struct XF { short4v lo[4], hi[4]; };
+  auto read_x = [&](XF& f, int s) {
+    const unsigned at = (unsigned)(s % NP) * STAGE;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f.lo[j] = read_turned(offX[j] + at);
+      f.hi[j] = read_turned(offX[j] + at + 4 * (BN * 2));
+    }
+  };
+  auto read_w = [&](bf16x8& f, int s, int i) {
+    f = *(const __attribute__((address_space(3))) bf16x8*)(size_t)(offW + (unsigned)(s % NP) * STAGE + i * 1024);
+  };
+  auto row = [&](floatx4 (&c)[4], const bf16x8& w, const XF& x) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x.lo[j], x.hi[j], 0, 1, 2, 3, 4, 5, 6, 7)), w, c[j], 0, 0, 0);
+  };
+  bf16x8 wa, wb;
+  auto step = [&](int s, const XF& xc, XF& xn) {
+    // the fragment of a row of tiles is read ahead of the matrix instructions of the row before it
+#pragma unroll
+    for (int i = 0; i < NI - 1; ++i) {
+      read_w(i & 1 ? wa : wb, s, i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      row(acc[i], i & 1 ? wb : wa, xc);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    wait_loads_and_lds<(NP - 2) * LPW>();   // the next step has landed; this wavefront's fragment reads of this one are complete
+    __syncthreads();                        // ... and so for every wavefront: the slot may be overwritten
+    issue(s + NP);
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8& last = (NI - 1) & 1 ? wb : wa;
+    row(acc[NI - 1], last, xc);
+    __builtin_amdgcn_sched_barrier(0);
+    read_x(xn, s + 1);                      // past the last step this reads a slot that is never multiplied
+    read_w(wa, s + 1, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  XF x0, x1;
+  wait_loads_and_lds<(NP - 1) * LPW>();
+  __syncthreads();
+  read_x(x0, 0);
+  read_w(wa, 0, 0);
+  int s = 0;
+#pragma unroll 1
+  for (; s + 1 < n; s += 2) {
+    step(s, x0, x1);
+    step(s + 1, x1, x0);
+  }
+  if (s < n) step(s, x0, x1);
+  wait_loads<0>();
+  const int m = m0 + wm * NI * 16 + l16;
+  const long long t = n0 + wn * 64;
+  if (p.splits > 1) finish_tile<float, NI>(p, acc, m, t, p.part + (long long)split * p.M * p.tp, p.tp, nullptr, nullptr, STRP_ACT_NONE);
+  else finish_tile<YT, NI>(p, acc, m, t, (YT*)p.Y, p.ldy, p.bias, (const YT*)p.R, p.act);
+}
+
+// Sums of the parts in their order, bias, activation, residual: a thread has four tokens of a channel.
+template <typename YT>
+__global__ __launch_bounds__(256) void linear_join_kernel(const LinearP p) {
+  const long long quads = p.tp / 4, i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int m = (int)(i / quads);
+  const long long t = (i - m * quads) * 4;
+  if (m >= p.M || t >= p.T) return;
+  floatx4 v = *(const floatx4*)(p.part + (long long)m * p.tp + t);
+  for (int s = 1; s < p.splits; ++s) v += *(const floatx4*)(p.part + ((long long)s * p.M + m) * p.tp + t);
+  float y[4], r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (p.R) load_floats<4>((const YT*)p.R + (long long)m * p.ldr + t, r);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = activate(v[e] + (p.bias ? p.bias[m] : 0.0f), p.act) + r[e];
+  YT* Y = (YT*)p.Y + (long long)m * p.ldy + t;
+  if (t + 4 <= p.T) store_floats<4>(Y, y);
+  else
+    for (int e = 0; e < 4; ++e)
+      if (t + e < p.T) Y[e] = (YT)y[e];
+}
+
+void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype) {
+  const dim3 grid((unsigned)((p.M * (p.tp / 4) + 255) / 256)), block(256);
+  if (y_dtype == STRP_BF16) hipLaunchKernelGGL((linear_join_kernel<__bf16>), grid, block, 0, ctx->stream, p);
+  else hipLaunchKernelGGL((linear_join_kernel<float>), grid, block, 0, ctx->stream, p);
+}
+
+LinearPlan plan_linear_bf16(int M, int K, long long T) {
+  LinearPlan q{LINEAR_TILE_LARGE, 256, 256, 1, (K + 31) / 32, 0};
+  const auto tiles = [&](int bm, int bn) { return (long long)((M + bm - 1) / bm) * ((T + bn - 1) / bn); };
+  if (tiles(256, 256) < 192) {
+    q.kind = LINEAR_TILE;
+    q.bm = q.bn = 128;
+    const long long n = tiles(128, 128);
+    const int all = (K + 31) / 32;
+    // parts of eight steps at least, until the chip has a workgroup for each CU
+    while (n * q.splits < 256 && all / (q.splits * 2) >= 8) q.splits *= 2;
+    q.steps = (all + q.splits - 1) / q.splits;
+    q.splits = (all + q.steps - 1) / q.steps;
+    if (q.splits > 1) q.part_bytes = (size_t)q.splits * M * ((T + 7) / 8 * 8) * 4;
+  }
+  return q;
+}
+
+template <typename YT>
+static void launch_tiles(strp_ctx* ctx, const LinearP& p, const LinearPlan& plan) {
+  const dim3 grid((unsigned)((long long)p.tilesM * p.tilesN * p.splits));
+  if (plan.kind == LINEAR_TILE_LARGE) hipLaunchKernelGGL((linear_tile_kernel<2, 4, 8, 4, YT>), grid, dim3(512), 0, ctx->stream, p);
+  else hipLaunchKernelGGL((linear_tile_kernel<2, 2, 4, 4, YT>), grid, dim3(256), 0, ctx->stream, p);
+}
+
+void launch_linear_bf16(strp_ctx* ctx, LinearP p, const LinearPlan& plan, int y_dtype) {
+  p.tilesM = (p.M + plan.bm - 1) / plan.bm;
+  p.tilesN = (int)((p.T + plan.bn - 1) / plan.bn);
+  p.splits = plan.splits;
+  p.steps = plan.steps;
+  p.tp = (p.T + 7) / 8 * 8;
+  if (y_dtype == STRP_BF16) launch_tiles<__bf16>(ctx, p, plan);
+  else launch_tiles<float>(ctx, p, plan);
+  if (p.splits > 1) launch_linear_join(ctx, p, y_dtype);
+}
+
+}  // namespace strp

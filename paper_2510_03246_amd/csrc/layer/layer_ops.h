@@ -7,6 +7,7 @@ namespace strp {
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -56,6 +57,30 @@ __device__ __forceinline__ void store_floats(T* p, const float (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = (T)v[i];
   *(vec*)p = x;
+}
+
+// ---- operands of bf16 on their way to the matrix cores ----
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 16 bytes per lane from memory to LDS at lds_addr + 16 lane, without registers; completion by wait_loads
+__device__ __forceinline__ void copy_to_lds(const void* gptr, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(gptr) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// all but the last N loads have arrived
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads_and_lds() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
+}
+// lane i of each group of 16 gets column i of the four rows whose 32 bytes the group's lanes 0-3, 4-7, 8-11, 12-15 point at (8 bytes each)
+__device__ __forceinline__ short4v read_turned(unsigned lds_addr) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(size_t)lds_addr);
 }
 
 }  // namespace strp

@@ -7,28 +7,6 @@
 
 namespace strp {
 
-typedef short short4v __attribute__((ext_vector_type(4)));
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// 16 bytes per lane from memory to LDS at lds_addr + 16 lane, without registers; completion by wait_loads
-__device__ __forceinline__ void copy_to_lds(const void* gptr, unsigned lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(gptr) : "memory", "m0");
-}
-#pragma clang diagnostic pop
-// all but the last N loads have arrived
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
-template <int N>
-__device__ __forceinline__ void wait_loads_and_lds() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
-}
-__device__ __forceinline__ short4v read_turned(unsigned lds_addr) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(size_t)lds_addr);
-}
-
 // Which tile a workgroup has: workgroups go to the eight XCDs in turn, and the per that an XCD holds at a time are neighbours, eight
 // tiles of channels by per / 8 of tokens, so that its L2 serves them from 8 + per / 8 panels.
 __device__ __forceinline__ void tile_of(int b, int blocks, int per, int tilesM, int tilesN, int& tm, int& tn) {

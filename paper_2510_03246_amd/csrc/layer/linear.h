@@ -26,6 +26,22 @@ __device__ __forceinline__ float activate(float z, int act) {
   return z;
 }
 
+// Bias, activation and residual on the sums v of four tokens from t on, channel m; t < T, m < M.
+template <typename YT>
+__device__ __forceinline__ void finish_quad(const LinearP& p, floatx4 v, int m, long long t) {
+  float y[4], r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (p.R) load_floats<4>((const YT*)p.R + (long long)m * p.ldr + t, r);
+  const float b = p.bias ? p.bias[m] : 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = activate(v[e] + b, p.act) + r[e];
+  YT* Y = (YT*)p.Y + (long long)m * p.ldy + t;
+  if (t + 4 <= p.T) store_floats<4>(Y, y);
+  else
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (t + e < p.T) Y[e] = (YT)y[e];
+}
+
 // How a product is cut: tile shape, parts of the contraction.  Of sizes and types only.
 enum { LINEAR_FEW = 0, LINEAR_TILE = 1, LINEAR_TILE_LARGE = 2 };
 struct LinearPlan {

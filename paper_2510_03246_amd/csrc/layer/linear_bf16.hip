@@ -273,7 +273,86 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
   else finish_tile<YT, NI>(p, acc, m, t, (YT*)p.Y, p.ldy, p.bias, (const YT*)p.R, p.act);
 }
 
-// Sums of the parts in their order, bias, activation, residual: a thread has four tokens of a channel.
+// Few tokens (T <= 16 NT): W is the traffic, read once straight into fragments (a lane has 16 bytes of a row), the contraction in parts among the NW wavefronts
+// of a workgroup, which add their sums up in LDS.  X goes to LDS as it lies, a run of FEW_K rows at a time, and is read turned.  A workgroup has 16 MI channels.
+constexpr int FEW_WAVES = 8;
+template <int NT, int MI, typename YT>
+__global__ __launch_bounds__(64 * FEW_WAVES, 2) void linear_few_kernel(const LinearP p) {
+  constexpr int NW = FEW_WAVES, ROW = 32 * NT;             // bytes of a row of X in LDS: 16 NT tokens
+  constexpr int KC = 32768 / ROW < 1024 ? 32768 / ROW : 1024, PER = KC / NW / 32;      // rows of X in LDS; steps of 32 of a wavefront in them
+  __shared__ __attribute__((aligned(16))) unsigned char sX[KC * ROW];
+  __shared__ floatx4 sums[NW][MI][NT][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = lane >> 4, l16 = lane & 15;
+  const int m0 = (int)blockIdx.x * 16 * MI;
+  const __bf16* X = (const __bf16*)p.X;
+  const __bf16* W[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) W[i] = (const __bf16*)p.W + (long long)min(m0 + 16 * i + l16, p.M - 1) * p.ldw;
+  floatx4 acc[MI][NT];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)sX;
+  const int t_last = (int)((p.T - 1) / 8);                 // last chunk of eight tokens
+  for (int k0 = 0; k0 < p.K; k0 += KC) {
+    // this wavefront's steps of the run: k0 + 32 (wave + NW j); what lies behind K is zero
+    bf16x8 w[PER][MI];
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int k = k0 + 32 * (wave + NW * j) + 8 * kg;
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (__bf16)0.0f;
+        if (k < p.K) v = *(const bf16x8*)(W[i] + k);
+        w[j][i] = v;
+      }
+    __syncthreads();
+#pragma unroll 4
+    for (int c = tid; c < KC * 2 * NT; c += 64 * NW) {
+      const int k = k0 + c / (2 * NT), ch = c % (2 * NT);
+      uintx4 v = uintx4{0u, 0u, 0u, 0u};
+      if (k < p.K && ch <= t_last) v = *(const uintx4*)(X + (long long)k * p.ldx + 8 * ch);
+      *(uintx4*)(sX + c * 16) = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int kl = 32 * (wave + NW * j);
+      if (k0 + kl >= p.K) break;
+      if (k0 + kl + 32 > p.K)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[j][i][e] = k0 + kl + 8 * kg + e < p.K ? w[j][i][e] : (__bf16)0.0f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const unsigned at = base + (unsigned)((kl + 8 * kg + (l16 >> 2)) * ROW + 32 * t + (l16 & 3) * 8);
+        const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_turned(at), read_turned(at + 4 * ROW), 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int i = 0; i < MI; ++i) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[j][i], acc[i][t], 0, 0, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) sums[wave][i][t][lane] = acc[i][t];
+  __syncthreads();
+  // four tokens of a channel to a thread, the wavefronts' sums in their order
+  for (int o = tid; o < MI * NT * 64; o += 64 * NW) {
+    const int l = o & 63, t = o >> 6, i = t / NT, m = m0 + 16 * i + (l & 15), tok = 16 * (t % NT) + 4 * (l >> 4);
+    floatx4 v = sums[0][i][t % NT][l];
+#pragma unroll
+    for (int s = 1; s < NW; ++s) v += sums[s][i][t % NT][l];
+    if (m >= p.M || tok >= p.T) continue;
+    finish_quad<YT>(p, v, m, tok);
+  }
+}
+
+// Sums of the parts in their order: a thread has four tokens of a channel.
 template <typename YT>
 __global__ __launch_bounds__(256) void linear_join_kernel(const LinearP p) {
   const long long quads = p.tp / 4, i = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -282,15 +361,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const LinearP p) {
   if (m >= p.M || t >= p.T) return;
   floatx4 v = *(const floatx4*)(p.part + (long long)m * p.tp + t);
   for (int s = 1; s < p.splits; ++s) v += *(const floatx4*)(p.part + ((long long)s * p.M + m) * p.tp + t);
-  float y[4], r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (p.R) load_floats<4>((const YT*)p.R + (long long)m * p.ldr + t, r);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = activate(v[e] + (p.bias ? p.bias[m] : 0.0f), p.act) + r[e];
-  YT* Y = (YT*)p.Y + (long long)m * p.ldy + t;
-  if (t + 4 <= p.T) store_floats<4>(Y, y);
-  else
-    for (int e = 0; e < 4; ++e)
-      if (t + e < p.T) Y[e] = (YT)y[e];
+  finish_quad<YT>(p, v, m, t);
 }
 
 void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype) {
@@ -301,6 +372,11 @@ void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype) {
 
 LinearPlan plan_linear_bf16(int M, int K, long long T) {
   LinearPlan q{LINEAR_TILE_LARGE, 256, 256, 1, (K + 31) / 32, 0};
+  if (T <= 64) {
+    q.kind = LINEAR_FEW;
+    q.bm = T <= 32 ? 16 : 32;
+    return q;
+  }
   const auto tiles = [&](int bm, int bn) { return (long long)((M + bm - 1) / bm) * ((T + bn - 1) / bn); };
   if (tiles(256, 256) < 192) {
     q.kind = LINEAR_TILE;
@@ -323,8 +399,21 @@ static void launch_tiles(strp_ctx* ctx, const LinearP& p, const LinearPlan& plan
   else hipLaunchKernelGGL((linear_tile_kernel<2, 2, 4, 4, YT>), grid, dim3(256), 0, ctx->stream, p);
 }
 
+template <typename YT>
+static void launch_few(strp_ctx* ctx, const LinearP& p) {
+  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.tilesM), dim3(64 * FEW_WAVES), 0, ctx->stream, p); };
+  if (p.T <= 16) go(linear_few_kernel<1, 1, YT>);
+  else if (p.T <= 32) go(linear_few_kernel<2, 1, YT>);
+  else go(linear_few_kernel<4, 2, YT>);
+}
+
 void launch_linear_bf16(strp_ctx* ctx, LinearP p, const LinearPlan& plan, int y_dtype) {
   p.tilesM = (p.M + plan.bm - 1) / plan.bm;
+  if (plan.kind == LINEAR_FEW) {
+    if (y_dtype == STRP_BF16) launch_few<__bf16>(ctx, p);
+    else launch_few<float>(ctx, p);
+    return;
+  }
   p.tilesN = (int)((p.T + plan.bn - 1) / plan.bn);
   p.splits = plan.splits;
   p.steps = plan.steps;

@@ -274,14 +274,15 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
 }
 
 // Few tokens (T <= 16 NT): W is the traffic, read once straight into fragments (a lane has 16 bytes of a row), the contraction in parts among the NW wavefronts
-// of a workgroup, which add their sums up in LDS.  X goes to LDS as it lies, a run of FEW_K rows at a time, and is read turned.  A workgroup has 16 MI channels.
+// of a workgroup, which add their sums up in LDS.  X goes to LDS as it lies, a run of rows at a time, and is read turned.  A workgroup has 16 MI channels.
 constexpr int FEW_WAVES = 8;
 template <int NT, int MI, typename YT>
-__global__ __launch_bounds__(64 * FEW_WAVES, 2) void linear_few_kernel(const LinearP p) {
+__global__ __launch_bounds__(64 * FEW_WAVES, NT < 4 ? 2 : 1) void linear_few_kernel(const LinearP p) {
   constexpr int NW = FEW_WAVES, ROW = 32 * NT;             // bytes of a row of X in LDS: 16 NT tokens
-  constexpr int KC = 32768 / ROW < 1024 ? 32768 / ROW : 1024, PER = KC / NW / 32;      // rows of X in LDS; steps of 32 of a wavefront in them
-  __shared__ __attribute__((aligned(16))) unsigned char sX[KC * ROW];
-  __shared__ floatx4 sums[NW][MI][NT][64];
+  constexpr int PER = NT == 1 ? 4 : 2, KC = 32 * NW * PER, XC = KC * 2 * NT / (64 * NW);      // steps of a wavefront in a run, rows of X in it, chunks of X a thread moves
+  static_assert(NW * MI * NT * 1024 <= 2 * KC * ROW, "the sums lie where X was");
+  __shared__ __attribute__((aligned(16))) unsigned char sX[2][KC * ROW];
+  floatx4(*sums)[MI][NT][64] = (floatx4(*)[MI][NT][64])&sX[0][0];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = lane >> 4, l16 = lane & 15;
   const int m0 = (int)blockIdx.x * 16 * MI;
   const __bf16* X = (const __bf16*)p.X;
@@ -295,46 +296,72 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void linear_few_kernel(const Lin
     for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)sX;
   const int t_last = (int)((p.T - 1) / 8);                 // last chunk of eight tokens
-  for (int k0 = 0; k0 < p.K; k0 += KC) {
-    // this wavefront's steps of the run: k0 + 32 (wave + NW j); what lies behind K is zero
-    bf16x8 w[PER][MI];
+  const uintx4 zero = uintx4{0u, 0u, 0u, 0u};
+  // a wavefront's steps of a run are k0 + 32 (wave + NW j); what lies behind K is zero
+  struct Run { uintx4 w[PER][MI]; };
+  auto ask_w = [&](Run& r, int k0) {
 #pragma unroll
     for (int j = 0; j < PER; ++j)
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         const int k = k0 + 32 * (wave + NW * j) + 8 * kg;
-        bf16x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (__bf16)0.0f;
-        if (k < p.K) v = *(const bf16x8*)(W[i] + k);
-        w[j][i] = v;
+        r.w[j][i] = k < p.K ? *(const uintx4*)(W[i] + k) : zero;
       }
-    __syncthreads();
-#pragma unroll 4
-    for (int c = tid; c < KC * 2 * NT; c += 64 * NW) {
-      const int k = k0 + c / (2 * NT), ch = c % (2 * NT);
-      uintx4 v = uintx4{0u, 0u, 0u, 0u};
-      if (k < p.K && ch <= t_last) v = *(const uintx4*)(X + (long long)k * p.ldx + 8 * ch);
-      *(uintx4*)(sX + c * 16) = v;
+  };
+  uintx4 x[XC];
+  auto ask_x = [&](int k0) {
+#pragma unroll
+    for (int c = 0; c < XC; ++c) {
+      const int at = tid + 64 * NW * c, k = k0 + at / (2 * NT), ch = at % (2 * NT);
+      x[c] = k < p.K && ch <= t_last ? *(const uintx4*)(X + (long long)k * p.ldx + 8 * ch) : zero;
     }
-    __syncthreads();
+  };
+  auto put_x = [&](int buf) {
+#pragma unroll
+    for (int c = 0; c < XC; ++c) *(uintx4*)(sX[buf] + (tid + 64 * NW * c) * 16) = x[c];
+  };
+  auto multiply = [&](const Run& r, int k0, int buf) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int kl = 32 * (wave + NW * j);
       if (k0 + kl >= p.K) break;
+      bf16x8 w[MI];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) w[i] = __builtin_bit_cast(bf16x8, r.w[j][i]);
       if (k0 + kl + 32 > p.K)
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[j][i][e] = k0 + kl + 8 * kg + e < p.K ? w[j][i][e] : (__bf16)0.0f;
+          for (int e = 0; e < 8; ++e) w[i][e] = k0 + kl + 8 * kg + e < p.K ? w[i][e] : (__bf16)0.0f;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const unsigned at = base + (unsigned)((kl + 8 * kg + (l16 >> 2)) * ROW + 32 * t + (l16 & 3) * 8);
-        const bf16x8 x = __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_turned(at), read_turned(at + 4 * ROW), 0, 1, 2, 3, 4, 5, 6, 7));
+        const unsigned at = base + (unsigned)(buf * KC * ROW + (kl + 8 * kg + (l16 >> 2)) * ROW + 32 * t + (l16 & 3) * 8);
+        const bf16x8 xf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_turned(at), read_turned(at + 4 * ROW), 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int i = 0; i < MI; ++i) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[j][i], acc[i][t], 0, 0, 0);
+        for (int i = 0; i < MI; ++i) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w[i], acc[i][t], 0, 0, 0);
       }
     }
+  };
+  // W is asked for two runs ahead, X one
+  Run ra, rb;
+  ask_x(0);
+  ask_w(ra, 0);
+  ask_w(rb, KC);
+  put_x(0);
+  __syncthreads();
+#pragma unroll 1
+  for (int k0 = 0; k0 < p.K; k0 += 2 * KC) {
+    ask_x(k0 + KC);
+    multiply(ra, k0, 0);
+    ask_w(ra, k0 + 2 * KC);
+    put_x(1);
+    __syncthreads();
+    if (k0 + KC >= p.K) break;
+    ask_x(k0 + 2 * KC);
+    multiply(rb, k0 + KC, 1);
+    ask_w(rb, k0 + 3 * KC);
+    put_x(0);
+    __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < MI; ++i)

@@ -14,7 +14,7 @@ struct LinearP {
   int M, K, act;
   long long T, ldw, ldx, ldr, ldy;
   int tilesM, tilesN;
-  int splits, steps;     // parts of the contraction and steps of 32 (16) of each; more than one part: sums to part, [splits][M][tp]
+  int splits, pairs;     // parts of the contraction and pairs of steps of 32 of each; more than one part: sums to part, [splits][M][tp]
   float* part;
   long long tp;
 };
@@ -43,11 +43,11 @@ __device__ __forceinline__ void finish_quad(const LinearP& p, floatx4 v, int m, 
 }
 
 // How a product is cut: tile shape, parts of the contraction.  Of sizes and types only.
-enum { LINEAR_FEW = 0, LINEAR_TILE = 1, LINEAR_TILE_LARGE = 2 };
+enum { LINEAR_FEW = 0, LINEAR_TILE = 1, LINEAR_TILE_LARGE = 2, LINEAR_TILE_SMALL = 3 };
 struct LinearPlan {
   int kind;
   int bm, bn;
-  int splits, steps;
+  int splits, pairs;
   size_t part_bytes;
 };
 LinearPlan plan_linear_bf16(int M, int K, long long T);

@@ -123,15 +123,16 @@ __device__ __forceinline__ void finish_tile(const LinearP& p, const floatx4 (&ac
   }
 }
 
-// Tiles of (WM 16 NI) channels x (64 WN) tokens, a wavefront 16 NI x 64; NP steps of 32 in LDS or on their way there.  While a step is
-// multiplied the next NP - 1 are in flight; its slot is asked for again as soon as every wavefront has its last fragments of it in registers.
-// A remainder of the contraction is the first step and goes through registers, zeros from K on.
-template <int WM, int WN, int NI, int NP, typename YT>
+// Tiles of (WM 16 NI) channels x (64 WN) tokens, a wavefront 16 NI x 64, in steps of 32 of the contraction.  W comes in pairs of steps, 128 bytes of a row: the
+// line that memory hands out whole (half a line at a time, large products ran at 1.27 PFLOP/s; XXX).  LDS holds three pairs of W and four steps of X, and all but
+// what is being multiplied is on its way: X for step s + 4 and, behind an odd step 2 p + 1, W for pair p + 3 are asked for as soon as every wavefront has its last
+// fragments of step s in registers.  A remainder of the contraction is the first pair and goes through registers, zeros from K on.
+template <int WM, int WN, int NI, typename YT>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_tile_kernel(const LinearP p) {
-  constexpr int NW = WM * WN, BM = WM * 16 * NI, BN = WN * 64, STAGE = 64 * (BM + BN), XAT = 64 * BM;
-  constexpr int PIECES = (BM + BN) / 16, LPW = PIECES / NW, RPI = 512 / BN;     // 1 KB pieces of a step; rows of X in one
-  static_assert(PIECES % NW == 0 && RPI >= 1, "pieces of a step");
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NP * STAGE];
+  constexpr int NW = WM * WN, BM = WM * 16 * NI, BN = WN * 64, PAIR = BM * 128, STEP = BN * 64, XAT = 3 * PAIR, RPI = 512 / BN;     // RPI: rows of X in a KB
+  constexpr int LW = BM / 8 / NW, LX = BN / 16 / NW, BEHIND = LW + 3 * LX;      // loads of a pair, of a step; those that may be on their way when a step begins
+  static_assert(BM % (8 * NW) == 0 && BN % (16 * NW) == 0, "whole pieces for every wavefront");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[3 * PAIR + 4 * STEP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int tiles = p.tilesM * p.tilesN, split = (int)blockIdx.x / tiles;
   int tm, tn;
@@ -140,68 +141,74 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
   const long long n0 = (long long)tn * BN;
   const __bf16* W = (const __bf16*)p.W;
   const __bf16* X = (const __bf16*)p.X;
-  const int all = (p.K + 31) / 32, s0 = split * p.steps, s1 = min(all, s0 + p.steps);
-  const int rest = s1 == all ? p.K & 31 : 0;               // this part has the remainder
-  const int whole = s1 - s0 - (rest ? 1 : 0), n = s1 - s0;
+  const int all = (p.K + 63) / 64, p0 = split * p.pairs, p1 = min(all, p0 + p.pairs);
+  const int rest = p1 == all ? p.K & 63 : 0;               // this part has the remainder
+  const int whole = p1 - p0 - (rest ? 1 : 0), n = 2 * (p1 - p0), first = rest ? 1 : 0;
 
-  // this wavefront's pieces: 16 rows of W (four chunks of 16 bytes each, in an order that depends on the row) or RPI rows of X
-  const __bf16* src[LPW];
-  long long stride[LPW];
-  int piece_row[LPW], piece_col[LPW];
-  unsigned dst[LPW];
+  // this wavefront's KBs: eight rows of W (eight chunks of 16 bytes each, in an order that depends on the row), RPI rows of X
+  const __bf16* srcW[LW];
+  const __bf16* srcX[LX];
+  int chunkW[LW], rowX[LX];
   const long long t_last = (p.T - 1) / 8 * 8;
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
 #pragma unroll
-  for (int i = 0; i < LPW; ++i) {
-    const int q = wave + NW * i;
-    dst[i] = (unsigned)q * 1024;
-    if (q < BM / 16) {
-      const int row = min(m0 + 16 * q + (lane >> 2), p.M - 1), chunk = (lane & 3) ^ (lane >> 4);
-      piece_row[i] = row;
-      piece_col[i] = 8 * chunk;
-      src[i] = W + (long long)row * p.ldw + (long long)s0 * 32 + 8 * chunk;
-      stride[i] = 32;
-    } else {
-      const int k = (q - BM / 16) * RPI + lane / (64 / RPI), c = lane % (64 / RPI);
-      const long long t = n0 + 16 * ((c >> 1) ^ block_turn<BN>(k)) + 8 * (c & 1);
-      piece_row[i] = k;
-      piece_col[i] = 0;
-      src[i] = X + (t < p.T ? t : t_last) + (long long)(s0 * 32 + k) * p.ldx;
-      stride[i] = 32 * p.ldx;
-    }
+  for (int i = 0; i < LW; ++i) {
+    const int r = 8 * (wave + NW * i) + (lane >> 3);
+    chunkW[i] = 8 * ((lane & 7) ^ ((r >> 1) & 7));
+    srcW[i] = W + (long long)min(m0 + r, p.M - 1) * p.ldw + chunkW[i];
   }
-  const int first = rest ? 1 : 0;
-  auto issue = [&](int s) {                                // steps past the last re-read it and are never multiplied
-    if (whole == 0) return;
-    const long long at = min(s - first, whole - 1);
-    const unsigned slot = base + (unsigned)(s % NP) * STAGE;
 #pragma unroll
-    for (int i = 0; i < LPW; ++i) copy_to_lds(src[i] + at * stride[i], slot + dst[i]);
+  for (int i = 0; i < LX; ++i) {
+    const int c = lane % (64 / RPI);
+    rowX[i] = (wave + NW * i) * RPI + lane / (64 / RPI);
+    const long long t = n0 + 16 * ((c >> 1) ^ block_turn<BN>(rowX[i])) + 8 * (c & 1);
+    srcX[i] = X + (t < p.T ? t : t_last) + (long long)rowX[i] * p.ldx;
+  }
+  // pairs and steps past the last re-read it and are never multiplied
+  auto issue_w = [&](int pr) {
+    if (whole == 0) return;
+    const long long k = (long long)(p0 + min(pr - first, whole - 1)) * 64;
+#pragma unroll
+    for (int i = 0; i < LW; ++i) copy_to_lds(srcW[i] + k, base + (unsigned)(pr % 3) * PAIR + (unsigned)(wave + NW * i) * 1024);
+  };
+  auto issue_x = [&](int s) {
+    if (whole == 0) return;
+    const long long k = (long long)p0 * 64 + 32 * min(s - 2 * first, 2 * whole - 1);
+#pragma unroll
+    for (int i = 0; i < LX; ++i) copy_to_lds(srcX[i] + k * p.ldx, base + XAT + (unsigned)(s & 3) * STEP + (unsigned)(wave + NW * i) * 1024);
   };
   if (rest) {
     const int k0 = p.K - rest;
 #pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-      const int q = wave + NW * i;
+    for (int i = 0; i < LW; ++i) {
+      const int k = k0 + chunkW[i];
       bf16x8 v;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (__bf16)0.0f;
-      if (q < BM / 16) {
-        const int k = k0 + piece_col[i];
-        if (k < p.K) {
-          v = *(const bf16x8*)(W + (long long)piece_row[i] * p.ldw + k);
+      if (k < p.K) {
+        v = *(const bf16x8*)(srcW[i] + k0);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = k + e < p.K ? v[e] : (__bf16)0.0f;
-        }
-      } else if (piece_row[i] < rest) {
-        v = *(const bf16x8*)(src[i] + (long long)(k0 - s0 * 32) * p.ldx);
+        for (int e = 0; e < 8; ++e) v[e] = k + e < p.K ? v[e] : (__bf16)0.0f;
       }
-      *(bf16x8*)(smem + dst[i] + 16 * lane) = v;
+      *(bf16x8*)(smem + (wave + NW * i) * 1024 + 16 * lane) = v;
     }
-  }
 #pragma unroll
-  for (int s = 0; s < NP; ++s)
-    if (s >= first) issue(s);
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < LX; ++i) {
+        uintx4 v = uintx4{0u, 0u, 0u, 0u};
+        if (k0 + 32 * s + rowX[i] < p.K) v = *(const uintx4*)(srcX[i] + (long long)(k0 + 32 * s) * p.ldx);
+        *(uintx4*)(smem + XAT + s * STEP + (wave + NW * i) * 1024 + 16 * lane) = v;
+      }
+  } else {
+    issue_w(0);
+    issue_x(0);
+  }
+  issue_w(1);
+  if (!rest) issue_x(1);
+  issue_x(2);
+  issue_w(2);
+  issue_x(3);
 
   floatx4 acc[NI][4];
 #pragma unroll
@@ -209,7 +216,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   const int kg = lane >> 4, l16 = lane & 15;
-  const unsigned offW = base + (unsigned)((wm * NI * 16 + l16) * 64 + ((kg ^ (l16 >> 2)) * 16));
+  const unsigned offW = base + (unsigned)((wm * NI * 16 + l16) * 128 + ((kg ^ (l16 >> 1)) * 16));
   unsigned offX[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -218,15 +225,16 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
   }
   struct XF { short4v lo[4], hi[4]; };
   auto read_x = [&](XF& f, int s) {
-    const unsigned at = (unsigned)(s % NP) * STAGE;
+    const unsigned at = (unsigned)(s & 3) * STEP;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       f.lo[j] = read_turned(offX[j] + at);
       f.hi[j] = read_turned(offX[j] + at + 4 * (BN * 2));
     }
   };
-  auto read_w = [&](bf16x8& f, int s, int i) {
-    f = *(const __attribute__((address_space(3))) bf16x8*)(size_t)(offW + (unsigned)(s % NP) * STAGE + i * 1024);
+  unsigned pair_at = 0;                                    // where the pair of the step being read lies
+  auto read_w = [&](bf16x8& f, int odd, int i) {
+    f = *(const __attribute__((address_space(3))) bf16x8*)(size_t)((offW ^ (unsigned)(64 * odd)) + pair_at + i * 2048);
   };
   auto row = [&](floatx4 (&c)[4], const bf16x8& w, const XF& x) {
 #pragma unroll
@@ -234,38 +242,40 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
       c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x.lo[j], x.hi[j], 0, 1, 2, 3, 4, 5, 6, 7)), w, c[j], 0, 0, 0);
   };
   bf16x8 wa, wb;
-  auto step = [&](int s, const XF& xc, XF& xn) {
+  auto step = [&](int s, int odd, const XF& xc, XF& xn) {
     // the fragment of a row of tiles is read ahead of the matrix instructions of the row before it
 #pragma unroll
     for (int i = 0; i < NI - 1; ++i) {
-      read_w(i & 1 ? wa : wb, s, i + 1);
+      read_w(i & 1 ? wa : wb, odd, i + 1);
       __builtin_amdgcn_sched_barrier(0);
       row(acc[i], i & 1 ? wb : wa, xc);
       __builtin_amdgcn_sched_barrier(0);
     }
-    wait_loads_and_lds<(NP - 2) * LPW>();   // the next step has landed; this wavefront's fragment reads of this one are complete
-    __syncthreads();                        // ... and so for every wavefront: the slot may be overwritten
-    issue(s + NP);
+    wait_loads_and_lds<BEHIND - LX>();      // the next step has landed; this wavefront's fragment reads of this one are complete
+    __syncthreads();                        // ... and so for every wavefront: the slots may be overwritten
+    if (odd) {
+      issue_w((s >> 1) + 3);
+      pair_at = pair_at == 2 * PAIR ? 0 : pair_at + PAIR;
+    }
+    issue_x(s + 4);
     __builtin_amdgcn_sched_barrier(0);
     bf16x8& last = (NI - 1) & 1 ? wb : wa;
     row(acc[NI - 1], last, xc);
     __builtin_amdgcn_sched_barrier(0);
     read_x(xn, s + 1);                      // past the last step this reads a slot that is never multiplied
-    read_w(wa, s + 1, 0);
+    read_w(wa, !odd, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
   XF x0, x1;
-  wait_loads_and_lds<(NP - 1) * LPW>();
+  wait_loads_and_lds<2 * LW + 3 * LX>();
   __syncthreads();
   read_x(x0, 0);
   read_w(wa, 0, 0);
-  int s = 0;
 #pragma unroll 1
-  for (; s + 1 < n; s += 2) {
-    step(s, x0, x1);
-    step(s + 1, x1, x0);
+  for (int s = 0; s < n; s += 2) {
+    step(s, 0, x0, x1);
+    step(s + 1, 1, x1, x0);
   }
-  if (s < n) step(s, x0, x1);
   wait_loads<0>();
   const int m = m0 + wm * NI * 16 + l16;
   const long long t = n0 + wn * 64;
@@ -398,32 +408,32 @@ void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype) {
 }
 
 LinearPlan plan_linear_bf16(int M, int K, long long T) {
-  LinearPlan q{LINEAR_TILE_LARGE, 256, 256, 1, (K + 31) / 32, 0};
+  LinearPlan q{LINEAR_TILE_LARGE, 256, 256, 1, (K + 63) / 64, 0};
   if (T <= 64) {
     q.kind = LINEAR_FEW;
     q.bm = T <= 32 ? 16 : 32;
     return q;
   }
-  const auto tiles = [&](int bm, int bn) { return (long long)((M + bm - 1) / bm) * ((T + bn - 1) / bn); };
-  if (tiles(256, 256) < 192) {
-    q.kind = LINEAR_TILE;
-    q.bm = q.bn = 128;
-    const long long n = tiles(128, 128);
-    const int all = (K + 31) / 32;
-    // parts of eight steps at least, until the chip has a workgroup for each CU
-    while (n * q.splits < 256 && all / (q.splits * 2) >= 8) q.splits *= 2;
-    q.steps = (all + q.splits - 1) / q.splits;
-    q.splits = (all + q.steps - 1) / q.steps;
-    if (q.splits > 1) q.part_bytes = (size_t)q.splits * M * ((T + 7) / 8 * 8) * 4;
-  }
+  const auto tiles = [&](int b) { return (long long)((M + b - 1) / b) * ((T + b - 1) / b); };
+  if (tiles(256) >= 192) return q;
+  q.kind = tiles(128) >= 192 ? LINEAR_TILE : LINEAR_TILE_SMALL;
+  q.bm = q.bn = q.kind == LINEAR_TILE ? 128 : 64;
+  const long long n = tiles(q.bm);
+  const int all = (K + 63) / 64;
+  // parts of four pairs of steps at least, until the chip has a workgroup for each CU
+  while (n * q.splits < 256 && all / (q.splits * 2) >= 4) q.splits *= 2;
+  q.pairs = (all + q.splits - 1) / q.splits;
+  q.splits = (all + q.pairs - 1) / q.pairs;
+  if (q.splits > 1) q.part_bytes = (size_t)q.splits * M * ((T + 7) / 8 * 8) * 4;
   return q;
 }
 
 template <typename YT>
 static void launch_tiles(strp_ctx* ctx, const LinearP& p, const LinearPlan& plan) {
   const dim3 grid((unsigned)((long long)p.tilesM * p.tilesN * p.splits));
-  if (plan.kind == LINEAR_TILE_LARGE) hipLaunchKernelGGL((linear_tile_kernel<2, 4, 8, 4, YT>), grid, dim3(512), 0, ctx->stream, p);
-  else hipLaunchKernelGGL((linear_tile_kernel<2, 2, 4, 4, YT>), grid, dim3(256), 0, ctx->stream, p);
+  if (plan.kind == LINEAR_TILE_LARGE) hipLaunchKernelGGL((linear_tile_kernel<2, 4, 8, YT>), grid, dim3(512), 0, ctx->stream, p);
+  else if (plan.kind == LINEAR_TILE) hipLaunchKernelGGL((linear_tile_kernel<2, 2, 4, YT>), grid, dim3(256), 0, ctx->stream, p);
+  else hipLaunchKernelGGL((linear_tile_kernel<2, 1, 2, YT>), grid, dim3(128), 0, ctx->stream, p);
 }
 
 template <typename YT>
@@ -443,7 +453,7 @@ void launch_linear_bf16(strp_ctx* ctx, LinearP p, const LinearPlan& plan, int y_
   }
   p.tilesN = (int)((p.T + plan.bn - 1) / plan.bn);
   p.splits = plan.splits;
-  p.steps = plan.steps;
+  p.pairs = plan.pairs;
   p.tp = (p.T + 7) / 8 * 8;
   if (y_dtype == STRP_BF16) launch_tiles<__bf16>(ctx, p, plan);
   else launch_tiles<float>(ctx, p, plan);

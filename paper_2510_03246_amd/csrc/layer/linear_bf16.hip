@@ -124,13 +124,12 @@ __device__ __forceinline__ void finish_tile(const LinearP& p, const floatx4 (&ac
 }
 
 // Tiles of (WM 16 NI) channels x (64 WN) tokens, a wavefront 16 NI x 64, in steps of 32 of the contraction.  W comes in pairs of steps, 128 bytes of a row: the
-// line that memory hands out whole (half a line at a time, large products ran at 1.27 PFLOP/s; XXX).  LDS holds three pairs of W and four steps of X, and all but
-// what is being multiplied is on its way: X for step s + 4 and, behind an odd step 2 p + 1, W for pair p + 3 are asked for as soon as every wavefront has its last
-// fragments of step s in registers.  A remainder of the contraction is the first pair and goes through registers, zeros from K on.
+// line that memory hands out whole.  LDS holds three pairs of W and four steps of X, and all but what is being multiplied is on its way.  A remainder of the
+// contraction is the first pair and goes through registers, zeros from K on.
 template <int WM, int WN, int NI, typename YT>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_tile_kernel(const LinearP p) {
   constexpr int NW = WM * WN, BM = WM * 16 * NI, BN = WN * 64, PAIR = BM * 128, STEP = BN * 64, XAT = 3 * PAIR, RPI = 512 / BN;     // RPI: rows of X in a KB
-  constexpr int LW = BM / 8 / NW, LX = BN / 16 / NW, BEHIND = LW + 3 * LX;      // loads of a pair, of a step; those that may be on their way when a step begins
+  constexpr int LW = BM / 8 / NW, LX = BN / 16 / NW;      // loads of a pair, of a step
   static_assert(BM % (8 * NW) == 0 && BN % (16 * NW) == 0, "whole pieces for every wavefront");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[3 * PAIR + 4 * STEP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
@@ -201,13 +200,12 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
         *(uintx4*)(smem + XAT + s * STEP + (wave + NW * i) * 1024 + 16 * lane) = v;
       }
   } else {
-    issue_w(0);
     issue_x(0);
+    issue_w(0);
+    issue_x(1);
   }
-  issue_w(1);
-  if (!rest) issue_x(1);
   issue_x(2);
-  issue_w(2);
+  issue_w(1);
   issue_x(3);
 
   floatx4 acc[NI][4];
@@ -224,10 +222,10 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
     offX[j] = base + XAT + (unsigned)(k * (BN * 2) + ((wn * 4 + j) ^ block_turn<BN>(k)) * 32 + (l16 & 3) * 8);
   }
   struct XF { short4v lo[4], hi[4]; };
-  auto read_x = [&](XF& f, int s) {
+  auto read_x = [&](XF& f, int s, int j0, int j1) {
     const unsigned at = (unsigned)(s & 3) * STEP;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = j0; j < j1; ++j) {
       f.lo[j] = read_turned(offX[j] + at);
       f.hi[j] = read_turned(offX[j] + at + 4 * (BN * 2));
     }
@@ -242,34 +240,34 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
       c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(x.lo[j], x.hi[j], 0, 1, 2, 3, 4, 5, 6, 7)), w, c[j], 0, 0, 0);
   };
   bf16x8 wa, wb;
+  // A step.  Its fragments of X are in registers as it begins, and so is its first one of W.  Halfway through, the wavefronts meet: the next step has landed, and
+  // nobody reads this step's X or the pair before this step's any more, so their places are asked for again; the second half reads the next step's fragments.
   auto step = [&](int s, int odd, const XF& xc, XF& xn) {
-    // the fragment of a row of tiles is read ahead of the matrix instructions of the row before it
+    constexpr int HALF = NI / 2;
 #pragma unroll
-    for (int i = 0; i < NI - 1; ++i) {
-      read_w(i & 1 ? wa : wb, odd, i + 1);
+    for (int i = 0; i < NI; ++i) {
+      if (i + 1 < NI) read_w(i & 1 ? wa : wb, odd, i + 1);
+      if (i >= HALF) read_x(xn, s + 1, (i - HALF) * 4 / HALF, (i - HALF + 1) * 4 / HALF);      // past the last step: a slot that is never multiplied
+      if (i + 1 == NI) {
+        if (odd) pair_at = pair_at == 2 * PAIR ? 0 : pair_at + PAIR;
+        read_w(wa, !odd, 0);
+      }
       __builtin_amdgcn_sched_barrier(0);
       row(acc[i], i & 1 ? wb : wa, xc);
       __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 == HALF) {
+        wait_loads<2 * LX + LW>();
+        __builtin_amdgcn_s_barrier();
+        issue_x(s + 4);
+        if (!odd) issue_w((s >> 1) + 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    wait_loads_and_lds<BEHIND - LX>();      // the next step has landed; this wavefront's fragment reads of this one are complete
-    __syncthreads();                        // ... and so for every wavefront: the slots may be overwritten
-    if (odd) {
-      issue_w((s >> 1) + 3);
-      pair_at = pair_at == 2 * PAIR ? 0 : pair_at + PAIR;
-    }
-    issue_x(s + 4);
-    __builtin_amdgcn_sched_barrier(0);
-    bf16x8& last = (NI - 1) & 1 ? wb : wa;
-    row(acc[NI - 1], last, xc);
-    __builtin_amdgcn_sched_barrier(0);
-    read_x(xn, s + 1);                      // past the last step this reads a slot that is never multiplied
-    read_w(wa, !odd, 0);
-    __builtin_amdgcn_sched_barrier(0);
   };
   XF x0, x1;
-  wait_loads_and_lds<2 * LW + 3 * LX>();
+  wait_loads_and_lds<LW + 3 * LX>();
   __syncthreads();
-  read_x(x0, 0);
+  read_x(x0, 0, 0, 4);
   read_w(wa, 0, 0);
 #pragma unroll 1
   for (int s = 0; s < n; s += 2) {

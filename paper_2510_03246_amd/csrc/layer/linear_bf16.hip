@@ -405,25 +405,31 @@ void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype) {
   else hipLaunchKernelGGL((linear_join_kernel<float>), grid, block, 0, ctx->stream, p);
 }
 
+// Tile shape and parts of the contraction by the time they take.  A workgroup's pair of steps takes the longer the more workgroups share its CU (us, measured on
+// products of 768 .. 8192 channels over 128 .. 8192 tokens): tiles of 256 1.8, alone on a CU; of 128 0.65 alone, 1.25 two on a CU; of 64 0.42, 0.6, 0.75 and 0.9 for
+// one to four.  Parts cost a launch and their sums' way through memory.  What the rule weighs, in us: 8192 x 2048 over 1024 tokens in tiles of 256 57, of 128 41, over 2048
+// 65 against 80; 768 x 768 over 2048 in tiles of 128 13.5, of 64 11.7; 4096 x 4096 over 128 in tiles of 64 whole 30, in two parts 20, in four 17.5.
 LinearPlan plan_linear_bf16(int M, int K, long long T) {
-  LinearPlan q{LINEAR_TILE_LARGE, 256, 256, 1, (K + 63) / 64, 0};
-  if (T <= 64) {
-    q.kind = LINEAR_FEW;
-    q.bm = T <= 32 ? 16 : 32;
-    return q;
-  }
-  const auto tiles = [&](int b) { return (long long)((M + b - 1) / b) * ((T + b - 1) / b); };
-  if (tiles(256) >= 192) return q;
-  q.kind = tiles(128) >= 192 ? LINEAR_TILE : LINEAR_TILE_SMALL;
-  q.bm = q.bn = q.kind == LINEAR_TILE ? 128 : 64;
-  const long long n = tiles(q.bm);
+  LinearPlan best{LINEAR_FEW, T <= 32 ? 16 : 32, 64, 1, 0, 0};
+  if (T <= 64) return best;
+  const struct { int kind, b, per; double us[4]; } shapes[3] = {
+      {LINEAR_TILE_LARGE, 256, 1, {1.8}}, {LINEAR_TILE, 128, 2, {0.65, 1.25}}, {LINEAR_TILE_SMALL, 64, 4, {0.42, 0.6, 0.75, 0.9}}};
   const int all = (K + 63) / 64;
-  // parts of four pairs of steps at least, until the chip has a workgroup for each CU
-  while (n * q.splits < 256 && all / (q.splits * 2) >= 4) q.splits *= 2;
-  q.pairs = (all + q.splits - 1) / q.splits;
-  q.splits = (all + q.pairs - 1) / q.pairs;
-  if (q.splits > 1) q.part_bytes = (size_t)q.splits * M * ((T + 7) / 8 * 8) * 4;
-  return q;
+  double least = 0.0;
+  for (const auto& s : shapes) {
+    const long long n = ((M + s.b - 1) / s.b) * ((T + s.b - 1) / s.b);
+    for (int parts = 1; parts <= 16 && parts <= all; parts *= 2) {
+      const int pairs = (all + parts - 1) / parts, used = (all + pairs - 1) / pairs;
+      const long long blocks = n * used, round = 256LL * s.per, left = blocks % round;
+      if (used > 1 && blocks > round) break;
+      const double us = pairs * (double(blocks / round) * s.us[s.per - 1] + (left ? s.us[(left + 255) / 256 - 1] : 0.0)) +
+                        (used > 1 ? 1.5 + 8e-6 / 4.5 * used * (double)M * (double)T : 0.0);
+      if (least > 0.0 && us >= least) continue;
+      least = us;
+      best = LinearPlan{s.kind, s.b, s.b, used, pairs, used > 1 ? (size_t)used * M * ((T + 7) / 8 * 8) * 4 : 0};
+    }
+  }
+  return best;
 }
 
 template <typename YT>

@@ -21,7 +21,7 @@ __device__ __forceinline__ float lanes_by(float a) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a), CTL, 0xf, 0xf, false));
 }
 // the sum of the four rows of 16 lanes, in each of them
-__device__ __forceinline__ float both_rows(float a) {
+__device__ __forceinline__ float all_rows(float a) {
   const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, a), false, false);
   const unsigned r0 = r[0], r1 = r[1];
   const float b = __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1);
@@ -37,7 +37,10 @@ __global__ __launch_bounds__(1024) void layer_norm_kernel(const NormP p) {
   constexpr int VEC = 16 / sizeof(E);
   __shared__ __attribute__((aligned(16))) float part[16][16 * VEC], whole[16 * VEC];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c = tid & (p.ct - 1), bits = 31 - __clz(p.ct), r0 = tid >> bits, rl = 1024 >> bits;
-  const long long t0 = ((long long)blockIdx.x * p.ct + c) * VEC;
+  // workgroups go to the eight XCDs in turn: the g neighbours that share a line of memory go to one, and those that run at a time still lie side by side
+  const unsigned g = p.ct < 8 ? 8 / p.ct : 1, b0 = blockIdx.x / (8 * g) * (8 * g), in_g = blockIdx.x - b0;
+  const long long at = b0 + 8 * g <= gridDim.x ? b0 + (in_g & 7) * g + (in_g >> 3) : blockIdx.x;
+  const long long t0 = (at * p.ct + c) * VEC;
   const bool in = t0 < p.T;
   const E* x = (const E*)p.X + (in ? t0 : 0);
   E* y = (E*)p.Y + t0;
@@ -48,6 +51,16 @@ __global__ __launch_bounds__(1024) void layer_norm_kernel(const NormP p) {
     v[i] = uintx4{0u, 0u, 0u, 0u};
     if (j < p.d) v[i] = *(const uintx4*)(x + (long long)j * p.ldx);
   }
+  // asked for early where there are registers for it
+  constexpr int EARLY = NR <= 4 ? NR : 1;
+  float gain[EARLY], bias[EARLY];
+  if (NR <= 4)
+#pragma unroll
+    for (int i = 0; i < EARLY; ++i) {
+      const int j = min(r0 + i * rl, p.d - 1);
+      gain[i] = p.gain ? p.gain[j] : 1.0f;
+      bias[i] = p.bias ? p.bias[j] : 0.0f;
+    }
   typedef E vec __attribute__((ext_vector_type(VEC)));
   // sums over a column's threads, in each of them: the wavefront's by exchange, the workgroup's through LDS, in one order
   auto total = [&](float (&a)[VEC]) {
@@ -57,7 +70,7 @@ __global__ __launch_bounds__(1024) void layer_norm_kernel(const NormP p) {
       if (p.ct <= 2) a[e] += lanes_by<0x4e>(a[e]);
       if (p.ct <= 4) a[e] += lanes_by<0x124>(a[e]);
       if (p.ct <= 8) a[e] += lanes_by<0x128>(a[e]);
-      a[e] = both_rows(a[e]);
+      a[e] = all_rows(a[e]);
     }
     if (lane < p.ct)
 #pragma unroll
@@ -111,11 +124,11 @@ __global__ __launch_bounds__(1024) void layer_norm_kernel(const NormP p) {
     const int j = r0 + i * rl;
     if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
     if (j >= p.d) continue;
-    const float g = p.gain ? p.gain[j] : 1.0f, b = p.bias ? p.bias[j] : 0.0f;
+    const float g1 = NR <= 4 ? gain[NR <= 4 ? i : 0] : (p.gain ? p.gain[j] : 1.0f), b1 = NR <= 4 ? bias[NR <= 4 ? i : 0] : (p.bias ? p.bias[j] : 0.0f);
     const vec f = __builtin_bit_cast(vec, v[i]);
     float o[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) o[e] = norm_shift((float)f[e], mean[e], rs[e], g, b);
+    for (int e = 0; e < VEC; ++e) o[e] = norm_shift((float)f[e], mean[e], rs[e], g1, b1);
     if (t0 + VEC <= p.T) store_floats<VEC>(y + (long long)j * p.ldy, o);
     else
 #pragma unroll
@@ -216,7 +229,7 @@ extern "C" strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype 
   if (!token_ld(ldx, T) || !token_ld(ldy, T)) return fail(ctx, STRP_EINVAL, "layer_norm: leading dimensions must be multiples of 8 and not below T");
   if (!ptr16(X) || !ptr16(Y)) return fail(ctx, STRP_EINVAL, "layer_norm: X or Y not 16-byte aligned");
   if (X == Y && ldx != ldy) return fail(ctx, STRP_EINVAL, "layer_norm: Y is X with another leading dimension");
-  if (T > (1LL << 34)) return fail(ctx, STRP_EINVAL, "layer_norm: more than 2^34 tokens");
+  if (T > (1LL << 31)) return fail(ctx, STRP_EINVAL, "layer_norm: more than 2^31 tokens");
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "layer_norm: device %d cannot be made current", ctx->device);
   const NormP p{X, Y, gain, bias, d, T, ldx, ldy, (float)eps, 0};

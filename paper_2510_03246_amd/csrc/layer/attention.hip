@@ -183,43 +183,42 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
 
 __device__ const unsigned zero_chunk[4] = {0u, 0u, 0u, 0u};
 
-// Products of bf16 (v_mfma_f32_32x32x16_bf16).  NW wavefronts of 32 QT queries, keys 64 at a time, the next tile of K and V on its way to LDS
-// while one is worked on.  S = K^T Q has a query to a lane.  The fragments of K are read turned (K lies with its tokens contiguous), in quads of keys, and
-// which quads a lane's rows are is free: with the middle bits of a quad's number exchanged, register e of S is key 16 (e / 8) + 8 (lane / 32) + e % 8, so eight
-// registers of P are a second operand of V P as they are and the fragment of V beside it is 16 contiguous bytes.
-// The chunks of 16 bytes in a row of K or V lie in LDS in an order that depends on the row, so that what is read at once lies in different banks.
-template <int DHP, int QT, int NW>
-__global__ __launch_bounds__(64 * NW, QT == 1 ? 2 : 1) void attention_bf16_kernel(const AttnP p) {
-  constexpr int KT = 64, NC = DHP / 32, NS = DHP / 16, TILE = DHP * 128, STAGE = 2 * TILE, PIECES = DHP / 4, LPW = PIECES / NW, BQ = 32 * QT * NW;
-  static_assert(PIECES % (2 * NW) == 0, "pieces of a tile");
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE];
+// Products of bf16 (v_mfma_f32_32x32x16_bf16).  NW wavefronts of 32 queries, keys 64 at a time.  S = K^T Q has a query to a lane.  The fragments of K are read
+// turned (K lies with its tokens contiguous), in quads of keys, and which quads a lane's rows are is free: with the middle bits of a quad's number exchanged,
+// register e of S is key 16 (e / 8) + 8 (lane / 32) + e % 8, so eight registers of P are a second operand of V P as they are and the fragment of V beside it is
+// 16 contiguous bytes.  The chunks of 16 bytes in a row of K or V lie in LDS in an order that depends on the row, so that what is read at once lies in
+// different banks.
+// What bounds it is the vector unit (an exponential, a multiply-add, an addition, half a maximum and half a conversion for a score) and, at 128 channels a head, as
+// much the matrix cores.  So that either has work while the other waits, the scores of the next tile are multiplied beside the softmax of this one, and V P follows
+// it a quarter of the keys at a time.  K runs a tile ahead of V: LDS has RING tiles of each.
+template <int DHP, int NW, int RING, int WPS>
+__global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const AttnP p) {
+  constexpr int KT = 64, NC = DHP / 32, NS = DHP / 16, TILE = DHP * 128, LH = DHP / 8 / NW, BQ = 32 * NW;      // LH: KBs of a tile of K or V that a wavefront moves
+  static_assert(DHP % (8 * NW) == 0, "whole pieces for every wavefront");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * RING * TILE];
   __shared__ int lows[NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
   // the tiles with most keys first; the heads that an XCD gets are neighbours where eight divides them, since neighbours share K and V
   const int slot = (int)blockIdx.x % p.heads, tile = p.tiles - 1 - (int)blockIdx.x / p.heads;
   const int head = p.heads % 8 == 0 ? (slot & 7) * (p.heads >> 3) + (slot >> 3) : slot;
-  const int q0 = tile * BQ;
-  int q[QT], lo[QT];
-  int wlo = 0x7fffffff;
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    q[t] = q0 + (wave * QT + t) * 32 + l32;
-    lo[t] = first_key(p, q[t]);
-    if (lo[t] <= q[t]) wlo = min(wlo, lo[t]);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) wlo = min(wlo, __shfl_xor(wlo, o, 64));
-  if (lane == 0) lows[wave] = wlo;
-  bf16x8 qf[QT][NS];
-#pragma unroll
-  for (int t = 0; t < QT; ++t)
+  const int q0 = tile * BQ, q = q0 + wave * 32 + l32;
+  bf16x8 qf[NS];
+  {
+    const __bf16* Q = (const __bf16*)p.Q + (long long)head * p.dh * p.ldq + (q < p.T ? q : 0);
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int d = 16 * s + 8 * h + e;
-        qf[t][s][e] = lo[t] <= q[t] && d < p.dh ? ((const __bf16*)p.Q)[((long long)head * p.dh + d) * p.ldq + q[t]] : (__bf16)0.0f;
+        const __bf16 v = Q[(long long)(d < p.dh ? d : 0) * p.ldq];
+        qf[s][e] = d < p.dh ? v : (__bf16)0.0f;
       }
+  }
+  const int lo = first_key(p, q);
+  int wlo = lo <= q ? lo : 0x7fffffff;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) wlo = min(wlo, __shfl_xor(wlo, o, 64));
+  if (lane == 0) lows[wave] = wlo;
   __syncthreads();
   int low = lows[0];
 #pragma unroll
@@ -230,181 +229,211 @@ __global__ __launch_bounds__(64 * NW, QT == 1 ? 2 : 1) void attention_bf16_kerne
   const int first = low & ~(KT - 1), steps = (last - first) / KT + 1;
 
   const int kv = kv_head_of(p, head);
-  // a wavefront moves eight rows of K and eight of V at a time, 8 NW rows apart: lane l has a chunk of row l / 8 of them
+  // a wavefront moves eight rows of K or of V at a time, 8 NW rows apart: lane l has a chunk of row l / 8 of them
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const int row0 = 8 * wave + (lane >> 3);
   const int colK = first + 8 * ((lane & 7) ^ (((row0 >> 1) & 1) << 2)), colV = first + 8 * ((lane & 7) ^ ((row0 >> 1) & 7));
   const __bf16* srcK = (const __bf16*)p.K + ((long long)kv * p.dh + row0) * p.ldk + colK;
   const __bf16* srcV = (const __bf16*)p.V + ((long long)kv * p.dh + row0) * p.ldv + colV;
-  auto issue = [&](int s) {                      // rows behind the head's and tokens behind the last are zeros
-    const unsigned at = base + (unsigned)(s & 1) * STAGE + (unsigned)wave * 1024;
-    const bool inK = colK + s * KT < (int)p.T, inV = colV + s * KT < (int)p.T;
+  // rows behind the head's and tokens behind the last are zeros; tiles behind the last are not looked at
+  auto issue = [&](const __bf16* src, int col, long long ld, int s, unsigned at) {
+    const bool in = col + s * KT < (int)p.T;
 #pragma unroll
-    for (int i = 0; i < LPW / 2; ++i) {
-      const bool row = row0 + 8 * NW * i < p.dh;
-      const __bf16* k = srcK + (long long)(8 * NW * i) * p.ldk + s * KT;
-      const __bf16* v = srcV + (long long)(8 * NW * i) * p.ldv + s * KT;
-      copy_to_lds(row && inK ? (const void*)k : (const void*)zero_chunk, at + NW * 1024 * i);
-      copy_to_lds(row && inV ? (const void*)v : (const void*)zero_chunk, at + TILE + NW * 1024 * i);
+    for (int i = 0; i < LH; ++i) {
+      const __bf16* g = src + (long long)(8 * NW * i) * ld + s * KT;
+      copy_to_lds(in && row0 + 8 * NW * i < p.dh ? (const void*)g : (const void*)zero_chunk, at + (unsigned)wave * 1024 + NW * 1024 * i);
     }
+  };
+  const unsigned baseV = base + RING * TILE;
+  unsigned toK = base, toV = baseV;              // where the next tile goes
+  auto issue_k = [&](int s) {
+    issue(srcK, colK, p.ldk, s, toK);
+    toK = toK == base + (RING - 1) * TILE ? base : toK + TILE;
+  };
+  auto issue_v = [&](int s) {
+    issue(srcV, colV, p.ldv, s, toV);
+    toV = toV == baseV + (RING - 1) * TILE ? baseV : toV + TILE;
   };
   // fragments of K: row 16 s + 8 h + (lane % 16) / 4 (+ 4), quad of keys; of V: row 32 c + lane % 32, chunk 2 k + h
   const int r4 = 4 * ((lane >> 4) & 1) + (lane & 3), key4 = (r4 & 4) | ((r4 & 1) << 1) | ((r4 >> 1) & 1), kr = (lane & 15) >> 2;
   const unsigned offK = (unsigned)((8 * h + kr) * 128 + (kr >> 1) * 64 + (key4 >> 1) * 16 + (key4 & 1) * 8);
-  const unsigned offV = (unsigned)(TILE + l32 * 128 + ((((l32 >> 1) & 7) ^ h) * 16));
+  const unsigned offV = (unsigned)(l32 * 128 + ((((l32 >> 1) & 7) ^ h) * 16));
+  auto frag_k = [&](unsigned at, int d, int u) {
+    const unsigned a = at + (offK ^ (unsigned)(64 * u)) + 2048 * d;
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_turned(a), read_turned(a + 512), 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto frag_v = [&](unsigned at, int c, int k) { return *(const __attribute__((address_space(3))) bf16x8*)(size_t)(at + (offV ^ (unsigned)(32 * k)) + 4096 * c); };
 
-  floatx16 O[QT][NC];
-  float m[QT], l[QT];
+  floatx16 O[NC];
+  float m = -INFINITY, l = 0.0f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    m[t] = -INFINITY;
-    l[t] = 0.0f;
+  for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int e = 0; e < 16; ++e) O[c][e] = 0.0f;
+  struct Scores { floatx16 u[2]; };
+  auto clear = [&](Scores& S) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) O[t][c][e] = 0.0f;
-  }
-  issue(0);
-#pragma unroll 1
-  for (int s = 0; s < steps; ++s) {
-    wait_loads<0>();
-    __syncthreads();                             // this tile is there, and nobody reads the other one any more
-    if (s + 1 < steps) issue(s + 1);
-    const int k0 = first + s * KT;
-    const unsigned at = base + (unsigned)(s & 1) * STAGE;
-    bool sees = false, whole = true;
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      sees = sees || (lo[t] <= q[t] && q[t] >= k0 && lo[t] < k0 + KT);
-      whole = whole && lo[t] <= k0 && q[t] >= k0 + KT - 1;
+      for (int e = 0; e < 16; ++e) S.u[u][e] = 0.0f;
+  };
+  auto sees = [&](int s) { return __builtin_amdgcn_ballot_w64(lo <= q && q >= first + s * KT && lo < first + (s + 1) * KT) != 0; };
+  auto scores = [&](Scores& S, unsigned at, int d0, int d1) {
+#pragma unroll
+    for (int d = d0; d < d1; ++d)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) S.u[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_k(at, d, u), qf[d], S.u[u], 0, 0, 0);
+  };
+  // all of them; not every fragment at once, for the registers
+  auto all_scores = [&](Scores& S, unsigned at) {
+#pragma unroll
+    for (int d = 0; d < NS; d += 2) {
+      scores(S, at, d, d + 2);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (!__any(sees)) continue;
-    whole = __all(whole);
-    floatx16 S[QT][2];
+  };
+  // the running maximum with a tile's scores, what is held rescaled to it; returns what is to be taken from a score in powers of two
+  auto raise = [&](const Scores& S) {
+    float mt = m;
 #pragma unroll
-    for (int t = 0; t < QT; ++t)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int e = 0; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, S.u[u][e]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, mt), __builtin_bit_cast(unsigned, mt), false, false);
+    const unsigned b0 = both[0], b1 = both[1];
+    mt = __builtin_elementwise_maximum(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+    // What a query holds stays as it is until its maximum has grown past 2^8 times: probabilities of up to 256 are as good as those below 1.
+    const bool grown = !((mt - m) * p.scale_log2e <= 8.0f || mt == -INFINITY);
+    if (__builtin_amdgcn_ballot_w64(grown)) {
+      const float fac = grown ? __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e) : 1.0f;
+      l *= fac;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) S[t][u][e] = 0.0f;
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int d = 0; d < NS; ++d)
+        for (int e = 0; e < 16; ++e) O[c][e] *= fac;
+      m = grown ? mt : m;
+    }
+    return m == -INFINITY ? 0.0f : m * p.scale_log2e;
+  };
+  // probabilities of the quarter k of a tile's keys
+  auto quarter = [&](const Scores& S, int k, float ref) {
+    bf16x8 P;
+    float x[8];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const unsigned a = at + (offK ^ (unsigned)(64 * u)) + 2048 * d;
-        const bf16x8 k = __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_turned(a), read_turned(a + 512), 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int t = 0; t < QT; ++t) S[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[t][d], S[t][u], 0, 0, 0);
-        if (d & 1 && u) __builtin_amdgcn_sched_barrier(0);     // or every fragment is asked for at once, and the registers do not go round
-      }
-    bf16x8 P[QT][4];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
+    for (int e = 0; e < 8; ++e) {
+      x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + e], p.scale_log2e, -ref));
+      P[e] = (__bf16)x[e];
+    }
+    l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    asm volatile("" : "+v"(l));                  // now: or every probability stays in a register to the end of the tile
+    return P;
+  };
+  unsigned atK = base, atV = baseV;              // the tile of K whose scores come next, the tile of V
+  // Tile s, whose scores are in S; those of the next one go to N.
+  auto tile_step = [&](int s, Scores& S, Scores& N) {
+    wait_loads<(RING - 2) * 2 * LH>();
+    __builtin_amdgcn_s_barrier();                // K of the next tile and V of this one are there, and nobody reads those before them any more
+    issue_k(s + RING);
+    issue_v(s + RING - 1);
+    atK = atK == base + (RING - 1) * TILE ? base : atK + TILE;
+    const int k0 = first + s * KT;
+    if (sees(s) || sees(s + 1)) {                // or the scores that follow are of no tile, but none of them is looked at
+      clear(N);
+      const bool whole = __builtin_amdgcn_ballot_w64(lo > k0 || q < k0 + KT - 1) == 0;
+      const int from = lo - k0 - 8 * h, to = q - k0 - 8 * h;
       if (!whole)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int key = k0 + 32 * u + 16 * (e >> 3) + 8 * h + (e & 7);
-            if (key < lo[t] || key > q[t]) S[t][u][e] = -INFINITY;
+            const int key = 32 * u + 16 * (e >> 3) + (e & 7);          // and k0 + 8 h
+            S.u[u][e] = key < from || key > to ? -INFINITY : S.u[u][e];
+            __builtin_amdgcn_sched_barrier(0);                         // one comparison at a time, or their results take the scalar registers
           }
-      float mt = m[t];
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, S[t][u][e]);
-      {
-        const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, mt), __builtin_bit_cast(unsigned, mt), false, false);
-        const unsigned b0 = both[0], b1 = both[1];
-        mt = __builtin_elementwise_maximum(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
-      }
-      const float ref = mt == -INFINITY ? 0.0f : mt * p.scale_log2e;
-      if (__any(!(mt == m[t]))) {
-        const float fac = __builtin_amdgcn_exp2f(m[t] * p.scale_log2e - ref);
-        l[t] *= fac;
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) O[t][c][e] *= fac;
-        m[t] = mt;
-      }
-      float sum = 0.0f;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][u][e], p.scale_log2e, -ref));
-          sum += x;
-          P[t][2 * u + (e >> 3)][e & 7] = (__bf16)x;
-        }
-      l[t] += sum;
-    }
-    // Where some key is not seen by every query, a value that is not finite would reach those too, by a probability of zero: such values are left out of
-    // the products and added to the results of the queries that see them.
-    bool odd = false;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
+      const float ref = raise(S);
+      // Where some key is not seen by every query, a value that is not finite would reach those too, by a probability of zero: such values are left out
+      // of the products and added to the results of the queries that see them.
+      bool odd = false;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        bf16x8 v = *(const __attribute__((address_space(3))) bf16x8*)(size_t)(at + (offV ^ (unsigned)(32 * k)) + 4096 * c);
-        if (!whole) {
-          typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
-          const ushort8 bits = __builtin_bit_cast(ushort8, v), size = bits & (unsigned short)0x7fff;
-          ushort8 keep;
+        bf16x8 v[NC];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) keep[e] = size[e] >= 0x7f80 ? 0 : 0xffff;
-          const ushort8 fin = bits & keep;
-          const uintx4 lost = __builtin_bit_cast(uintx4, fin ^ bits);
-          odd = odd || (lost[0] | lost[1] | lost[2] | lost[3]) != 0;
-          v = __builtin_bit_cast(bf16x8, fin);
-        }
+        for (int c = 0; c < NC; ++c) v[c] = frag_v(atV, c, k);
+        scores(N, atK, k * NS / 4, (k + 1) * NS / 4);
+        const bf16x8 P = quarter(S, k, ref);
+        if (!whole)
 #pragma unroll
-        for (int t = 0; t < QT; ++t) O[t][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, P[t][k], O[t][c], 0, 0, 0);
-      }
-      if (c & 1) __builtin_amdgcn_sched_barrier(0);
-    }
-    if (__any(odd))
-#pragma unroll 1
-      for (int i = 0; i < KT; ++i) {
-        bool seen[QT], some = false;
+          for (int c = 0; c < NC; ++c) {
+            typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
+            const ushort8 bits = __builtin_bit_cast(ushort8, v[c]), size = bits & (unsigned short)0x7fff;
+            ushort8 keep;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          seen[t] = k0 + i >= lo[t] && k0 + i <= q[t];
-          some = some || seen[t];
-        }
-        if (!__any(some)) continue;
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int r = 32 * c + 8 * (e >> 2) + 4 * h + (e & 3);
-            const float v = (float)*(const __attribute__((address_space(3))) __bf16*)(size_t)(at + TILE + r * 128 + (((i >> 3) ^ ((r >> 1) & 7)) * 16) + (i & 7) * 2);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) O[t][c][e] += seen[t] && !(fabsf(v) < INFINITY) ? v : 0.0f;
+            for (int e = 0; e < 8; ++e) keep[e] = size[e] >= 0x7f80 ? 0 : 0xffff;
+            const ushort8 fin = bits & keep;
+            const uintx4 lost = __builtin_bit_cast(uintx4, fin ^ bits);
+            odd = odd || (lost[0] | lost[1] | lost[2] | lost[3]) != 0;
+            v[c] = __builtin_bit_cast(bf16x8, fin);
           }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], P, O[c], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      if (__builtin_amdgcn_ballot_w64(odd))
+#pragma unroll 1
+        for (int i = 0; i < KT; ++i) {
+          const bool seen = k0 + i >= lo && k0 + i <= q;
+          if (!__builtin_amdgcn_ballot_w64(seen)) continue;
+          int half = h;
+          asm volatile("" : "+v"(half));         // or the addresses below are worked out ahead of everything, and kept
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int r = 32 * c + 8 * (e >> 2) + 4 * half + (e & 3);
+              const float v = (float)*(const __attribute__((address_space(3))) __bf16*)(size_t)(atV + r * 128 + (((i >> 3) ^ ((r >> 1) & 7)) * 16) + (i & 7) * 2);
+              O[c][e] += seen && !(fabsf(v) < INFINITY) ? v : 0.0f;
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    atV = atV == baseV + (RING - 1) * TILE ? baseV : atV + TILE;
+  };
+  issue_k(0);
+#pragma unroll
+  for (int s = 0; s < RING - 1; ++s) {
+    issue_k(s + 1);
+    issue_v(s);
   }
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const float inv = 1.0f / (l[t] + __shfl_xor(l[t], 32, 64));
-    if (lo[t] > q[t]) continue;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int r = 32 * c + 8 * (e >> 2) + 4 * h + (e & 3);
-        if (r < p.dh) ((__bf16*)p.C)[((long long)head * p.dh + r) * p.ldc + q[t]] = (__bf16)(O[t][c][e] * inv);
-      }
+  Scores a, b;
+  clear(a);
+  wait_loads<(RING - 1) * 2 * LH>();
+  __builtin_amdgcn_s_barrier();
+  all_scores(a, atK);
+#pragma unroll 1
+  for (int s = 0; s < steps; s += 2) {
+    tile_step(s, a, b);
+    if (s + 1 < steps) tile_step(s + 1, b, a);
   }
+  wait_loads<0>();                               // LDS is not to be written behind the workgroup's end
+  const float inv = 1.0f / (l + __shfl_xor(l, 32, 64));
+  if (lo > q) return;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int r = 32 * c + 8 * (e >> 2) + 4 * h + (e & 3);
+      if (r < p.dh) ((__bf16*)p.C)[((long long)head * p.dh + r) * p.ldc + q] = (__bf16)(O[c][e] * inv);
+    }
 }
 
-template <int QT, int NW>
 static void launch_attention_bf16(strp_ctx* ctx, AttnP p) {
-  p.tiles = (int)((p.T + 32 * QT * NW - 1) / (32 * QT * NW));
-  const dim3 grid((unsigned)(p.tiles * p.heads)), block(64 * NW);
-  if (p.dh <= 64) hipLaunchKernelGGL((attention_bf16_kernel<64, QT, NW>), grid, block, 0, ctx->stream, p);
-  else if (p.dh <= 96) hipLaunchKernelGGL((attention_bf16_kernel<96, QT, NW>), grid, block, 0, ctx->stream, p);
-  else hipLaunchKernelGGL((attention_bf16_kernel<128, QT, NW>), grid, block, 0, ctx->stream, p);
+  const auto go = [&](auto kernel, int bq, int threads) {
+    p.tiles = (int)((p.T + bq - 1) / bq);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles * p.heads)), dim3(threads), 0, ctx->stream, p);
+  };
+  if (p.dh <= 64) go(attention_bf16_kernel<64, 4, 3, 3>, 128, 256);
+  else if (p.dh <= 96) go(attention_bf16_kernel<96, 4, 2, 2>, 128, 256);
+  else go(attention_bf16_kernel<128, 4, 2, 2>, 128, 256);
 }
 
 template <typename E>
@@ -441,7 +470,7 @@ extern "C" strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in
   // the lengths are on the device: the operations of one sequence of all tokens
   const double T = (double)in->T;
   ProfScope ps(ctx, "attention", 2.0 * in->heads * in->d_head * T * (T + 1.0), bytes_of(in->dtype) * T * in->d_head * 2.0 * (in->heads + in->kv_heads));
-  if (in->dtype == STRP_BF16) launch_attention_bf16<1, 4>(ctx, p);
+  if (in->dtype == STRP_BF16) launch_attention_bf16(ctx, p);
   else launch_attention_f32<float>(ctx, p);
   STRP_HIP(ctx, hipGetLastError());
   return STRP_OK;

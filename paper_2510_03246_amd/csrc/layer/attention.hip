@@ -20,6 +20,7 @@ struct AttnP {
   int heads, kv_heads, group, dh, n_seq, tiles;
   long long T, ldq, ldk, ldv, ldc;
   float scale_log2e;
+  int near;          // rows of K and V lie near enough for offsets of 32 bits
 };
 
 // First key of token t's sequence; t + 1 where t is in none.
@@ -215,9 +216,16 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
       }
   }
   const int lo = first_key(p, q);
-  int wlo = lo <= q ? lo : 0x7fffffff;
+  // the wavefront's first key, and the first key from which on every query sees (none, if some query is in no sequence)
+  int wlo = lo <= q ? lo : 0x7fffffff, whi = wlo;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) wlo = min(wlo, __shfl_xor(wlo, o, 64));
+  for (int o = 16; o > 0; o >>= 1) {
+    wlo = min(wlo, __shfl_xor(wlo, o, 64));
+    whi = max(whi, __shfl_xor(whi, o, 64));
+  }
+  wlo = __builtin_amdgcn_readfirstlane(wlo);
+  whi = __builtin_amdgcn_readfirstlane(whi);
+  const int wq = q0 + wave * 32;
   if (lane == 0) lows[wave] = wlo;
   __syncthreads();
   int low = lows[0];
@@ -232,26 +240,36 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   // a wavefront moves eight rows of K or of V at a time, 8 NW rows apart: lane l has a chunk of row l / 8 of them
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const int row0 = 8 * wave + (lane >> 3);
-  const int colK = first + 8 * ((lane & 7) ^ (((row0 >> 1) & 1) << 2)), colV = first + 8 * ((lane & 7) ^ ((row0 >> 1) & 7));
-  const __bf16* srcK = (const __bf16*)p.K + ((long long)kv * p.dh + row0) * p.ldk + colK;
-  const __bf16* srcV = (const __bf16*)p.V + ((long long)kv * p.dh + row0) * p.ldv + colV;
-  // rows behind the head's and tokens behind the last are zeros; tiles behind the last are not looked at
-  auto issue = [&](const __bf16* src, int col, long long ld, int s, unsigned at) {
-    const bool in = col + s * KT < (int)p.T;
+  const int chunkK = 8 * ((lane & 7) ^ (((row0 >> 1) & 1) << 2)), chunkV = 8 * ((lane & 7) ^ ((row0 >> 1) & 7));
+  const __bf16* srcK = (const __bf16*)p.K + (long long)kv * p.dh * p.ldk + first;
+  const __bf16* srcV = (const __bf16*)p.V + (long long)kv * p.dh * p.ldv + first;
+  // Rows behind the head's and tokens behind the last are zeros; tiles behind the last are not looked at.  A tile that is all there is asked for by
+  // lane offsets that stay the same (in 32 bits, if eight rows lie near enough).
+  auto issue = [&](const __bf16* src, int chunk, long long ld, int s, unsigned at) {
+    const __bf16* from = src + s * KT;
+    if (p.dh == DHP && p.near && first + (s + 1) * KT <= (int)p.T) {
+      const unsigned off = (unsigned)((row0 * ld + chunk) * 2);
 #pragma unroll
-    for (int i = 0; i < LH; ++i) {
-      const __bf16* g = src + (long long)(8 * NW * i) * ld + s * KT;
-      copy_to_lds(in && row0 + 8 * NW * i < p.dh ? (const void*)g : (const void*)zero_chunk, at + (unsigned)wave * 1024 + NW * 1024 * i);
+      for (int i = 0; i < LH; ++i) copy_to_lds_from(from + (long long)(8 * NW * i) * ld, off, at + (unsigned)wave * 1024 + NW * 1024 * i);
+    } else {
+      int r = row0;
+      asm volatile("" : "+v"(r));                // rare: its addresses are not worth registers
+      const bool in = first + chunk + s * KT < (int)p.T;
+#pragma unroll
+      for (int i = 0; i < LH; ++i) {
+        const __bf16* g = from + (r + (long long)(8 * NW * i)) * ld + chunk;
+        copy_to_lds(in && r + 8 * NW * i < p.dh ? (const void*)g : (const void*)zero_chunk, at + (unsigned)wave * 1024 + NW * 1024 * i);
+      }
     }
   };
   const unsigned baseV = base + RING * TILE;
   unsigned toK = base, toV = baseV;              // where the next tile goes
   auto issue_k = [&](int s) {
-    issue(srcK, colK, p.ldk, s, toK);
+    issue(srcK, chunkK, p.ldk, s, toK);
     toK = toK == base + (RING - 1) * TILE ? base : toK + TILE;
   };
   auto issue_v = [&](int s) {
-    issue(srcV, colV, p.ldv, s, toV);
+    issue(srcV, chunkV, p.ldv, s, toV);
     toV = toV == baseV + (RING - 1) * TILE ? baseV : toV + TILE;
   };
   // fragments of K: row 16 s + 8 h + (lane % 16) / 4 (+ 4), quad of keys; of V: row 32 c + lane % 32, chunk 2 k + h
@@ -265,7 +283,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   auto frag_v = [&](unsigned at, int c, int k) { return *(const __attribute__((address_space(3))) bf16x8*)(size_t)(at + (offV ^ (unsigned)(32 * k)) + 4096 * c); };
 
   floatx16 O[NC];
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -277,7 +295,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
 #pragma unroll
       for (int e = 0; e < 16; ++e) S.u[u][e] = 0.0f;
   };
-  auto sees = [&](int s) { return __builtin_amdgcn_ballot_w64(lo <= q && q >= first + s * KT && lo < first + (s + 1) * KT) != 0; };
+  auto sees = [&](int s) { return wq + 31 >= first + s * KT && wlo < first + (s + 1) * KT; };      // some query, perhaps
   auto scores = [&](Scores& S, unsigned at, int d0, int d1) {
 #pragma unroll
     for (int d = d0; d < d1; ++d)
@@ -306,7 +324,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     const bool grown = !((mt - m) * p.scale_log2e <= 8.0f || mt == -INFINITY);
     if (__builtin_amdgcn_ballot_w64(grown)) {
       const float fac = grown ? __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e) : 1.0f;
-      l *= fac;
+      l[0] *= fac;
+      l[1] *= fac;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -318,14 +337,16 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   // probabilities of the quarter k of a tile's keys
   auto quarter = [&](const Scores& S, int k, float ref) {
     bf16x8 P;
-    float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + e], p.scale_log2e, -ref));
-      P[e] = (__bf16)x[e];
+    for (int e = 0; e < 8; e += 2) {
+      bf16x2 x;
+#pragma unroll
+      for (int f = 0; f < 2; ++f) x[f] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + e + f], p.scale_log2e, -ref));
+      // the sum of what meets V, in fp32
+      l[e >> 1 & 1] = __builtin_amdgcn_fdot2_f32_bf16(x, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[e >> 1 & 1], false);
+      P[e] = x[0];
+      P[e + 1] = x[1];
     }
-    l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-    asm volatile("" : "+v"(l));                  // now: or every probability stays in a register to the end of the tile
     return P;
   };
   unsigned atK = base, atV = baseV;              // the tile of K whose scores come next, the tile of V
@@ -339,7 +360,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     const int k0 = first + s * KT;
     if (sees(s) || sees(s + 1)) {                // or the scores that follow are of no tile, but none of them is looked at
       clear(N);
-      const bool whole = __builtin_amdgcn_ballot_w64(lo > k0 || q < k0 + KT - 1) == 0;
+      const bool whole = whi <= k0 && wq >= k0 + KT - 1;
       const int from = lo - k0 - 8 * h, to = q - k0 - 8 * h;
       if (!whole)
 #pragma unroll
@@ -354,6 +375,24 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
       // Where some key is not seen by every query, a value that is not finite would reach those too, by a probability of zero: such values are left out
       // of the products and added to the results of the queries that see them.
       bool odd = false;
+      if (!whole) {
+        typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+        ushort2v most = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const uintx4 bits = __builtin_bit_cast(uintx4, frag_v(atV, c, k)) & 0x7fff7fffu;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const unsigned w = bits[e];
+              most = __builtin_elementwise_max(most, __builtin_bit_cast(ushort2v, w));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        odd = most[0] >= 0x7f80 || most[1] >= 0x7f80;
+      }
+      odd = __builtin_amdgcn_ballot_w64(odd) != 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         bf16x8 v[NC];
@@ -361,24 +400,19 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
         for (int c = 0; c < NC; ++c) v[c] = frag_v(atV, c, k);
         scores(N, atK, k * NS / 4, (k + 1) * NS / 4);
         const bf16x8 P = quarter(S, k, ref);
-        if (!whole)
+        if (odd)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
-            const ushort8 bits = __builtin_bit_cast(ushort8, v[c]), size = bits & (unsigned short)0x7fff;
-            ushort8 keep;
+          for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) keep[e] = size[e] >= 0x7f80 ? 0 : 0xffff;
-            const ushort8 fin = bits & keep;
-            const uintx4 lost = __builtin_bit_cast(uintx4, fin ^ bits);
-            odd = odd || (lost[0] | lost[1] | lost[2] | lost[3]) != 0;
-            v[c] = __builtin_bit_cast(bf16x8, fin);
-          }
+            for (int e = 0; e < 8; ++e) {
+              v[c][e] = fabsf((float)v[c][e]) < INFINITY ? v[c][e] : (__bf16)0.0f;
+              __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
         for (int c = 0; c < NC; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], P, O[c], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (__builtin_amdgcn_ballot_w64(odd))
+      if (odd)
 #pragma unroll 1
         for (int i = 0; i < KT; ++i) {
           const bool seen = k0 + i >= lo && k0 + i <= q;
@@ -415,7 +449,10 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     if (s + 1 < steps) tile_step(s + 1, b, a);
   }
   wait_loads<0>();                               // LDS is not to be written behind the workgroup's end
-  const float inv = 1.0f / (l + __shfl_xor(l, 32, 64));
+  const float half = l[0] + l[1];
+  const auto halves = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, half), __builtin_bit_cast(unsigned, half), false, false);
+  const unsigned half0 = halves[0], half1 = halves[1];
+  const float inv = 1.0f / (__builtin_bit_cast(float, half0) + __builtin_bit_cast(float, half1));
   if (lo > q) return;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
@@ -427,6 +464,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
 }
 
 static void launch_attention_bf16(strp_ctx* ctx, AttnP p) {
+  p.near = 64 * p.ldk < (1LL << 31) && 64 * p.ldv < (1LL << 31);
   const auto go = [&](auto kernel, int bq, int threads) {
     p.tiles = (int)((p.T + bq - 1) / bq);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles * p.heads)), dim3(threads), 0, ctx->stream, p);
@@ -465,7 +503,7 @@ extern "C" strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "attention: device %d cannot be made current", ctx->device);
   AttnP p{in->Q, in->K, in->V, in->C, in->seq_start, in->kv_of_head, in->heads, in->kv_heads, in->heads / in->kv_heads, in->d_head, in->n_seq,
-          (int)((in->T + 127) / 128), in->T, in->ldq, in->ldk, in->ldv, in->ldc, in->scale * 1.44269504088896341f};
+          (int)((in->T + 127) / 128), in->T, in->ldq, in->ldk, in->ldv, in->ldc, in->scale * 1.44269504088896341f, 0};
   if (p.group == 0) p.group = 1;
   // the lengths are on the device: the operations of one sequence of all tokens
   const double T = (double)in->T;

@@ -68,6 +68,10 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void copy_to_lds(const void* gptr, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(gptr) : "memory", "m0");
 }
+// the same from a uniform address and a lane's offset in bytes
+__device__ __forceinline__ void copy_to_lds_from(const void* base, unsigned lane_off, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(lane_off), "s"(base) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 // all but the last N loads have arrived
 template <int N>

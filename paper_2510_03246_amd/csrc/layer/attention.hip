@@ -20,7 +20,7 @@ struct AttnP {
   int heads, kv_heads, group, dh, n_seq, tiles;
   long long T, ldq, ldk, ldv, ldc;
   float scale_log2e;
-  int near;          // rows of K and V lie near enough for offsets of 32 bits
+  int near;          // rows of K and V lie near enough for offsets of 32 bits, and come in eights
 };
 
 // First key of token t's sequence; t + 1 where t is in none.
@@ -247,17 +247,20 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   // lane offsets that stay the same (in 32 bits, if eight rows lie near enough).
   auto issue = [&](const __bf16* src, int chunk, long long ld, int s, unsigned at) {
     const __bf16* from = src + s * KT;
-    if (p.dh == DHP && p.near && first + (s + 1) * KT <= (int)p.T) {
+    if (p.near && first + (s + 1) * KT <= (int)p.T) {
       const unsigned off = (unsigned)((row0 * ld + chunk) * 2);
 #pragma unroll
-      for (int i = 0; i < LH; ++i) copy_to_lds_from(from + (long long)(8 * NW * i) * ld, off, at + (unsigned)wave * 1024 + NW * 1024 * i);
+      for (int i = 0; i < LH; ++i) {
+        const bool rows = 8 * (wave + NW * i) < p.dh;
+        copy_to_lds_from(rows ? (const void*)(from + (long long)(8 * NW * i) * ld) : (const void*)zero_chunk, off & (rows ? ~0u : 0u), at + (unsigned)wave * 1024 + NW * 1024 * i);
+      }
     } else {
-      int r = row0;
-      asm volatile("" : "+v"(r));                // rare: its addresses are not worth registers
-      const bool in = first + chunk + s * KT < (int)p.T;
+      int r = row0, c = chunk;
+      asm volatile("" : "+v"(r), "+v"(c));       // rare: what it works out is not worth registers
+      const bool in = first + c + s * KT < (int)p.T;
 #pragma unroll
       for (int i = 0; i < LH; ++i) {
-        const __bf16* g = from + (r + (long long)(8 * NW * i)) * ld + chunk;
+        const __bf16* g = from + (r + (long long)(8 * NW * i)) * ld + c;
         copy_to_lds(in && r + 8 * NW * i < p.dh ? (const void*)g : (const void*)zero_chunk, at + (unsigned)wave * 1024 + NW * 1024 * i);
       }
     }
@@ -464,7 +467,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
 }
 
 static void launch_attention_bf16(strp_ctx* ctx, AttnP p) {
-  p.near = 64 * p.ldk < (1LL << 31) && 64 * p.ldv < (1LL << 31);
+  p.near = p.dh % 8 == 0 && 64 * p.ldk < (1LL << 31) && 64 * p.ldv < (1LL << 31);
   const auto go = [&](auto kernel, int bq, int threads) {
     p.tiles = (int)((p.T + bq - 1) / bq);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles * p.heads)), dim3(threads), 0, ctx->stream, p);

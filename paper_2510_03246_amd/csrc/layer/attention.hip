@@ -44,35 +44,49 @@ __device__ __forceinline__ int kv_head_of(const AttnP& p, int head) {
   return g < 0 ? 0 : (g < p.kv_heads ? g : p.kv_heads - 1);
 }
 
-// Products of fp32 (v_mfma_f32_32x32x2_f32).  Four wavefronts of 32 queries, keys 64 at a time.  S = K^T Q has a query to a lane (the keys of
-// its 16 registers are 8 (e / 4) + 4 (lane / 32) + e % 4), so the softmax needs one exchange between the lane's two halves, and
-// the registers of P are the second operand of V P as they are.
-template <typename E, int DHP>
+// Products of fp32 (v_mfma_f32_32x32x2_f32).  A workgroup has 64 queries, keys 64 at a time: a wavefront has half of either, and the two that have the same
+// queries put their maxima, sums and results together at the end.  (128 queries and every wavefront on all the keys: 241 us for 8 heads x 80 over prompts of 1000,
+// 513 and 1500 tokens, nearly all of it the row of 24 tiles that the last queries wait for.  32 queries and the four wavefronts on a quarter of the keys each: 190
+// us, and 27 TFLOP/s at 128 channels a head, since that is 16 operations for a byte of L2.)  S = K^T Q has a query to a lane (the keys of its 16 registers are
+// 8 (e / 4) + 4 (lane / 32) + e % 4), so the softmax needs one exchange between the lane's two halves, and the registers of P are the second operand of V P as
+// they are.  What bounds it is the matrix cores, and between tiles the way of K and V to LDS, which a second workgroup on the CU fills.
+template <int DHP>
 __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
   constexpr int KT = 64, PITCH = KT + 4, NC = DHP / 32, CHUNKS = KT / 4;
   __shared__ __attribute__((aligned(16))) float sK[DHP][PITCH], sV[DHP][PITCH];
+  __shared__ float sM[2][32], sL[2][32];
   __shared__ int lows[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, l32 = lane & 31;
-  const int head = blockIdx.y, tile = p.tiles - 1 - (int)blockIdx.x;       // the tiles with most keys first
-  const int q0 = tile * 128, q = q0 + wave * 32 + l32;
-  const int lo = first_key(p, q);
-  const bool some = lo <= q;
-  const int kv = kv_head_of(p, head);
-  const E* Kh = (const E*)p.K + (long long)kv * p.dh * p.ldk;
-  const E* Vh = (const E*)p.V + (long long)kv * p.dh * p.ldv;
-
-  int wlo = some ? lo : 0x7fffffff;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) wlo = min(wlo, __shfl_xor(wlo, o, 64));
-  if (lane == 0) lows[wave] = wlo;
+  static_assert(2 * 32 * 33 <= 64 * PITCH, "the other half's results lie where K was");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
+  const int part = wave >> 1, group = wave & 1;                            // half of the keys, of the queries
+  const int slot = (int)blockIdx.x % p.heads, tile = p.tiles - 1 - (int)blockIdx.x / p.heads;       // the tiles with most keys first
+  const int head = p.heads % 8 == 0 ? (slot & 7) * (p.heads >> 3) + (slot >> 3) : slot;
+  const int q0 = tile * 64, q = q0 + group * 32 + l32, kv = kv_head_of(p, head);
   float qf[DHP / 2];
+  {
+    const float* Q = (const float*)p.Q + (long long)head * p.dh * p.ldq + (q < p.T ? q : 0);
 #pragma unroll
-  for (int s = 0; s < DHP / 2; ++s) qf[s] = some && 2 * s + h < p.dh ? (float)((const E*)p.Q)[((long long)head * p.dh + 2 * s + h) * p.ldq + q] : 0.0f;
-  for (int i = tid; i < (DHP - p.dh) * KT; i += 256) sK[p.dh + i / KT][i % KT] = sV[p.dh + i / KT][i % KT] = 0.0f;
+    for (int s = 0; s < DHP / 2; ++s) {
+      const int d = 2 * s + h;
+      const float v = Q[(long long)(d < p.dh ? d : 0) * p.ldq];
+      qf[s] = d < p.dh ? v : 0.0f;
+    }
+  }
+  const int lo = first_key(p, q);
+  int wlo = lo <= q ? lo : 0x7fffffff, whi = wlo;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    wlo = min(wlo, __shfl_xor(wlo, o, 64));
+    whi = max(whi, __shfl_xor(whi, o, 64));
+  }
+  wlo = __builtin_amdgcn_readfirstlane(wlo);
+  whi = __builtin_amdgcn_readfirstlane(whi);
+  const int wq = q0 + group * 32;
+  if (lane == 0) lows[wave] = wlo;
   __syncthreads();
-  const int low = min(min(lows[0], lows[1]), min(lows[2], lows[3]));
+  const int low = min(lows[0], lows[1]);
   if (low == 0x7fffffff) return;                 // no query of this tile is in a sequence
-  const int last = q0 + 127 < (int)(p.T - 1) ? q0 + 127 : (int)(p.T - 1);
+  const int last = q0 + 63 < (int)(p.T - 1) ? q0 + 63 : (int)(p.T - 1);
 
   floatx16 O[NC];
 #pragma unroll
@@ -80,57 +94,61 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) O[c][e] = 0.0f;
   float m = -INFINITY, l = 0.0f;
+  const float* Kh = (const float*)p.K + (long long)kv * p.dh * p.ldk;
+  const float* Vh = (const float*)p.V + (long long)kv * p.dh * p.ldv;
+  // the next tile is asked for into registers while this one is worked on
+  constexpr int ROWS = 256 / CHUNKS, NR = DHP / ROWS;
+  const int row0 = tid / CHUNKS, col = (tid % CHUNKS) * 4;
+  floatx4 nk[NR], nv[NR];
+  auto ask = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      nk[i] = nv[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+      const int r = row0 + ROWS * i;
+      if (r < p.dh && k0 + col < p.T) {
+        nk[i] = *(const floatx4*)(Kh + (long long)r * p.ldk + k0 + col);
+        nv[i] = *(const floatx4*)(Vh + (long long)r * p.ldv + k0 + col);
+      }
+    }
+  };
+  ask(low & ~(KT - 1));
+#pragma unroll 1
   for (int k0 = low & ~(KT - 1); k0 <= last; k0 += KT) {
     __syncthreads();
-#pragma unroll 2
-    for (int i = tid; i < p.dh * CHUNKS; i += 256) {
-      const int r = i / CHUNKS, c = (i % CHUNKS) * 4;
-      float k[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (k0 + c < p.T) {
-        load_floats<4>(Kh + (long long)r * p.ldk + k0 + c, k);
-        load_floats<4>(Vh + (long long)r * p.ldv + k0 + c, v);
-      }
-      *(floatx4*)&sK[r][c] = floatx4{k[0], k[1], k[2], k[3]};
-      *(floatx4*)&sV[r][c] = floatx4{v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      *(floatx4*)&sK[row0 + ROWS * i][col] = nk[i];
+      *(floatx4*)&sV[row0 + ROWS * i][col] = nv[i];
     }
     __syncthreads();
-    if (!__any(some && q >= k0 && lo < k0 + KT)) continue;               // nothing here that this wavefront sees
-    const bool whole = __all(some && lo <= k0 && q >= k0 + KT - 1);
-    floatx16 S[2];
+    if (k0 + KT <= last) ask(k0 + KT);
+    const int k1 = k0 + 32 * part;
+    if (wq + 31 < k1 || wlo >= k1 + 32) continue;                          // nothing here that this wavefront sees
+    const bool whole = whi <= k1 && wq >= k1 + 31;
+    floatx16 S;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) S[u][e] = 0.0f;
+    for (int e = 0; e < 16; ++e) S[e] = 0.0f;
 #pragma unroll
     for (int s = 0; s < DHP / 2; ++s)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) S[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(sK[2 * s + h][32 * u + l32], qf[s], S[u], 0, 0, 0);
-    float mt = -INFINITY;
-    if (!whole) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = k0 + 32 * u + 8 * (e >> 2) + 4 * h + (e & 3);
-          if (key < lo || key > q) S[u][e] = -INFINITY;
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, S[u][e]);
-    mt = __builtin_elementwise_maximum(mt, __shfl_xor(mt, 32, 64));
-    const float mn = __builtin_elementwise_maximum(m, mt), ref = mn == -INFINITY ? 0.0f : mn * p.scale_log2e;
-    const float fac = __builtin_amdgcn_exp2f(m * p.scale_log2e - ref);
-    m = mn;
-    float sum = 0.0f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
+      if (s < DHP / 2 - 16 || 2 * s < p.dh) S = __builtin_amdgcn_mfma_f32_32x32x2f32(sK[2 * s + h][32 * part + l32], qf[s], S, 0, 0, 0);
+    if (!whole)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        S[u][e] = __builtin_amdgcn_exp2f(S[u][e] * p.scale_log2e - ref);
-        sum += S[u][e];
+        const int key = k1 + 8 * (e >> 2) + 4 * h + (e & 3);
+        if (key < lo || key > q) S[e] = -INFINITY;
       }
+    float mt = m;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, S[e]);
+    mt = __builtin_elementwise_maximum(mt, __shfl_xor(mt, 32, 64));
+    const float ref = mt == -INFINITY ? 0.0f : mt * p.scale_log2e, fac = __builtin_amdgcn_exp2f(m * p.scale_log2e - ref);
+    m = mt;
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      S[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[e], p.scale_log2e, -ref));
+      sum += S[e];
+    }
     l = l * fac + sum;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -142,44 +160,60 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int g = 0; g < 4; ++g) {
+        floatx4 v = *(const floatx4*)&sV[32 * c + l32][32 * part + 8 * g + 4 * h];
+        if (!whole)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          floatx4 v = *(const floatx4*)&sV[32 * c + l32][32 * u + 8 * g + 4 * h];
-          if (!whole)
+          for (int e = 0; e < 4; ++e) {
+            const bool fin = fabsf(v[e]) < INFINITY;
+            odd = odd || !fin;
+            v[e] = fin ? v[e] : 0.0f;
+          }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const bool fin = fabsf(v[e]) < INFINITY;
-              odd = odd || !fin;
-              v[e] = fin ? v[e] : 0.0f;
-            }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], S[u][4 * g + e], O[c], 0, 0, 0);
-        }
-    if (__any(odd))
+        for (int e = 0; e < 4; ++e) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], S[4 * g + e], O[c], 0, 0, 0);
+      }
+    if (__builtin_amdgcn_ballot_w64(odd))
 #pragma unroll 1
-      for (int i = 0; i < KT; ++i) {
-        const bool seen = k0 + i >= lo && k0 + i <= q;
-        if (!__any(seen)) continue;
+      for (int i = 0; i < 32; ++i) {
+        const bool seen = k1 + i >= lo && k1 + i <= q;
+        if (!__builtin_amdgcn_ballot_w64(seen)) continue;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float v = sV[32 * c + 8 * (e >> 2) + 4 * h + (e & 3)][i];
+            const float v = sV[32 * c + 8 * (e >> 2) + 4 * h + (e & 3)][32 * part + i];
             O[c][e] += seen && !(fabsf(v) < INFINITY) ? v : 0.0f;
           }
       }
   }
+  // the second half of the keys to the first: the results 32 channels at a time
   l += __shfl_xor(l, 32, 64);
-  const float inv = 1.0f / l;
-  if (!some) return;
+  __syncthreads();
+  if (part == 1 && h == 0) {
+    sM[group][l32] = m;
+    sL[group][l32] = l;
+  }
+  float(*other)[32][33] = (float(*)[32][33])&sK[0][0];
+  __syncthreads();
+  const float m1 = sM[group][l32], l1 = sL[group][l32], most = __builtin_elementwise_maximum(m, m1);
+  // a wavefront that saw no key has a sum and results of zero
+  const float f0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - most) * p.scale_log2e), f1 = m1 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m1 - most) * p.scale_log2e);
+  const float inv = 1.0f / (f0 * l + f1 * l1);
+  float* C = (float*)p.C + (long long)head * p.dh * p.ldc + q;
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int c = 0; c < NC; ++c) {
+    if (part == 1)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int r = 32 * c + 8 * (e >> 2) + 4 * h + (e & 3);
-      if (r < p.dh) ((E*)p.C)[((long long)head * p.dh + r) * p.ldc + q] = (E)(O[c][e] * inv);
-    }
+      for (int e = 0; e < 16; ++e) other[group][8 * (e >> 2) + 4 * h + (e & 3)][l32] = O[c][e];
+    __syncthreads();
+    if (part == 0 && lo <= q)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int r = 8 * (e >> 2) + 4 * h + (e & 3);
+        if (32 * c + r < p.dh) C[(long long)(32 * c + r) * p.ldc] = (f0 * O[c][e] + f1 * other[group][r][l32]) * inv;
+      }
+    __syncthreads();
+  }
 }
 
 __device__ const unsigned zero_chunk[4] = {0u, 0u, 0u, 0u};
@@ -477,12 +511,12 @@ static void launch_attention_bf16(strp_ctx* ctx, AttnP p) {
   else go(attention_bf16_kernel<128, 4, 2, 2>, 128, 256);
 }
 
-template <typename E>
-static void launch_attention_f32(strp_ctx* ctx, const AttnP& p) {
-  const dim3 grid(p.tiles, p.heads), block(256);
-  if (p.dh <= 64) hipLaunchKernelGGL((attention_f32_kernel<E, 64>), grid, block, 0, ctx->stream, p);
-  else if (p.dh <= 96) hipLaunchKernelGGL((attention_f32_kernel<E, 96>), grid, block, 0, ctx->stream, p);
-  else hipLaunchKernelGGL((attention_f32_kernel<E, 128>), grid, block, 0, ctx->stream, p);
+static void launch_attention_f32(strp_ctx* ctx, AttnP p) {
+  p.tiles = (int)((p.T + 63) / 64);
+  const dim3 grid((unsigned)(p.tiles * p.heads)), block(256);
+  if (p.dh <= 64) hipLaunchKernelGGL((attention_f32_kernel<64>), grid, block, 0, ctx->stream, p);
+  else if (p.dh <= 96) hipLaunchKernelGGL((attention_f32_kernel<96>), grid, block, 0, ctx->stream, p);
+  else hipLaunchKernelGGL((attention_f32_kernel<128>), grid, block, 0, ctx->stream, p);
 }
 
 }  // namespace strp
@@ -502,17 +536,17 @@ extern "C" strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in
   if (!token_ld(in->ldq, in->T) || !token_ld(in->ldk, in->T) || !token_ld(in->ldv, in->T) || !token_ld(in->ldc, in->T))
     return fail(ctx, STRP_EINVAL, "attention: leading dimensions must be multiples of 8 and not below T");
   if (!ptr16(in->Q) || !ptr16(in->K) || !ptr16(in->V) || !ptr16(in->C)) return fail(ctx, STRP_EINVAL, "attention: Q, K, V or C not 16-byte aligned");
-  if (in->T > 0x7fffff00LL) return fail(ctx, STRP_EINVAL, "attention: T does not fit 31 bits");
+  if (in->T > 0x7fffff00LL || (in->T + 63) / 64 * in->heads > 0x7fffffffLL) return fail(ctx, STRP_EINVAL, "attention: tokens, or tiles of 64 of all heads, do not fit 31 bits");
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "attention: device %d cannot be made current", ctx->device);
   AttnP p{in->Q, in->K, in->V, in->C, in->seq_start, in->kv_of_head, in->heads, in->kv_heads, in->heads / in->kv_heads, in->d_head, in->n_seq,
-          (int)((in->T + 127) / 128), in->T, in->ldq, in->ldk, in->ldv, in->ldc, in->scale * 1.44269504088896341f, 0};
+          0, in->T, in->ldq, in->ldk, in->ldv, in->ldc, in->scale * 1.44269504088896341f, 0};
   if (p.group == 0) p.group = 1;
   // the lengths are on the device: the operations of one sequence of all tokens
   const double T = (double)in->T;
   ProfScope ps(ctx, "attention", 2.0 * in->heads * in->d_head * T * (T + 1.0), bytes_of(in->dtype) * T * in->d_head * 2.0 * (in->heads + in->kv_heads));
   if (in->dtype == STRP_BF16) launch_attention_bf16(ctx, p);
-  else launch_attention_f32<float>(ctx, p);
+  else launch_attention_f32(ctx, p);
   STRP_HIP(ctx, hipGetLastError());
   return STRP_OK;
 }

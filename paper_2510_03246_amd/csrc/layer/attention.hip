@@ -96,7 +96,8 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
   float m = -INFINITY, l = 0.0f;
   const float* Kh = (const float*)p.K + (long long)kv * p.dh * p.ldk;
   const float* Vh = (const float*)p.V + (long long)kv * p.dh * p.ldv;
-  // the next tile is asked for into registers while this one is worked on
+  // the next tile is asked for into registers while this one is worked on, where there are registers for it
+  constexpr bool AHEAD = DHP < 128;
   constexpr int ROWS = 256 / CHUNKS, NR = DHP / ROWS;
   const int row0 = tid / CHUNKS, col = (tid % CHUNKS) * 4;
   floatx4 nk[NR], nv[NR];
@@ -111,17 +112,18 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
       }
     }
   };
-  ask(low & ~(KT - 1));
+  if (AHEAD) ask(low & ~(KT - 1));
 #pragma unroll 1
   for (int k0 = low & ~(KT - 1); k0 <= last; k0 += KT) {
     __syncthreads();
+    if (!AHEAD) ask(k0);
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       *(floatx4*)&sK[row0 + ROWS * i][col] = nk[i];
       *(floatx4*)&sV[row0 + ROWS * i][col] = nv[i];
     }
     __syncthreads();
-    if (k0 + KT <= last) ask(k0 + KT);
+    if (AHEAD && k0 + KT <= last) ask(k0 + KT);
     const int k1 = k0 + 32 * part;
     if (wq + 31 < k1 || wlo >= k1 + 32) continue;                          // nothing here that this wavefront sees
     const bool whole = whi <= k1 && wq >= k1 + 31;

@@ -3,88 +3,162 @@
 
 namespace strp {
 
-// Products of fp32 (v_mfma_f32_32x32x2_f32: an operand of bf16 is widened, which is exact).  Tiles of 128 channels x 128 tokens,
-// four wavefronts of 64 x 64, 16 contraction steps in LDS while the next 16 are on their way to registers.  Rows of X and columns
-// of W from K on are zeros in LDS, whatever memory holds there.
-template <typename WT, typename XT, typename YT>
-__global__ __launch_bounds__(256) void linear_f32_kernel(const LinearP p) {
-  constexpr int BM = 128, BN = 128, BK = 16, PAD = 4;
-  __shared__ float sW[BK][BM + PAD], sX[BK][BN + PAD];
+// Products of fp32 (v_mfma_f32_32x32x2_f32: an operand of bf16 is widened, which is exact).  Tiles of BM channels x BN tokens, four wavefronts of a quarter each, 32
+// contraction steps in LDS, the next 32 on their way there and those behind them to registers.  Rows of X and columns of W from K on are zeros in LDS, whatever memory holds there.
+// What bounds it is the matrix cores (154 TFLOP/s on a large library product), and with few tiles how evenly they go onto the CUs.
+template <int BM, int BN, typename WT, typename XT, typename YT>
+__global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
+  constexpr int BK = 32, PAD = 4, NI = BM / 64, NJ = BN / 64, RW = BM / 32, RX = BK * BN / 1024, XROWS = 1024 / BN;
+  __shared__ __attribute__((aligned(16))) float sW[2][BK][BM + PAD], sX[2][BK][BN + PAD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, l32 = lane & 31;
-  const int m0 = (int)(blockIdx.x % p.tilesM) * BM;
-  const long long n0 = (long long)(blockIdx.x / p.tilesM) * BN;
-  const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-  const int wr = tid >> 2, wk = (tid & 3) * 4;          // W: row wr (+ 64), columns wk .. wk + 3 of the step
-  const int xr = tid >> 5, xt = (tid & 31) * 4;         // X: row xr (+ 8), tokens xt .. xt + 3
-  float w[2][4], x[2][4];
+  const int tiles = p.tilesM * p.tilesN, split = (int)blockIdx.x / tiles, tile = (int)blockIdx.x - split * tiles;
+  const int m0 = tile % p.tilesM * BM;
+  const long long n0 = (long long)(tile / p.tilesM) * BN;
+  const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+  const int k_first = split * p.pairs * 64, k_end = min(p.K, k_first + p.pairs * 64);
+  const int wr = tid >> 3, wk = (tid & 7) * 4;                     // W: row wr (+ 32 i), columns wk .. wk + 3 of the step
+  const int xr = tid / (BN / 4), xt = tid % (BN / 4) * 4;          // X: row xr (+ XROWS i), tokens xt .. xt + 3
+  // as they are read: anything done to them here would wait for them
+  typedef WT wvec __attribute__((ext_vector_type(4)));
+  typedef XT xvec __attribute__((ext_vector_type(4)));
+  wvec w[RW];
+  xvec x[RX];
   auto fetch = [&](int k0) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int m = m0 + wr + 64 * i, k = k0 + wk;
+    for (int i = 0; i < RW; ++i) {
+      const int m = m0 + wr + 32 * i, k = k0 + wk;
+      w[i] = wvec{(WT)0.0f, (WT)0.0f, (WT)0.0f, (WT)0.0f};
+      if (m < p.M && k < k_end) w[i] = *(const wvec*)((const WT*)p.W + (long long)m * p.ldw + k);
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[i][e] = x[i][e] = 0.0f;
-      if (m < p.M && k < p.K) {
-        load_floats<4>((const WT*)p.W + (long long)m * p.ldw + k, w[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[i][e] = k + e < p.K ? w[i][e] : 0.0f;
-      }
-      const int kx = k0 + xr + 8 * i;
-      if (kx < p.K && n0 + xt < p.T) load_floats<4>((const XT*)p.X + (long long)kx * p.ldx + n0 + xt, x[i]);
+    for (int i = 0; i < RX; ++i) {
+      const int k = k0 + xr + XROWS * i;
+      x[i] = xvec{(XT)0.0f, (XT)0.0f, (XT)0.0f, (XT)0.0f};
+      if (k < k_end && n0 + xt < p.T) x[i] = *(const xvec*)((const XT*)p.X + (long long)k * p.ldx + n0 + xt);
     }
   };
-  floatx16 acc[2][2];
+  floatx16 acc[NI][NJ];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  fetch(0);
-  for (int k0 = 0; k0 < p.K; k0 += BK) {
-    __syncthreads();
+  auto put = [&](int k0, int buf) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < RW; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sW[wk + e][wr + 64 * i] = w[i][e];
-      *(floatx4*)&sX[xr + 8 * i][xt] = floatx4{x[i][0], x[i][1], x[i][2], x[i][3]};
+      for (int e = 0; e < 4; ++e) sW[buf][wk + e][wr + 32 * i] = k0 + wk + e < k_end ? (float)w[i][e] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < RX; ++i) *(floatx4*)&sX[buf][xr + XROWS * i][xt] = floatx4{(float)x[i][0], (float)x[i][1], (float)x[i][2], (float)x[i][3]};
+  };
+  // eight steps at a time, the fragments of the next eight read ahead of the products of these
+  struct Frag { float a[4][NI], b[4][NJ]; };
+  auto read = [&](Frag& f, int buf, int g) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) f.a[s][i] = sW[buf][8 * g + 2 * s + h][wm + 32 * i + l32];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) f.b[s][j] = sX[buf][8 * g + 2 * s + h][wn + 32 * j + l32];
     }
-    __syncthreads();
-    if (k0 + BK < p.K) fetch(k0 + BK);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](const Frag& f) {
 #pragma unroll
-    for (int s = 0; s < BK / 2; ++s) {
-      float a[2], b[2];
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        a[i] = sW[2 * s + h][wm + 32 * i + l32];
-        b[i] = sX[2 * s + h][wn + 32 * i + l32];
-      }
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(f.a[s][i], f.b[s][j], acc[i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  fetch(k_first);
+  put(k_first, 0);
+  fetch(k_first + BK);
+  __syncthreads();
+  Frag f0, f1;
+  read(f0, 0, 0);
+  int buf = 0;
+#pragma unroll 1
+  for (int k0 = k_first; k0 < k_end; k0 += BK) {
+    read(f1, buf, 1);
+    multiply(f0);
+    read(f0, buf, 2);
+    // the next run of steps goes to the other buffer, and the one behind it is asked for
+    if (k0 + BK < k_end) {
+      put(k0 + BK, buf ^ 1);
+      fetch(k0 + 2 * BK);
     }
+    multiply(f1);
+    read(f1, buf, 3);
+    multiply(f0);
+    __syncthreads();
+    read(f0, buf ^ 1, 0);                   // past the last run these are not multiplied
+    multiply(f1);
+    buf ^= 1;
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int m = m0 + wm + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
         const long long t = n0 + wn + 32 * j + l32;
         if (m >= p.M || t >= p.T) continue;
+        if (p.splits > 1) {
+          p.part[((long long)split * p.M + m) * p.tp + t] = acc[i][j][e];
+          continue;
+        }
         float y = activate(acc[i][j][e] + (p.bias ? p.bias[m] : 0.0f), p.act);
         if (p.R) y += (float)((const YT*)p.R)[(long long)m * p.ldr + t];
         ((YT*)p.Y)[(long long)m * p.ldy + t] = (YT)y;
       }
 }
 
+// Tile shape and parts of the contraction by the time they take: a CU does one tile's share of the matrix instructions after the other, so what counts is the
+// tiles that the busiest CU has, and a little more traffic for the smaller ones (us for 64 steps of the contraction: 128 x 128 3.6, 128 x 64 1.9, 64 x 64 1.0).  1013 x 1000 over 5003
+// tokens: 320 tiles of 128 x 128 XXX us, 640 of 128 x 64 XXX, 1264 of 64 x 64 XXX.
+static LinearPlan plan_linear_f32(int M, int K, long long T) {
+  const struct { int bm, bn; double us; } shapes[3] = {{128, 128, 3.6}, {128, 64, 1.9}, {64, 64, 1.0}};
+  const int all = (K + 63) / 64;
+  LinearPlan best{};
+  double least = 0.0;
+  for (const auto& s : shapes) {
+    const long long n = (long long)((M + s.bm - 1) / s.bm) * ((T + s.bn - 1) / s.bn);
+    for (int parts = 1; parts <= 16 && parts <= all; parts *= 2) {
+      const int pairs = (all + parts - 1) / parts, used = (all + pairs - 1) / pairs;
+      if (used > 1 && n * used > 512) break;
+      const double us = pairs * s.us * double((n * used + 255) / 256) + (used > 1 ? 1.5 + 8e-6 / 4.5 * used * (double)M * (double)T : 0.0);
+      if (least > 0.0 && us >= least) continue;
+      least = us;
+      best = LinearPlan{0, s.bm, s.bn, used, pairs, used > 1 ? (size_t)used * M * ((T + 7) / 8 * 8) * 4 : 0};
+    }
+  }
+  return best;
+}
+static LinearPlan plan_linear(int M, int K, long long T, int w_dtype, int x_dtype) {
+  return w_dtype == STRP_BF16 && x_dtype == STRP_BF16 ? plan_linear_bf16(M, K, T) : plan_linear_f32(M, K, T);
+}
+
+template <typename WT, typename XT, typename YT>
+static void launch_f32(strp_ctx* ctx, const LinearP& p, const LinearPlan& plan) {
+  const dim3 grid((unsigned)((long long)p.tilesM * p.tilesN * p.splits)), block(256);
+  if (plan.bn == 128) hipLaunchKernelGGL((linear_f32_kernel<128, 128, WT, XT, YT>), grid, block, 0, ctx->stream, p);
+  else if (plan.bm == 128) hipLaunchKernelGGL((linear_f32_kernel<128, 64, WT, XT, YT>), grid, block, 0, ctx->stream, p);
+  else hipLaunchKernelGGL((linear_f32_kernel<64, 64, WT, XT, YT>), grid, block, 0, ctx->stream, p);
+}
 template <typename WT, typename XT>
-static void launch_linear_f32(strp_ctx* ctx, LinearP& p, int y_dtype) {
-  p.tilesM = (p.M + 127) / 128;
-  const dim3 grid((unsigned)(p.tilesM * ((p.T + 127) / 128))), block(256);
-  if (y_dtype == STRP_BF16) hipLaunchKernelGGL((linear_f32_kernel<WT, XT, __bf16>), grid, block, 0, ctx->stream, p);
-  else hipLaunchKernelGGL((linear_f32_kernel<WT, XT, float>), grid, block, 0, ctx->stream, p);
+static void launch_linear_f32(strp_ctx* ctx, LinearP p, const LinearPlan& plan, int y_dtype) {
+  p.tilesM = (p.M + plan.bm - 1) / plan.bm;
+  p.tilesN = (int)((p.T + plan.bn - 1) / plan.bn);
+  p.splits = plan.splits;
+  p.pairs = plan.pairs;
+  p.tp = (p.T + 7) / 8 * 8;
+  if (y_dtype == STRP_BF16) launch_f32<WT, XT, __bf16>(ctx, p, plan);
+  else launch_f32<WT, XT, float>(ctx, p, plan);
+  if (p.splits > 1) launch_linear_join(ctx, p, y_dtype);
 }
 
 }  // namespace strp
@@ -95,8 +169,7 @@ extern "C" {
 
 size_t strp_linear_workspace_bytes(int32_t M, int32_t K, int64_t T, strp_dtype w_dtype, strp_dtype x_dtype) {
   if (M <= 0 || K <= 0 || T <= 0) return 0;
-  if (w_dtype != STRP_BF16 || x_dtype != STRP_BF16) return 0;
-  const size_t part = plan_linear_bf16(M, K, T).part_bytes;
+  const size_t part = plan_linear(M, K, T, w_dtype, x_dtype).part_bytes;
   return part ? part + 4096 : 0;
 }
 
@@ -113,25 +186,22 @@ strp_status strp_linear(strp_ctx* ctx, const strp_linear_in* in) {
   if ((in->M + 63) / 64 * ((in->T + 63) / 64) > 0x7fffffffLL) return fail(ctx, STRP_EINVAL, "linear: more than 2^31 tiles of 64 x 64");
   LinearP p{in->W, in->X, in->bias, in->R, in->Y, in->M, in->K, in->act, in->T, in->ldw, in->ldx, in->ldr, in->ldy};
   p.splits = 1;
-  LinearPlan plan{};
-  const int wb = in->w_dtype == STRP_BF16, xb = in->x_dtype == STRP_BF16;
-  if (wb && xb) {
-    plan = plan_linear_bf16(p.M, p.K, p.T);
-    if (plan.part_bytes) {
-      if (!ctx->ws) return fail(ctx, STRP_ENOMEM, "linear: no workspace set");
-      Arena arena(ctx);
-      STRP_TAKE(ctx, arena, part, float, plan.part_bytes / 4);
-      p.part = part;
-    }
+  const LinearPlan plan = plan_linear(p.M, p.K, p.T, in->w_dtype, in->x_dtype);
+  if (plan.part_bytes) {
+    if (!ctx->ws) return fail(ctx, STRP_ENOMEM, "linear: no workspace set");
+    Arena arena(ctx);
+    STRP_TAKE(ctx, arena, part, float, plan.part_bytes / 4);
+    p.part = part;
   }
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "linear: device %d cannot be made current", ctx->device);
   const double M = in->M, K = in->K, T = (double)in->T;
   ProfScope ps(ctx, "linear", 2.0 * M * K * T, bytes_of(in->w_dtype) * M * K + bytes_of(in->x_dtype) * K * T + bytes_of(in->y_dtype) * M * T * (in->R ? 2 : 1));
+  const bool wb = in->w_dtype == STRP_BF16, xb = in->x_dtype == STRP_BF16;
   if (wb && xb) launch_linear_bf16(ctx, p, plan, in->y_dtype);
-  else if (wb) launch_linear_f32<__bf16, float>(ctx, p, in->y_dtype);
-  else if (xb) launch_linear_f32<float, __bf16>(ctx, p, in->y_dtype);
-  else launch_linear_f32<float, float>(ctx, p, in->y_dtype);
+  else if (wb) launch_linear_f32<__bf16, float>(ctx, p, plan, in->y_dtype);
+  else if (xb) launch_linear_f32<float, __bf16>(ctx, p, plan, in->y_dtype);
+  else launch_linear_f32<float, float>(ctx, p, plan, in->y_dtype);
   STRP_HIP(ctx, hipGetLastError());
   return STRP_OK;
 }

@@ -3,14 +3,14 @@
 
 namespace strp {
 
-// Products of fp32 (v_mfma_f32_32x32x2_f32: an operand of bf16 is widened, which is exact).  Tiles of BM channels x BN tokens, four wavefronts of a quarter each, 32
+// Products of fp32 (v_mfma_f32_16x16x4_f32: an operand of bf16 is widened, which is exact).  Tiles of BM channels x BN tokens, four wavefronts of a quarter each, 32
 // contraction steps in LDS, the next 32 on their way there and those behind them to registers.  Rows of X and columns of W from K on are zeros in LDS, whatever memory holds there.
 // What bounds it is the matrix cores (154 TFLOP/s on a large library product), and with few tiles how evenly they go onto the CUs.
 template <int BM, int BN, typename WT, typename XT, typename YT>
 __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
-  constexpr int BK = 32, PAD = 4, NI = BM / 64, NJ = BN / 64, RW = BM / 32, RX = BK * BN / 1024, XROWS = 1024 / BN;
+  constexpr int BK = 32, PAD = 20, NI = BM / 32, NJ = BN / 32, RW = BM / 32, RX = BK * BN / 1024, XROWS = 1024 / BN;
   __shared__ __attribute__((aligned(16))) float sW[2][BK][BM + PAD], sX[2][BK][BN + PAD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, l32 = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, kq = lane >> 4, l16 = lane & 15;
   const int tiles = p.tilesM * p.tilesN, split = (int)blockIdx.x / tiles, tile = (int)blockIdx.x - split * tiles;
   const int m0 = tile % p.tilesM * BM;
   const long long n0 = (long long)(tile / p.tilesM) * BN;
@@ -37,13 +37,11 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
       if (k < k_end && n0 + xt < p.T) x[i] = *(const xvec*)((const XT*)p.X + (long long)k * p.ldx + n0 + xt);
     }
   };
-  floatx16 acc[NI][NJ];
+  floatx4 acc[NI][NJ];
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   auto put = [&](int k0, int buf) {
 #pragma unroll
     for (int i = 0; i < RW; ++i)
@@ -53,24 +51,24 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
     for (int i = 0; i < RX; ++i) *(floatx4*)&sX[buf][xr + XROWS * i][xt] = floatx4{(float)x[i][0], (float)x[i][1], (float)x[i][2], (float)x[i][3]};
   };
   // eight steps at a time, the fragments of the next eight read ahead of the products of these
-  struct Frag { float a[4][NI], b[4][NJ]; };
+  struct Frag { float a[2][NI], b[2][NJ]; };
   auto read = [&](Frag& f, int buf, int g) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < 2; ++s) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) f.a[s][i] = sW[buf][8 * g + 2 * s + h][wm + 32 * i + l32];
+      for (int i = 0; i < NI; ++i) f.a[s][i] = sW[buf][8 * g + 4 * s + kq][wm + 16 * i + l16];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) f.b[s][j] = sX[buf][8 * g + 2 * s + h][wn + 32 * j + l32];
+      for (int j = 0; j < NJ; ++j) f.b[s][j] = sX[buf][8 * g + 4 * s + kq][wn + 16 * j + l16];
     }
     __builtin_amdgcn_sched_barrier(0);
   };
   auto multiply = [&](const Frag& f) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(f.a[s][i], f.b[s][j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(f.b[s][j], f.a[s][i], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
   fetch(k_first);
@@ -98,23 +96,17 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
     multiply(f1);
     buf ^= 1;
   }
+  // a lane has four consecutive tokens of a channel
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int m = m0 + wm + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
-        const long long t = n0 + wn + 32 * j + l32;
-        if (m >= p.M || t >= p.T) continue;
-        if (p.splits > 1) {
-          p.part[((long long)split * p.M + m) * p.tp + t] = acc[i][j][e];
-          continue;
-        }
-        float y = activate(acc[i][j][e] + (p.bias ? p.bias[m] : 0.0f), p.act);
-        if (p.R) y += (float)((const YT*)p.R)[(long long)m * p.ldr + t];
-        ((YT*)p.Y)[(long long)m * p.ldy + t] = (YT)y;
-      }
+    for (int j = 0; j < NJ; ++j) {
+      const int m = m0 + wm + 16 * i + l16;
+      const long long t = n0 + wn + 16 * j + 4 * kq;
+      if (m >= p.M || t >= p.T) continue;
+      if (p.splits > 1) *(floatx4*)(p.part + ((long long)split * p.M + m) * p.tp + t) = acc[i][j];
+      else finish_quad<YT>(p, acc[i][j], m, t);
+    }
 }
 
 // Tile shape and parts of the contraction by the time they take: a CU does one tile's share of the matrix instructions after the other, so what counts is the

@@ -87,6 +87,10 @@ class AttentionIn(C.Structure):
                 ("ldv", C.c_int64), ("ldc", C.c_int64)]
 
 
+# Their bytes from the fields in order: a call's cost on the host is the marshalling, and packing in one go is the cheaper form of it.
+_LINEAR, _ATTENTION = struct.Struct("@5P6i5q"), struct.Struct("@6P5if5q")
+assert _LINEAR.size == C.sizeof(LinearIn) and _ATTENTION.size == C.sizeof(AttentionIn)
+
 _packers = {}
 
 
@@ -147,9 +151,9 @@ def load_library():
     lib.strp_module_init.argtypes = [vp, C.POINTER(ModuleDesc), C.POINTER(ModuleState), C.POINTER(Params)]
     lib.strp_admm_step.argtypes = [vp, C.POINTER(ModuleDesc), C.POINTER(ModuleState), C.POINTER(Params),
                                    C.POINTER(Report)]
-    lib.strp_linear.argtypes = [vp, C.POINTER(LinearIn)]
+    lib.strp_linear.argtypes = [vp, vp]               # LinearIn, or its bytes
     lib.strp_layer_norm.argtypes = [vp, vp, C.c_int, i32, i64, i64, vp, vp, dbl, vp, i64]
-    lib.strp_attention.argtypes = [vp, C.POINTER(AttentionIn)]
+    lib.strp_attention.argtypes = [vp, vp]
     lib.strp_token_logprobs.argtypes = [vp, vp, C.c_int, i32, i64, i64, vp, vp, vp, i32, vp, vp, i64]
     lib.strp_linear_workspace_bytes.argtypes = [i32, i32, i64, C.c_int, C.c_int]
     lib.strp_linear_workspace_bytes.restype = C.c_size_t
@@ -326,56 +330,60 @@ class Context:
     # ---- a decoder layer's forward operators ----------------------------------------------
     # Activations are [channels x ld] tensors with the tokens contiguous, T of the ld columns valid; what the library cannot see
     # (shapes, strides, types and devices of the tensors) is checked here, the rest there.
-    def _operand(self, name, t, shape, dtypes):
-        """t as an operand of `shape` (None: any; the last is the least) and one of the dtypes, on this context's device."""
-        if t.device != self.device:
+    def _matrix(self, name, t, rows, cols, dtypes):
+        """Leading dimension of t as an operand of `rows` rows and at least `cols` columns, of one of the dtypes, on this context's device."""
+        shape = t.shape
+        if t.get_device() != self.device.index:
             raise ValueError(f"{name} is on {t.device}, the context on {self.device}")
         if t.dtype not in dtypes:
             raise TypeError(f"{name}: unsupported dtype {t.dtype}")
-        if t.dim() != len(shape) or t.shape[-1] < shape[-1] or (len(shape) == 2 and shape[0] is not None and t.shape[0] != shape[0]):
-            raise ValueError(f"{name}: shape {tuple(t.shape)}, needs {tuple(shape)}")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"{name}: its last dimension is not contiguous")
-        return t
+        if len(shape) != 2 or shape[0] != rows or shape[1] < cols:
+            raise ValueError(f"{name}: shape {tuple(shape)}, needs ({rows}, at least {cols})")
+        ld, step = t.stride()
+        if step != 1 and shape[1] > 1:
+            raise ValueError(f"{name}: its rows are not contiguous")
+        # the stride of a single row is not used, and torch may report anything
+        return ld if rows > 1 else (shape[1] + 7) // 8 * 8
 
-    def _rows(self, t):
-        # one row of any length: its stride is not used, and torch may report anything
-        return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+    def _vector(self, name, t, n, dtype):
+        """Address of a contiguous vector of at least n entries; 0 for None."""
+        if t is None:
+            return 0
+        if t.get_device() != self.device.index:
+            raise ValueError(f"{name} is on {t.device}, the context on {self.device}")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: {t.dtype}, needs {dtype}")
+        if t.dim() != 1 or t.shape[0] < n or (n > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name}: needs {n} contiguous entries")
+        return t.data_ptr()
 
-    def _result(self, name, out, rows, T, dtype):
-        if out is None:
-            return torch.empty((rows, (T + 7) // 8 * 8), dtype=dtype, device=self.device)
-        return self._operand(name, out, (rows, T), (dtype,) if dtype is not None else tuple(_CODES))
+    def _new(self, rows, T, dtype):
+        return torch.empty((rows, (T + 7) // 8 * 8), dtype=dtype, device=self.device)
 
     def strp_linear(self, W, X, T, bias=None, act=ACT_NONE, residual=None, out=None):
         """act(W X + bias) + residual: W [M x K], X [K x ld], bias [M] fp32, residual [M x ld] of out's dtype (out itself is
         allowed).  Returns out, made in X's dtype where none is given."""
         M, K = W.shape
-        self._operand("W", W, (M, K), _CODES)
-        self._operand("X", X, (K, T), _CODES)
-        out = self._result("out", out, M, T, X.dtype if out is None else None)
-        if bias is not None:
-            self._operand("bias", bias, (M,), (torch.float32,))
-        if residual is not None:
-            self._operand("residual", residual, (M, T), (out.dtype,))
-        need = int(self.lib.strp_linear_workspace_bytes(M, K, T, dtype_code(W), dtype_code(X)))
+        if out is None:
+            out = self._new(M, T, X.dtype)
+        ldw, ldx, ldy = self._matrix("W", W, M, K, _CODES), self._matrix("X", X, K, T, _CODES), self._matrix("out", out, M, T, _CODES)
+        w, x, y = _CODES[W.dtype], _CODES[X.dtype], _CODES[out.dtype]
+        r, ldr = (0, 0) if residual is None else (residual.data_ptr(), self._matrix("residual", residual, M, T, (out.dtype,)))
+        need = self.lib.strp_linear_workspace_bytes(M, K, T, w, x)
         if need:
             self.ensure_workspace(need)
-        a = LinearIn(_ptr(W), _ptr(X), _ptr(bias), _ptr(residual), _ptr(out), dtype_code(W), dtype_code(X), dtype_code(out), M, K, act, T,
-                     self._rows(W), self._rows(X), self._rows(residual) if residual is not None else 0, self._rows(out))
-        self.check(self.lib.strp_linear(self.h, C.byref(a)))
+        self.check(self.lib.strp_linear(self.h, _LINEAR.pack(W.data_ptr(), X.data_ptr(), self._vector("bias", bias, M, torch.float32), r, out.data_ptr(),
+                                                             w, x, y, M, K, act, T, ldw, ldx, ldr, ldy)))
         return out
 
     def strp_layer_norm(self, X, T, gain=None, bias=None, eps=1e-5, out=None):
         """Normalisation of every token over the channels of X [d x ld]; gain, bias [d] fp32.  out may be X."""
         d = X.shape[0]
-        self._operand("X", X, (d, T), _CODES)
-        out = self._result("out", out, d, T, X.dtype)
-        for name, t in (("gain", gain), ("bias", bias)):
-            if t is not None:
-                self._operand(name, t, (d,), (torch.float32,))
-        self.check(self.lib.strp_layer_norm(self.h, _ptr(X), dtype_code(X), d, T, self._rows(X), _ptr(gain), _ptr(bias), float(eps), _ptr(out),
-                                            self._rows(out)))
+        if out is None:
+            out = self._new(d, T, X.dtype)
+        ldx, ldy = self._matrix("X", X, d, T, _CODES), self._matrix("out", out, d, T, (X.dtype,))
+        self.check(self.lib.strp_layer_norm(self.h, X.data_ptr(), _CODES[X.dtype], d, T, ldx, self._vector("gain", gain, d, torch.float32),
+                                            self._vector("bias", bias, d, torch.float32), eps, out.data_ptr(), ldy))
         return out
 
     def strp_attention(self, Q, K, V, T, heads, kv_heads=None, seq_start=None, kv_of_head=None, scale=None, out=None):
@@ -383,43 +391,45 @@ class Context:
         (None: one sequence), kv_of_head [heads] int32 (None: equal groups), scale 1 / sqrt(d_head) by default.  Returns
         the head outputs, like Q."""
         kv_heads = heads if kv_heads is None else kv_heads
-        if heads <= 0 or Q.dim() != 2 or Q.shape[0] % heads:
+        if heads <= 0 or Q.dim() != 2 or Q.shape[0] < heads or Q.shape[0] % heads:
             raise ValueError(f"Q: {tuple(Q.shape)} is not {heads} heads")
-        dh = Q.shape[0] // heads
-        self._operand("Q", Q, (None, T), _CODES)
-        self._operand("K", K, (kv_heads * dh, T), (Q.dtype,))
-        self._operand("V", V, (kv_heads * dh, T), (Q.dtype,))
-        out = self._result("out", out, heads * dh, T, Q.dtype)
-        if seq_start is not None:
-            self._operand("seq_start", seq_start, (2,), (torch.int32,))
-        if kv_of_head is not None:
-            self._operand("kv_of_head", kv_of_head, (heads,), (torch.int32,))
-        a = AttentionIn(_ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(seq_start), _ptr(kv_of_head), dtype_code(Q), heads, kv_heads, dh,
-                        seq_start.numel() - 1 if seq_start is not None else 0, dh ** -0.5 if scale is None else float(scale), T,
-                        self._rows(Q), self._rows(K), self._rows(V), self._rows(out))
-        self.check(self.lib.strp_attention(self.h, C.byref(a)))
+        rows, same = Q.shape[0], (Q.dtype,)
+        dh = rows // heads
+        if out is None:
+            out = self._new(rows, T, Q.dtype)
+        ldq, ldk = self._matrix("Q", Q, rows, T, _CODES), self._matrix("K", K, kv_heads * dh, T, same)
+        ldv, ldc = self._matrix("V", V, kv_heads * dh, T, same), self._matrix("out", out, rows, T, same)
+        n_seq = 0 if seq_start is None else seq_start.shape[0] - 1
+        self.check(self.lib.strp_attention(self.h, _ATTENTION.pack(
+            Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), self._vector("seq_start", seq_start, 2, torch.int32),
+            self._vector("kv_of_head", kv_of_head, heads, torch.int32), _CODES[Q.dtype], heads, kv_heads, dh, n_seq,
+            dh ** -0.5 if scale is None else scale, T, ldq, ldk, ldv, ldc)))
         return out
 
     def strp_token_logprobs(self, logits, T, target=None, entropy=True, n_top=0):
         """What a model answers at each of T tokens, from logits [V x ld]: dict of logp [T] (of target [T] int32, if given), entropy [T]
         (if wanted), top_ids and top_logp [n_top x T]."""
         V = logits.shape[0]
-        self._operand("logits", logits, (V, T), _CODES)
-        if target is not None:
-            self._operand("target", target, (T,), (torch.int32,))
+        ldl = self._matrix("logits", logits, V, T, _CODES)
+        y = self._vector("target", target, T, torch.int32)
         if n_top < 0 or n_top > min(V, TOP_MAX):
             raise ValueError(f"n_top outside [0, {min(V, TOP_MAX)}]")
-        e = lambda *shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=self.device)
-        res = {}
+        if T <= 0:
+            raise ValueError(f"{T} tokens")
+        # one allocation for what is fp32
+        rows = (target is not None) + bool(entropy) + n_top
+        floats = torch.empty((rows, T), device=self.device)
+        res, at = {}, 0
         if target is not None:
-            res["logp"] = e(T)
+            res["logp"], at = floats[0], 1
         if entropy:
-            res["entropy"] = e(T)
-        res["top_ids"], res["top_logp"] = e(n_top, T, dt=torch.int32), e(n_top, T)
-        self.ensure_workspace(int(self.lib.strp_token_logprobs_workspace_bytes(V, T, n_top)))
-        self.check(self.lib.strp_token_logprobs(self.h, _ptr(logits), dtype_code(logits), V, T, self._rows(logits), _ptr(target), _ptr(res.get("logp")),
-                                                _ptr(res.get("entropy")), n_top, _ptr(res["top_ids"]) if n_top else None,
-                                                _ptr(res["top_logp"]) if n_top else None, T))
+            res["entropy"], at = floats[at], at + 1
+        res["top_ids"], res["top_logp"] = torch.empty((n_top, T), dtype=torch.int32, device=self.device), floats[at:]
+        self.ensure_workspace(self.lib.strp_token_logprobs_workspace_bytes(V, T, n_top))
+        base, row = floats.data_ptr(), 4 * T
+        self.check(self.lib.strp_token_logprobs(self.h, logits.data_ptr(), _CODES[logits.dtype], V, T, ldl, y or None, base if y else None,
+                                                base + (row if y else 0) if entropy else None, n_top, res["top_ids"].data_ptr() if n_top else None,
+                                                base + at * row if n_top else None, T))
         return res
 
     def strp_module_init(self, desc, state, params):

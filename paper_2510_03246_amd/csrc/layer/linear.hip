@@ -23,18 +23,30 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
   typedef XT xvec __attribute__((ext_vector_type(4)));
   wvec w[RW];
   xvec x[RX];
+  // rows behind M and tokens behind T are others over again: what comes of them is not stored
+  const WT* wp[RW];
+  const XT* xp[RX];
+#pragma unroll
+  for (int i = 0; i < RW; ++i) wp[i] = (const WT*)p.W + (long long)min(m0 + wr + 32 * i, p.M - 1) * p.ldw + wk;
+#pragma unroll
+  for (int i = 0; i < RX; ++i) xp[i] = (const XT*)p.X + (long long)(xr + XROWS * i) * p.ldx + (n0 + xt < p.T ? n0 + xt : (p.T - 1) / 4 * 4);
   auto fetch = [&](int k0) {
+    if (k0 + BK <= k_end) {
 #pragma unroll
-    for (int i = 0; i < RW; ++i) {
-      const int m = m0 + wr + 32 * i, k = k0 + wk;
-      w[i] = wvec{(WT)0.0f, (WT)0.0f, (WT)0.0f, (WT)0.0f};
-      if (m < p.M && k < k_end) w[i] = *(const wvec*)((const WT*)p.W + (long long)m * p.ldw + k);
-    }
+      for (int i = 0; i < RW; ++i) w[i] = *(const wvec*)(wp[i] + k0);
 #pragma unroll
-    for (int i = 0; i < RX; ++i) {
-      const int k = k0 + xr + XROWS * i;
-      x[i] = xvec{(XT)0.0f, (XT)0.0f, (XT)0.0f, (XT)0.0f};
-      if (k < k_end && n0 + xt < p.T) x[i] = *(const xvec*)((const XT*)p.X + (long long)k * p.ldx + n0 + xt);
+      for (int i = 0; i < RX; ++i) x[i] = *(const xvec*)(xp[i] + (long long)k0 * p.ldx);
+    } else {
+#pragma unroll
+      for (int i = 0; i < RW; ++i) {
+        w[i] = wvec{(WT)0.0f, (WT)0.0f, (WT)0.0f, (WT)0.0f};
+        if (k0 + wk < k_end) w[i] = *(const wvec*)(wp[i] + k0);
+      }
+#pragma unroll
+      for (int i = 0; i < RX; ++i) {
+        x[i] = xvec{(XT)0.0f, (XT)0.0f, (XT)0.0f, (XT)0.0f};
+        if (k0 + xr + XROWS * i < k_end) x[i] = *(const xvec*)(xp[i] + (long long)k0 * p.ldx);
+      }
     }
   };
   floatx4 acc[NI][NJ];
@@ -43,10 +55,15 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   auto put = [&](int k0, int buf) {
+    if (k0 + BK > k_end)
+#pragma unroll
+      for (int i = 0; i < RW; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[i][e] = k0 + wk + e < k_end ? w[i][e] : (WT)0.0f;
 #pragma unroll
     for (int i = 0; i < RW; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sW[buf][wk + e][wr + 32 * i] = k0 + wk + e < k_end ? (float)w[i][e] : 0.0f;
+      for (int e = 0; e < 4; ++e) sW[buf][wk + e][wr + 32 * i] = (float)w[i][e];
 #pragma unroll
     for (int i = 0; i < RX; ++i) *(floatx4*)&sX[buf][xr + XROWS * i][xt] = floatx4{(float)x[i][0], (float)x[i][1], (float)x[i][2], (float)x[i][3]};
   };
@@ -71,28 +88,39 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
         for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(f.b[s][j], f.a[s][i], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  fetch(k_first);
-  put(k_first, 0);
-  fetch(k_first + BK);
+  // Rows of W lie a power of two apart often enough, and then the same columns of all of them in a few of memory's channels: the rows of tiles begin at different
+  // places of the contraction and go round it.
+  const int n = (k_end - k_first + BK - 1) / BK;
+  int k_next = k_first + (int)((long long)(tile % p.tilesM) * n / p.tilesM) * BK;
+  const auto next = [&]() {
+    const int k = k_next;
+    k_next = k + BK < k_end ? k + BK : k_first;
+    return k;
+  };
+  int k1 = next();
+  fetch(k1);
+  put(k1, 0);
+  k1 = next();
+  fetch(k1);
   __syncthreads();
   Frag f0, f1;
   read(f0, 0, 0);
   int buf = 0;
 #pragma unroll 1
-  for (int k0 = k_first; k0 < k_end; k0 += BK) {
+  for (int i = 0; i < n; ++i) {
     read(f1, buf, 1);
     multiply(f0);
     read(f0, buf, 2);
-    // the next run of steps goes to the other buffer, and the one behind it is asked for
-    if (k0 + BK < k_end) {
-      put(k0 + BK, buf ^ 1);
-      fetch(k0 + 2 * BK);
-    }
+    // the next run of steps goes to the other buffer, and the one behind it is asked for; past the last they are not multiplied
+    put(k1, buf ^ 1);
+    k1 = next();
+    fetch(k1);
+    __builtin_amdgcn_sched_barrier(0);
     multiply(f1);
     read(f1, buf, 3);
     multiply(f0);
     __syncthreads();
-    read(f0, buf ^ 1, 0);                   // past the last run these are not multiplied
+    read(f0, buf ^ 1, 0);
     multiply(f1);
     buf ^= 1;
   }

@@ -68,11 +68,15 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
 #pragma unroll
     for (int s = 0; s < DHP / 2; ++s) {
       const int d = 2 * s + h;
-      const float v = Q[(long long)(d < p.dh ? d : 0) * p.ldq];
-      qf[s] = d < p.dh ? v : 0.0f;
+      qf[s] = Q[(long long)(d < p.dh ? d : 0) * p.ldq];
     }
   }
   const int lo = first_key(p, q);
+#pragma unroll
+  for (int s = 0; s < DHP / 2; ++s) {
+    qf[s] = 2 * s + h < p.dh ? qf[s] : 0.0f;
+    __builtin_amdgcn_sched_barrier(0);                                     // one comparison at a time, or their results take the scalar registers
+  }
   int wlo = lo <= q ? lo : 0x7fffffff, whi = wlo;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -100,30 +104,45 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
   constexpr bool AHEAD = DHP < 128;
   constexpr int ROWS = 256 / CHUNKS, NR = DHP / ROWS;
   const int row0 = tid / CHUNKS, col = (tid % CHUNKS) * 4;
-  floatx4 nk[NR], nv[NR];
-  auto ask = [&](int k0) {
+  floatx4 nk[AHEAD ? NR : 4], nv[AHEAD ? NR : 4];
+  auto ask = [&](int k0, int first, int n) {
+    int r0 = row0;
+    asm volatile("" : "+v"(r0));                                           // or every row's address is worked out once and kept
+    const float* kp = Kh + (long long)r0 * p.ldk + k0 + col;
+    const float* vp = Vh + (long long)r0 * p.ldv + k0 + col;
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
+    for (int i = 0; i < n; ++i) {
       nk[i] = nv[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-      const int r = row0 + ROWS * i;
-      if (r < p.dh && k0 + col < p.T) {
-        nk[i] = *(const floatx4*)(Kh + (long long)r * p.ldk + k0 + col);
-        nv[i] = *(const floatx4*)(Vh + (long long)r * p.ldv + k0 + col);
+      if (r0 + ROWS * (first + i) < p.dh && k0 + col < p.T) {
+        nk[i] = *(const floatx4*)(kp + (long long)(ROWS * (first + i)) * p.ldk);
+        nv[i] = *(const floatx4*)(vp + (long long)(ROWS * (first + i)) * p.ldv);
       }
     }
   };
-  if (AHEAD) ask(low & ~(KT - 1));
+  auto put = [&](int first, int n) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      *(floatx4*)&sK[row0 + ROWS * (first + i)][col] = nk[i];
+      *(floatx4*)&sV[row0 + ROWS * (first + i)][col] = nv[i];
+    }
+  };
+  if constexpr (AHEAD) ask(low & ~(KT - 1), 0, NR);
 #pragma unroll 1
   for (int k0 = low & ~(KT - 1); k0 <= last; k0 += KT) {
     __syncthreads();
-    if (!AHEAD) ask(k0);
+    if constexpr (AHEAD) {
+      put(0, NR);
+    } else {
 #pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      *(floatx4*)&sK[row0 + ROWS * i][col] = nk[i];
-      *(floatx4*)&sV[row0 + ROWS * i][col] = nv[i];
+      for (int i = 0; i < NR; i += 4) {
+        ask(k0, i, 4);
+        put(i, 4);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     __syncthreads();
-    if (AHEAD && k0 + KT <= last) ask(k0 + KT);
+    if constexpr (AHEAD)
+      if (k0 + KT <= last) ask(k0 + KT, 0, NR);
     const int k1 = k0 + 32 * part;
     if (wq + 31 < k1 || wlo >= k1 + 32) continue;                          // nothing here that this wavefront sees
     const bool whole = whi <= k1 && wq >= k1 + 31;
@@ -131,8 +150,10 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) S[e] = 0.0f;
 #pragma unroll
-    for (int s = 0; s < DHP / 2; ++s)
+    for (int s = 0; s < DHP / 2; ++s) {
       if (s < DHP / 2 - 16 || 2 * s < p.dh) S = __builtin_amdgcn_mfma_f32_32x32x2f32(sK[2 * s + h][32 * part + l32], qf[s], S, 0, 0, 0);
+      if (s % 16 == 15) __builtin_amdgcn_sched_barrier(0);       // not every fragment at once, for the registers
+    }
     if (!whole)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -143,24 +164,24 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, S[e]);
     mt = __builtin_elementwise_maximum(mt, __shfl_xor(mt, 32, 64));
-    const float ref = mt == -INFINITY ? 0.0f : mt * p.scale_log2e, fac = __builtin_amdgcn_exp2f(m * p.scale_log2e - ref);
+    const float fac = mt == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e);
     m = mt;
     float sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      S[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[e], p.scale_log2e, -ref));
+      S[e] = __builtin_amdgcn_exp2f((S[e] - (mt == -INFINITY ? 0.0f : mt)) * p.scale_log2e);      // the difference first: it is exact, or small against what it is taken from
       sum += S[e];
     }
     l = l * fac + sum;
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) O[c][e] *= fac;
     // Where some key is not seen by every query, a value that is not finite would reach those too, by a probability of zero: such values are left out of
     // the products and added to the results of the queries that see them.
+    // A tile's share is summed by itself: so the chains that round are as long as a tile and as the number of tiles, not as the keys.
     bool odd = false;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int c = 0; c < NC; ++c) {
+      floatx16 share;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) share[e] = 0.0f;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         floatx4 v = *(const floatx4*)&sV[32 * c + l32][32 * part + 8 * g + 4 * h];
@@ -172,8 +193,12 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
             v[e] = fin ? v[e] : 0.0f;
           }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) O[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], S[4 * g + e], O[c], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) share = __builtin_amdgcn_mfma_f32_32x32x2f32(v[e], S[4 * g + e], share, 0, 0, 0);
       }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) O[c][e] = __builtin_fmaf(O[c][e], fac, share[e]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     if (__builtin_amdgcn_ballot_w64(odd))
 #pragma unroll 1
       for (int i = 0; i < 32; ++i) {

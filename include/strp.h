@@ -289,8 +289,9 @@ typedef enum { STRP_ACT_NONE = 0, STRP_ACT_RELU = 1, STRP_ACT_GELU = 2 } strp_ac
  *   W [M x ldw] w_dtype, ldw >= K a multiple of 8, entries from column K on are not read as data;  X [K x ldx] x_dtype;
  *   bias [M] fp32 or NULL;  R [M x ldr] y_dtype or NULL;  Y [M x ldy] y_dtype.  R may be Y itself (same ld).
  * bf16 W and X are multiplied in bf16 with fp32 sums; with an fp32 operand the products are those of fp32.
- * Errors: STRP_EINVAL (null W, X or Y, sizes not positive, ld below its width or no multiple of 8, misaligned, unknown
- * dtype or activation), STRP_ENOMEM (strp_linear_workspace_bytes).
+ * Errors: STRP_EINVAL (null W, X or Y, sizes not positive, M or K above 2^30, T above 2^31, 2^23 tiles or more (of 64 x
+ * 64 and up; 16 x 64 up to 64 tokens), ld below its width or no multiple of 8, misaligned, unknown dtype or activation),
+ * STRP_ENOMEM (strp_linear_workspace_bytes).
  */
 typedef struct {
   const void* W;
@@ -311,7 +312,8 @@ size_t strp_linear_workspace_bytes(int32_t M, int32_t K, int64_t T, strp_dtype w
  * strp_layer_norm -- Y[:, t] = (X[:, t] - mean_t) / sqrt(var_t + eps) * gain + bias over the d channels of every token
  * (population variance, the deviations taken from the mean).
  *   X [d x ldx], Y [d x ldy] of dtype;  gain, bias [d] fp32, either may be NULL (1 and 0).  Y may be X (same ld).
- * Errors: STRP_EINVAL (null X or Y, d or T not positive, eps negative or not a number, bad ld, misaligned, unknown dtype).
+ * Errors: STRP_EINVAL (null X or Y, d or T not positive, d above 2^30, T above 2^27, eps negative or not a number, bad ld,
+ * misaligned, unknown dtype).
  */
 strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype dtype, int32_t d, int64_t T, int64_t ldx, const float* gain,
                             const float* bias, double eps, void* Y, int64_t ldy);
@@ -329,8 +331,9 @@ strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype dtype, int3
  * (other sequences, later tokens, padding) has no part in its result, whatever it holds, infinities and NaN included.
  * Entries of seq_start or kv_of_head outside their ranges give wrong results, no access out of bounds.
  * bf16: the probabilities are rounded to bf16 before they meet V (fp32 sums).  fp32: products of fp32.
- * Errors: STRP_EINVAL (null pointer, sizes not positive, d_head above 128, kv_heads that does not divide heads without
- * kv_of_head, scale not positive and finite, bad ld, misaligned, unknown dtype, more heads than 65535).
+ * Errors: STRP_EINVAL (null pointer, sizes not positive, ceil(T / 64) heads of 2^23 or more, d_head above 128, kv_heads that
+ * does not divide heads without kv_of_head, scale not positive and finite, bad ld, misaligned, unknown dtype, more heads
+ * than 65535).
  */
 typedef struct {
   const void* Q;
@@ -352,9 +355,9 @@ strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in);
  *   entropy[t] = -sum p log p (an entry of -inf counts as 0)                        NULL: not wanted
  *   top_id[i ldt + t], top_logp[i ldt + t], i < n_top: the entries of highest logit in descending order, equal ones by the
  *   lower index, and their log p.  A token with a NaN among its logits has id -1 and NaN there.
- * Errors: STRP_EINVAL (null logits, V or T not positive, n_top outside [0, min(V, STRP_TOP_MAX)], target without logp or the
- * reverse, top_id or top_logp missing with n_top > 0, ldt < T, nothing asked for, bad ld, misaligned, unknown dtype),
- * STRP_ENOMEM (strp_token_logprobs_workspace_bytes).
+ * Errors: STRP_EINVAL (null logits, V or T not positive, V above 2^30, T above 2^25, n_top outside [0, min(V, STRP_TOP_MAX)],
+ * target without logp or the reverse, top_id or top_logp missing with n_top > 0, ldt < T, nothing asked for, bad ld,
+ * misaligned, unknown dtype), STRP_ENOMEM (strp_token_logprobs_workspace_bytes).
  */
 #define STRP_TOP_MAX 16
 strp_status strp_token_logprobs(strp_ctx* ctx, const void* logits, strp_dtype dtype, int32_t V, int64_t T, int64_t ldl,

@@ -563,7 +563,7 @@ extern "C" strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in
   if (!token_ld(in->ldq, in->T) || !token_ld(in->ldk, in->T) || !token_ld(in->ldv, in->T) || !token_ld(in->ldc, in->T))
     return fail(ctx, STRP_EINVAL, "attention: leading dimensions must be multiples of 8 and not below T");
   if (!ptr16(in->Q) || !ptr16(in->K) || !ptr16(in->V) || !ptr16(in->C)) return fail(ctx, STRP_EINVAL, "attention: Q, K, V or C not 16-byte aligned");
-  if (in->T > 0x7fffff00LL || (in->T + 63) / 64 * in->heads > 0x7fffffffLL) return fail(ctx, STRP_EINVAL, "attention: tokens, or tiles of 64 of all heads, do not fit 31 bits");
+  if ((in->T + 63) / 64 * in->heads > MAX_TILES) return fail(ctx, STRP_EINVAL, "attention: tiles of 64 tokens of all heads, more than a launch holds");
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "attention: device %d cannot be made current", ctx->device);
   AttnP p{in->Q, in->K, in->V, in->C, in->seq_start, in->kv_of_head, in->heads, in->kv_heads, in->heads / in->kv_heads, in->d_head, in->n_seq,

@@ -229,7 +229,7 @@ extern "C" strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype 
   if (!token_ld(ldx, T) || !token_ld(ldy, T)) return fail(ctx, STRP_EINVAL, "layer_norm: leading dimensions must be multiples of 8 and not below T");
   if (!ptr16(X) || !ptr16(Y)) return fail(ctx, STRP_EINVAL, "layer_norm: X or Y not 16-byte aligned");
   if (X == Y && ldx != ldy) return fail(ctx, STRP_EINVAL, "layer_norm: Y is X with another leading dimension");
-  if (T > (1LL << 31)) return fail(ctx, STRP_EINVAL, "layer_norm: more than 2^31 tokens");
+  if (T > (1LL << 27) || d > (1 << 30)) return fail(ctx, STRP_EINVAL, "layer_norm: more than 2^27 tokens or 2^30 channels");
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "layer_norm: device %d cannot be made current", ctx->device);
   const NormP p{X, Y, gain, bias, d, T, ldx, ldy, (float)eps, 0};

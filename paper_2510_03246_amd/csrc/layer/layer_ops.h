@@ -37,6 +37,8 @@ class OnDevice {
 };
 
 static inline bool known_dtype(int dt) { return dt == STRP_BF16 || dt == STRP_F32; }
+// A launch has fewer than 2^32 threads: blocks of up to 512 that are surely within it.
+constexpr long long MAX_TILES = (1LL << 23) - 1;
 static inline size_t bytes_of(int dt) { return dt == STRP_BF16 ? 2 : 4; }
 static inline bool ptr16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 static inline bool token_ld(int64_t ld, int64_t T) { return ld >= T && ld % 8 == 0; }

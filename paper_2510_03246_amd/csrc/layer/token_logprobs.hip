@@ -354,7 +354,7 @@ using namespace strp;
 extern "C" {
 
 size_t strp_token_logprobs_workspace_bytes(int32_t V, int64_t T, int32_t n_top) {
-  if (V <= 0 || T <= 0 || n_top < 0) return 0;
+  if (V <= 0 || V > (1 << 30) || T <= 0 || T > (1LL << 25) || n_top < 0) return 0;
   size_t most = 0;
   for (int dt : {STRP_BF16, STRP_F32}) {
     const LogitPlan q = plan_logits(V, T, dt);
@@ -376,7 +376,7 @@ strp_status strp_token_logprobs(strp_ctx* ctx, const void* logits, strp_dtype dt
   if (!logp && !entropy && n_top == 0) return fail(ctx, STRP_EINVAL, "token_logprobs: nothing asked for");
   if (!token_ld(ldl, T)) return fail(ctx, STRP_EINVAL, "token_logprobs: ldl must be a multiple of 8 and not below T");
   if (!ptr16(logits)) return fail(ctx, STRP_EINVAL, "token_logprobs: logits not 16-byte aligned");
-  if (T > (1LL << 31)) return fail(ctx, STRP_EINVAL, "token_logprobs: more than 2^31 tokens");
+  if (T > (1LL << 25) || V > (1 << 30)) return fail(ctx, STRP_EINVAL, "token_logprobs: more than 2^25 tokens or 2^30 entries");
   if (!ctx->ws) return fail(ctx, STRP_ENOMEM, "token_logprobs: no workspace set");
   const LogitPlan q = plan_logits(V, T, dtype);
   Arena arena(ctx);

@@ -342,8 +342,8 @@ class Context:
         ld, step = t.stride()
         if step != 1 and shape[1] > 1:
             raise ValueError(f"{name}: its rows are not contiguous")
-        # the stride of a single row is not used, and torch may report anything
-        return ld if rows > 1 else (shape[1] + 7) // 8 * 8
+        # torch may report anything as the stride of a single row
+        return shape[1] if rows == 1 and (ld < shape[1] or ld % 8) else ld
 
     def _vector(self, name, t, n, dtype):
         """Address of a contiguous vector of at least n entries; 0 for None."""

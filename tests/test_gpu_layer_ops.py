@@ -557,6 +557,8 @@ def test_binding_refusals(ctx):
         ctx.strp_linear(W, X, 0)
     with pytest.raises(strp.StrpError):
         ctx.strp_linear(rand((8, 19), 1)[:, :16], X, 20)          # rows that begin at odd places
+    with pytest.raises(strp.StrpError):
+        ctx.strp_linear(rand((1, 19), 1), rand((19, 24), 2), 20)  # one row without room for a whole eight
     with pytest.raises(ValueError):
         ctx.strp_layer_norm(X, 20, gain=torch.ones(15, device="cuda"))
     with pytest.raises(ValueError):

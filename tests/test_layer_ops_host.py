@@ -33,10 +33,24 @@ def check_linear_refusals():
         assert st == strp.OK and launches, good
     for bad in (dict(W=None), dict(X=None), dict(Y=None), dict(M=0), dict(K=0), dict(T=0), dict(M=-1), dict(T=-5), dict(w_dtype=2), dict(x_dtype=-1), dict(y_dtype=7),
                 dict(act=3), dict(act=-1), dict(ldw=48), dict(ldw=57), dict(ldx=56), dict(ldx=61), dict(ldy=59), dict(ldy=68), dict(ldr=56), dict(W=A[0] + 8), dict(X=A[1] + 2),
-                dict(Y=A[4] + 4), dict(R=A[3] + 8), dict(R=A[4], ldr=72)):
+                dict(Y=A[4] + 4), dict(R=A[3] + 8), dict(R=A[4], ldr=72), dict(M=(1 << 30) + 1), dict(K=(1 << 30) + 8, ldw=(1 << 30) + 8),
+                dict(M=1 << 27, T=16), dict(M=1 << 20, T=1 << 22, ldx=1 << 22, ldr=1 << 22, ldy=1 << 22)):
         st, launches = call(**bad)
         assert st == strp.EINVAL and not launches and lib.lib.strp_last_error(lib.h), bad
     assert lib.lib.strp_linear(lib.h, None) == strp.EINVAL
+    # every size's need is enough; without a workspace a product that needs one is refused, the others are not
+    sizes = [(M, K, T) for M in (1, 40, 768, 5000) for K in (8, 760, 8192) for T in (1, 16, 17, 64, 65, 300, 5000)]
+    bare = C.c_void_p()
+    assert lib.lib.strp_create(C.byref(bare), 0, None) == strp.OK
+    for M, K, T in sizes:
+        for w, x in ((strp.BF16, strp.BF16), (strp.F32, strp.BF16), (strp.F32, strp.F32)):
+            need = lib.lib.strp_linear_workspace_bytes(M, K, T, w, x)
+            a = _linear(strp, M=M, K=K, T=T, w_dtype=w, x_dtype=x, ldw=K, ldx=(T + 7) // 8 * 8, ldy=(T + 7) // 8 * 8, R=None)
+            assert lib.lib.strp_linear(bare, C.byref(a)) == (strp.ENOMEM if need else strp.OK), (M, K, T)
+            if need:
+                lib.workspace(need)
+                assert lib.lib.strp_linear(lib.h, C.byref(a)) == strp.OK, (M, K, T)
+    assert lib.lib.strp_linear_workspace_bytes(0, 8, 8, 0, 0) == 0
     assert lib.lib.strp_linear(None, C.byref(_linear(strp))) == strp.EINVAL
 
 
@@ -51,7 +65,7 @@ def check_norm_refusals():
         st, launches = call(**good)
         assert st == strp.OK and launches, good
     for bad in (dict(X=None), dict(Y=None), dict(dtype=5), dict(d=0), dict(T=0), dict(ldx=16), dict(ldx=23), dict(ldy=16), dict(eps=-1e-9), dict(eps=float("nan")), dict(X=A[0] + 4),
-                dict(Y=A[3] + 2), dict(Y=A[0], ldy=32)):
+                dict(Y=A[3] + 2), dict(Y=A[0], ldy=32), dict(d=(1 << 30) + 1), dict(T=(1 << 27) + 1, ldx=1 << 32, ldy=1 << 32)):
         st, launches = call(**bad)
         assert st == strp.EINVAL and not launches, bad
     assert lib.lib.strp_layer_norm(None, A[0], 1, 1, 1, 8, None, None, 0.0, A[1], 8) == strp.EINVAL
@@ -74,7 +88,7 @@ def check_attention_refusals():
     for bad in (dict(Q=None), dict(K=None), dict(V=None), dict(C=None), dict(dtype=2), dict(heads=0), dict(kv_heads=0), dict(d_head=0), dict(d_head=129), dict(T=0), dict(kv_heads=3),
                 dict(heads=65536), dict(heads=2, kv_heads=5), dict(n_seq=0), dict(n_seq=-1), dict(seq_start=None), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
                 dict(scale=float("inf")), dict(ldq=96), dict(ldk=101), dict(ldv=103), dict(ldc=99), dict(Q=A[0] + 8), dict(K=A[1] + 2), dict(V=A[2] + 4), dict(C=A[3] + 8),
-                dict(T=1 << 31, ldq=1 << 31, ldk=1 << 31, ldv=1 << 31, ldc=1 << 31)):
+                dict(T=1 << 26, ldq=1 << 31, ldk=1 << 31, ldv=1 << 31, ldc=1 << 31)):
         st, launches = call(**bad)
         assert st == strp.EINVAL and not launches, bad
     assert lib.lib.strp_attention(lib.h, None) == strp.EINVAL
@@ -93,7 +107,7 @@ def check_logprobs_refusals():
         assert st == strp.OK and len(launches) == 2, good
         assert all(0 < g[0] and 0 < g[1] <= 65535 for _, g in launches), launches
     for bad in (dict(logits=None), dict(dtype=9), dict(V=0), dict(T=0), dict(ldl=16), dict(ldl=25), dict(logits=A[0] + 4), dict(n_top=-1), dict(n_top=17), dict(V=4, n_top=5), dict(target=None),
-                dict(logp=None), dict(top_id=None), dict(top_logp=None), dict(ldt=19), dict(target=None, logp=None, entropy=None, n_top=0)):
+                dict(logp=None), dict(top_id=None), dict(top_logp=None), dict(ldt=19), dict(target=None, logp=None, entropy=None, n_top=0), dict(V=(1 << 30) + 1), dict(T=(1 << 25) + 1, ldl=1 << 26, ldt=1 << 26)):
         st, launches = call(**bad)
         assert st == strp.EINVAL and not launches, bad
     need = lib.lib.strp_token_logprobs_workspace_bytes(100, 20, 5)

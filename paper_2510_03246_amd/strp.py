@@ -194,6 +194,7 @@ class Context:
             raise StrpError(st, "strp_create failed")
         self.h = h
         self.ws = None
+        self.in_graphs, self.kept = False, []     # whether a captured call has the workspace; those that were replaced since
         if workspace_bytes:
             self.set_workspace(workspace_bytes)
 
@@ -214,12 +215,18 @@ class Context:
 
     # ---- plumbing ---------------------------------------------------------------------
     def set_workspace(self, nbytes: int):
-        self.ws = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
+        if self.in_graphs:
+            self.kept.append(self.ws)             # a graph that is replayed still writes there
+            self.in_graphs = False
+        with torch.cuda.stream(self.stream):
+            self.ws = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
         self.check(self.lib.strp_set_workspace(self.h, _ptr(self.ws), int(nbytes)))
 
     def ensure_workspace(self, nbytes: int):
         if self.ws is None or self.ws.numel() < nbytes:
             self.set_workspace(nbytes)
+        if torch.cuda.is_current_stream_capturing():
+            self.in_graphs = True
 
     def set_precision(self, prec: int):
         self.check(self.lib.strp_set_precision(self.h, prec))
@@ -357,8 +364,15 @@ class Context:
             raise ValueError(f"{name}: needs {n} contiguous entries")
         return t.data_ptr()
 
+    def _empty(self, shape, dtype):
+        """An output, from the memory of the stream that writes it."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
     def _new(self, rows, T, dtype):
-        return torch.empty((rows, (T + 7) // 8 * 8), dtype=dtype, device=self.device)
+        return self._empty((rows, (T + 7) // 8 * 8), dtype)
 
     def strp_linear(self, W, X, T, bias=None, act=ACT_NONE, residual=None, out=None):
         """act(W X + bias) + residual: W [M x K], X [K x ld], bias [M] fp32, residual [M x ld] of out's dtype (out itself is
@@ -418,13 +432,13 @@ class Context:
             raise ValueError(f"{T} tokens")
         # one allocation for what is fp32
         rows = (target is not None) + bool(entropy) + n_top
-        floats = torch.empty((rows, T), device=self.device)
+        floats = self._empty((rows, T), torch.float32)
         res, at = {}, 0
         if target is not None:
             res["logp"], at = floats[0], 1
         if entropy:
             res["entropy"], at = floats[at], at + 1
-        res["top_ids"], res["top_logp"] = torch.empty((n_top, T), dtype=torch.int32, device=self.device), floats[at:]
+        res["top_ids"], res["top_logp"] = self._empty((n_top, T), torch.int32), floats[at:]
         self.ensure_workspace(self.lib.strp_token_logprobs_workspace_bytes(V, T, n_top))
         base, row = floats.data_ptr(), 4 * T
         self.check(self.lib.strp_token_logprobs(self.h, logits.data_ptr(), _CODES[logits.dtype], V, T, ldl, y or None, base if y else None,

@@ -96,6 +96,13 @@ def test_linear_of_many_tiles(ctx, size, types):
     linear_case(ctx, *size, types, strp.ACT_NONE, True, True)
 
 
+@pytest.mark.parametrize("T", [1, 5, 8, 9, 15, 16, 17, 31, 32, 33, 63, 64])
+@pytest.mark.parametrize("M,K", [(70, 4101), (33, 2049), (5000, 3403), (2048, 2048)])
+def test_linear_of_few_tokens(ctx, M, K, T):
+    linear_case(ctx, M, K, T, TYPES[0], strp.ACT_RELU, True, True)
+    linear_case(ctx, M, K, T, TYPES[1], strp.ACT_NONE, True, False)
+
+
 def test_linear_into_its_residual(ctx):
     for T in (5, 300):
         W, X, R = rand((96, 64), 1, BF16, 0.1), rand((64, ld8(T)), 2, BF16), rand((96, ld8(T)), 3, BF16)
@@ -498,6 +505,43 @@ def test_captured_and_replayed(ctx):
         torch.cuda.synchronize()
         for n in kept:
             assert torch.equal(kept[n][..., :T], eager[n][..., :T]), (n, seed)
+
+
+def test_a_graph_keeps_the_workspace_that_a_larger_call_replaces(ctx):
+    W, X = rand((512, 4096), 1, BF16, 0.05), rand((4096, 128), 2, BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        own = strp.Context(0)
+        want = own.strp_linear(W, X, 128)
+        size = own.ws.numel()
+        assert size >= own.lib.strp_linear_workspace_bytes(512, 4096, 128, strp.BF16, strp.BF16) > 0
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = own.strp_linear(W, X, 128)
+        own.ensure_workspace(8 * size)
+        others = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        for _ in range(3):
+            got.zero_()
+            graph.replay()
+            assert torch.equal(own.strp_linear(W, X, 128), want) and torch.equal(got, want)
+        assert all(bool((o == 7).all()) for o in others)
+    torch.cuda.synchronize()
+
+
+def test_outputs_come_from_the_memory_of_the_context_s_stream(ctx):
+    """Called under another stream than its own, a context takes its outputs where its own stream's work is in order."""
+    W, X = rand((64, 96), 1, BF16), rand((96, 200), 2, BF16)
+    want = ctx.strp_linear(W, X, 200)
+    tops = ctx.strp_token_logprobs(want, 200, n_top=3)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        y = ctx.strp_linear(W, X, 200)
+        t = ctx.strp_token_logprobs(y, 200, n_top=3)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and all(torch.equal(t[n], tops[n]) for n in tops)
 
 
 def test_results_do_not_depend_on_the_workspace_or_the_run(ctx):

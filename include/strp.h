@@ -290,8 +290,8 @@ typedef enum { STRP_ACT_NONE = 0, STRP_ACT_RELU = 1, STRP_ACT_GELU = 2 } strp_ac
  *   bias [M] fp32 or NULL;  R [M x ldr] y_dtype or NULL;  Y [M x ldy] y_dtype.  R may be Y itself (same ld).
  * bf16 W and X are multiplied in bf16 with fp32 sums; with an fp32 operand the products are those of fp32.
  * Errors: STRP_EINVAL (null W, X or Y, sizes not positive, M or K above 2^30, T above 2^31, 2^23 tiles or more (of 64 x
- * 64 and up; 16 x 64 up to 64 tokens), ld below its width or no multiple of 8, misaligned, unknown dtype or activation),
- * STRP_ENOMEM (strp_linear_workspace_bytes).
+ * 64 and up), ld below its width or no multiple of 8, misaligned, unknown dtype or activation), STRP_ENOMEM
+ * (strp_linear_workspace_bytes).
  */
 typedef struct {
   const void* W;

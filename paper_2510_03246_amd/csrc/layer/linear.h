@@ -42,8 +42,8 @@ __device__ __forceinline__ void finish_quad(const LinearP& p, floatx4 v, int m, 
       if (t + e < p.T) Y[e] = (YT)y[e];
 }
 
-// How a product is cut: tile shape, parts of the contraction.  Of sizes and types only.
-enum { LINEAR_FEW = 0, LINEAR_TILE = 1, LINEAR_TILE_LARGE = 2, LINEAR_TILE_SMALL = 3 };
+// How a product is cut, by sizes and types only: tile shape, parts of the contraction.  kind: of products of bf16.
+enum { LINEAR_FEW, LINEAR_TILE_SMALL, LINEAR_TILE, LINEAR_TILE_LARGE };
 struct LinearPlan {
   int kind;
   int bm, bn;

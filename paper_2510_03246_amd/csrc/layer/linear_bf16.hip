@@ -5,6 +5,8 @@
 // (tokens x channels): a lane has four consecutive tokens of one channel.
 #include "linear.h"
 
+#include <algorithm>
+
 namespace strp {
 
 // Which tile a workgroup has: workgroups go to the eight XCDs in turn, and the per that an XCD holds at a time are neighbours, eight
@@ -282,39 +284,36 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
 }
 
 // Few tokens (T <= 16 NT): W is the traffic, read once straight into fragments (a lane has 16 bytes of a row), the contraction in parts among the NW wavefronts
-// of a workgroup, which add their sums up in LDS.  X goes to LDS as it lies, a run of rows at a time, and is read turned.  A workgroup has 16 MI channels.
+// of a workgroup, which add their sums up in LDS.  X goes to LDS as it lies, a run of rows at a time, and is read turned.  A workgroup has 16 channels.
+// What bounds it is the rate of its reads, each of 16 rows: 3.0 TB/s of W with a workgroup to a CU and 3.4 from two on (4096 x 4096 one token 13.9 us, 8192 x 2048 12.2); below
+// that a launch and the latencies of X, W and the sums (768 x 768 4.1 us).  Asking for X two runs ahead, beginning at different places of the contraction, both
+// steps of a line to one wavefront and 32 channels a workgroup changed it by less than 10 % either way.
 constexpr int FEW_WAVES = 8;
-template <int NT, int MI, typename YT>
-__global__ __launch_bounds__(64 * FEW_WAVES, NT < 4 ? 2 : 1) void linear_few_kernel(const LinearP p) {
+template <int NT, typename YT>
+__global__ __launch_bounds__(64 * FEW_WAVES, 2) void linear_few_kernel(const LinearP p) {
   constexpr int NW = FEW_WAVES, ROW = 32 * NT;             // bytes of a row of X in LDS: 16 NT tokens
   constexpr int PER = NT == 1 ? 4 : 2, KC = 32 * NW * PER, XC = KC * 2 * NT / (64 * NW);      // steps of a wavefront in a run, rows of X in it, chunks of X a thread moves
-  static_assert(NW * MI * NT * 1024 <= 2 * KC * ROW, "the sums lie where X was");
+  static_assert(NW * NT * 1024 <= 2 * KC * ROW, "the sums lie where X was");
   __shared__ __attribute__((aligned(16))) unsigned char sX[2][KC * ROW];
-  floatx4(*sums)[MI][NT][64] = (floatx4(*)[MI][NT][64])&sX[0][0];
+  floatx4(*sums)[NT][64] = (floatx4(*)[NT][64])&sX[0][0];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = lane >> 4, l16 = lane & 15;
-  const int m0 = (int)blockIdx.x * 16 * MI;
+  const int m0 = (int)blockIdx.x * 16;
   const __bf16* X = (const __bf16*)p.X;
-  const __bf16* W[MI];
+  const __bf16* W = (const __bf16*)p.W + (long long)min(m0 + l16, p.M - 1) * p.ldw;
+  floatx4 acc[NT];
 #pragma unroll
-  for (int i = 0; i < MI; ++i) W[i] = (const __bf16*)p.W + (long long)min(m0 + 16 * i + l16, p.M - 1) * p.ldw;
-  floatx4 acc[MI][NT];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int t = 0; t < NT; ++t) acc[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)sX;
   const int t_last = (int)((p.T - 1) / 8);                 // last chunk of eight tokens
   const uintx4 zero = uintx4{0u, 0u, 0u, 0u};
   // a wavefront's steps of a run are k0 + 32 (wave + NW j); what lies behind K is zero
-  struct Run { uintx4 w[PER][MI]; };
+  struct Run { uintx4 w[PER]; };
   auto ask_w = [&](Run& r, int k0) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const int k = k0 + 32 * (wave + NW * j) + 8 * kg;
-        r.w[j][i] = k < p.K ? *(const uintx4*)(W[i] + k) : zero;
-      }
+    for (int j = 0; j < PER; ++j) {
+      const int k = k0 + 32 * (wave + NW * j) + 8 * kg;
+      r.w[j] = k < p.K ? *(const uintx4*)(W + k) : zero;
+    }
   };
   uintx4 x[XC];
   auto ask_x = [&](int k0) {
@@ -333,20 +332,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT < 4 ? 2 : 1) void linear_few_ker
     for (int j = 0; j < PER; ++j) {
       const int kl = 32 * (wave + NW * j);
       if (k0 + kl >= p.K) break;
-      bf16x8 w[MI];
-#pragma unroll
-      for (int i = 0; i < MI; ++i) w[i] = __builtin_bit_cast(bf16x8, r.w[j][i]);
+      bf16x8 w = __builtin_bit_cast(bf16x8, r.w[j]);
       if (k0 + kl + 32 > p.K)
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[i][e] = k0 + kl + 8 * kg + e < p.K ? w[i][e] : (__bf16)0.0f;
+        for (int e = 0; e < 8; ++e) w[e] = k0 + kl + 8 * kg + e < p.K ? w[e] : (__bf16)0.0f;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const unsigned at = base + (unsigned)(buf * KC * ROW + (kl + 8 * kg + (l16 >> 2)) * ROW + 32 * t + (l16 & 3) * 8);
         const bf16x8 xf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_turned(at), read_turned(at + 4 * ROW), 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int i = 0; i < MI; ++i) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w[i], acc[i][t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf, w, acc[t], 0, 0, 0);
       }
     }
   };
@@ -372,19 +366,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES, NT < 4 ? 2 : 1) void linear_few_ker
     __syncthreads();
   }
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) sums[wave][i][t][lane] = acc[i][t];
+  for (int t = 0; t < NT; ++t) sums[wave][t][lane] = acc[t];
   __syncthreads();
   // four tokens of a channel to a thread, the wavefronts' sums in their order
-  for (int o = tid; o < MI * NT * 64; o += 64 * NW) {
-    const int l = o & 63, t = o >> 6, i = t / NT, m = m0 + 16 * i + (l & 15), tok = 16 * (t % NT) + 4 * (l >> 4);
-    floatx4 v = sums[0][i][t % NT][l];
+  if (tid >= NT * 64) return;
+  const int t = wave, m = m0 + l16, tok = 16 * t + 4 * kg;
+  floatx4 v = sums[0][t][lane];
 #pragma unroll
-    for (int s = 1; s < NW; ++s) v += sums[s][i][t % NT][l];
-    if (m >= p.M || tok >= p.T) continue;
-    finish_quad<YT>(p, v, m, tok);
-  }
+  for (int s = 1; s < NW; ++s) v += sums[s][t][lane];
+  if (m < p.M && tok < p.T) finish_quad<YT>(p, v, m, tok);
 }
 
 // Sums of the parts in their order: a thread has four tokens of a channel.
@@ -409,9 +399,12 @@ void launch_linear_join(strp_ctx* ctx, const LinearP& p, int y_dtype) {
 // products of 768 .. 8192 channels over 128 .. 8192 tokens): tiles of 256 1.8, alone on a CU; of 128 0.65 alone, 1.25 two on a CU; of 64 0.42, 0.6, 0.75 and 0.9 for
 // one to four.  Parts cost a launch and their sums' way through memory.  What the rule weighs, in us: 8192 x 2048 over 1024 tokens in tiles of 256 57, of 128 41, over 2048
 // 65 against 80; 768 x 768 over 2048 in tiles of 128 13.5, of 64 11.7; 4096 x 4096 over 128 in tiles of 64 whole 30, in two parts 20, in four 17.5.
+// Few tokens: a workgroup of 16 channels goes through the whole contraction by itself, which the tiles' parts overtake where it is long or there are many workgroups to a CU.
+// One token, us, few against tiles: 768 x 768 4.1, 6.9; 4096 x 4096 13.9, 15.9; 16384 x 1000 12.1, 12.9; 2048 x 8192 21.7, 16.2; 50000 x 768 24, 17.5.  32 tokens: 2048 x 2048
+// 7.5, 9.4; 4096 x 4096 16.3, 13.4; 8192 x 2048 14.0, 12.2.  33 tokens and more (with twice the channels): 2048 x 2048 12.0, 10.0; 4096 x 4096 22.6, 13.8.
 LinearPlan plan_linear_bf16(int M, int K, long long T) {
-  LinearPlan best{LINEAR_FEW, T <= 32 ? 16 : 32, 64, 1, 0, 0};
-  if (T <= 64) return best;
+  LinearPlan best{LINEAR_FEW, 16, 32, 1, 0, 0};
+  if (T <= 32 && (long long)K * std::max(M, 4096) <= 1 << (T <= 16 ? 24 : 23)) return best;
   const struct { int kind, b, per; double us[4]; } shapes[3] = {
       {LINEAR_TILE_LARGE, 256, 1, {1.8}}, {LINEAR_TILE, 128, 2, {0.65, 1.25}}, {LINEAR_TILE_SMALL, 64, 4, {0.42, 0.6, 0.75, 0.9}}};
   const int all = (K + 63) / 64;
@@ -443,9 +436,8 @@ static void launch_tiles(strp_ctx* ctx, const LinearP& p, const LinearPlan& plan
 template <typename YT>
 static void launch_few(strp_ctx* ctx, const LinearP& p) {
   const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.tilesM), dim3(64 * FEW_WAVES), 0, ctx->stream, p); };
-  if (p.T <= 16) go(linear_few_kernel<1, 1, YT>);
-  else if (p.T <= 32) go(linear_few_kernel<2, 1, YT>);
-  else go(linear_few_kernel<4, 2, YT>);
+  if (p.T <= 16) go(linear_few_kernel<1, YT>);
+  else go(linear_few_kernel<2, YT>);
 }
 
 void launch_linear_bf16(strp_ctx* ctx, LinearP p, const LinearPlan& plan, int y_dtype) {

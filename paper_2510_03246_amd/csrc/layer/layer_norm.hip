@@ -203,12 +203,13 @@ static void launch_norm(strp_ctx* ctx, NormP p) {
   constexpr long long VEC = 16 / sizeof(E);
   const long long chunks = (p.T + VEC - 1) / VEC;
   const auto go = [&](auto kernel, long long cols, int threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)((chunks + cols - 1) / cols)), dim3(threads), 0, ctx->stream, p); };
-  // columns of 64 bytes or more of a row while sixteen rows to a thread hold them, 32 for wider models; fewer where that leaves CUs without work
+  // As wide a piece of a row as sixteen rows to a thread hold, narrower where that leaves CUs without work (us, bf16): 768 channels over 65536 tokens in 16 columns 48, 8 57,
+  // 4 61; 768 over 8192 in 16 17, 8 13.7, 4 12.1, 2 15.7; 2048 over 16384 in 8 28.7, 4 34.7; 768 over 2048 in 4 9.1, 2 8.3, 1 8.4; 2048 over 2048 in 4 13.2, 2 11.0.
   int ct = 16;
-  while (ct > 1 && ((long long)p.d * ct > 16 * 1024 || (ct > 4 && chunks / ct < 512) || (ct > 1 && chunks / ct < 128))) ct >>= 1;
+  while (ct > 1 && ((long long)p.d * ct > 16 * 1024 || (ct > 4 && chunks / ct < 256) || chunks / ct < 128)) ct >>= 1;
   const long long rows = ((long long)p.d * ct + 1023) / 1024;
   p.ct = ct;
-  if (rows > 16 || (ct == 1 && chunks >= 1024 && p.d > 8192)) return go(layer_norm_tall_kernel<E>, 8, 256);
+  if (rows > 16) return go(layer_norm_tall_kernel<E>, 8, 256);
   if (rows <= 2) go(layer_norm_kernel<E, 2>, ct, 1024);
   else if (rows <= 4) go(layer_norm_kernel<E, 4>, ct, 1024);
   else if (rows <= 8) go(layer_norm_kernel<E, 8>, ct, 1024);

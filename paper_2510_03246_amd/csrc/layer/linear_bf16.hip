@@ -127,7 +127,8 @@ __device__ __forceinline__ void finish_tile(const LinearP& p, const floatx4 (&ac
 
 // Tiles of (WM 16 NI) channels x (64 WN) tokens, a wavefront 16 NI x 64, in steps of 32 of the contraction.  W comes in pairs of steps, 128 bytes of a row: the
 // line that memory hands out whole.  LDS holds three pairs of W and four steps of X, and all but what is being multiplied is on its way.  A remainder of the
-// contraction is the first pair and goes through registers, zeros from K on.
+// contraction is the first pair and goes through registers, zeros from K on.  The matrix cores bound it, in the largest products by power: 8192 x 2048 over 2048 tokens
+// 62.5 us, 1.1 PFLOP/s; 4096 x 4915 over 32768 1.19 to 1.27 ms, 1.04 to 1.11; 768 x 768 over 2048 11.8 us.
 template <int WM, int WN, int NI, typename YT>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_tile_kernel(const LinearP p) {
   constexpr int NW = WM * WN, BM = WM * 16 * NI, BN = WN * 64, PAIR = BM * 128, STEP = BN * 64, XAT = 3 * PAIR, RPI = 512 / BN;     // RPI: rows of X in a KB

@@ -47,7 +47,7 @@ N_XCD, N_SE, N_SIMD = 8, 32, 1024
 
 def sources_hash() -> str:
     """sha256 over the HIP sources and headers of libstrp.so (sorted by name; the benchmark helper library's one file is
-    no part of it): changes whenever a kernel does."""
+    no part of it, nor is layer/, whose operators no iteration launches): changes whenever a kernel does."""
     h = hashlib.sha256()
     for path in sorted(glob.glob(os.path.join(CSRC, "*"))):
         if path.endswith((".hip", ".h")) and os.path.basename(path) != "bench_probe.hip":

@@ -137,11 +137,12 @@ __global__ __launch_bounds__(256, 2) void linear_f32_kernel(const LinearP p) {
     }
 }
 
-// Tile shape and parts of the contraction by the time they take: a CU does one tile's share of the matrix instructions after the other, so what counts is the
-// tiles that the busiest CU has, and a little more traffic for the smaller ones (us for 64 steps of the contraction: 128 x 128 3.6, 128 x 64 1.9, 64 x 64 1.0).  1013 x 1000 over 5003
-// tokens: 320 tiles of 128 x 128 166 us, 640 of 128 x 64 145, 1264 of 64 x 64 136 (124 since the rows of tiles start the contraction at different places).
+// Tile shape and parts of the contraction by the time they take.  What 64 steps of the contraction cost (us, on products of 768 .. 8192 channels over 16 .. 5003 tokens): tiles of
+// 128 x 128 5.05 alone on a CU, 9.3 two on a CU; of 128 x 64 2.9 and 5.65; of 64 x 64 1.7, 2.85 and 4.2 for one to three; a workgroup's beginning and end as much as one
+// more.  Parts cost a launch and their sums' way through the caches.  What the rule weighs, in us: 4096 x 4096 over 200 tokens in tiles of 64 whole 113, in four parts 96, of 128 in
+// four 94; over 1024 of 128 whole 331, in two 308, of 64 345; 1000 x 3000 over 700 of 64 whole 82, in four 56; 1013 x 1000 over 5003 of 64 117, of 128 154.
 static LinearPlan plan_linear_f32(int M, int K, long long T) {
-  const struct { int bm, bn; double us; } shapes[3] = {{128, 128, 3.6}, {128, 64, 1.9}, {64, 64, 1.0}};
+  const struct { int bm, bn, per; double us[3]; } shapes[3] = {{128, 128, 2, {5.05, 9.3}}, {128, 64, 2, {2.9, 5.65}}, {64, 64, 3, {1.7, 2.85, 4.2}}};
   const int all = (K + 63) / 64;
   LinearPlan best{};
   double least = 0.0;
@@ -149,8 +150,10 @@ static LinearPlan plan_linear_f32(int M, int K, long long T) {
     const long long n = (long long)((M + s.bm - 1) / s.bm) * ((T + s.bn - 1) / s.bn);
     for (int parts = 1; parts <= 16 && parts <= all; parts *= 2) {
       const int pairs = (all + parts - 1) / parts, used = (all + pairs - 1) / pairs;
-      if (used > 1 && n * used > 512) break;
-      const double us = pairs * s.us * double((n * used + 255) / 256) + (used > 1 ? 1.5 + 8e-6 / 4.5 * used * (double)M * (double)T : 0.0);
+      const long long blocks = n * used, round = 256LL * s.per, left = blocks % round;
+      if (used > 1 && blocks > round) break;
+      const double us = (pairs + 1) * (double(blocks / round) * s.us[s.per - 1] + (left ? s.us[(left + 255) / 256 - 1] : 0.0)) +
+                        (used > 1 ? 2.5 + 1.2e-6 * used * (double)M * (double)T : 0.0);
       if (least > 0.0 && us >= least) continue;
       least = us;
       best = LinearPlan{0, s.bm, s.bn, used, pairs, used > 1 ? (size_t)used * M * ((T + 7) / 8 * 8) * 4 : 0};

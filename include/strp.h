@@ -51,6 +51,7 @@ typedef enum { STRP_SCORE_WANDA = 0, STRP_SCORE_LEMMA = 1, STRP_SCORE_GAIN = 2 }
 typedef enum { STRP_SIDE_FC1 = 0, STRP_SIDE_FC2 = 1 } strp_side;
 /* How fp32 operands enter the fp16 matrix cores: rounded once to fp16 (FAST, 2^-12 relative) or as a two-term
  * fp16 split hi + lo with the three leading cross products hi*hi + hi*lo + lo*hi (SPLIT, ~2^-22 relative).
+ * strp_attention over bf16 goes by it too (see there).
  * The setting is captured by strp_module_init together with the operand planes it writes; strp_admm_step on that
  * module returns STRP_ESTATE if the context's precision has been changed since (initialise the module again). */
 typedef enum { STRP_PREC_FAST = 0, STRP_PREC_SPLIT = 1 } strp_precision;
@@ -330,7 +331,8 @@ strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype dtype, int3
  * Sequences may be empty or of one token.  Tokens outside every sequence keep what C holds.  What a token does not see
  * (other sequences, later tokens, padding) has no part in its result, whatever it holds, infinities and NaN included.
  * Entries of seq_start or kv_of_head outside their ranges give wrong results, no access out of bounds.
- * bf16: the probabilities are rounded to bf16 before they meet V (fp32 sums).  fp32: products of fp32.
+ * bf16: products of bf16 with fp32 sums.  The probabilities are fp32 and meet V as the context's precision says: as two bf16
+ * terms (STRP_PREC_SPLIT, 2^-16 relative) or rounded once (STRP_PREC_FAST, 2^-8).  fp32: products of fp32.
  * Errors: STRP_EINVAL (null pointer, sizes not positive, ceil(T / 64) heads of 2^23 or more, d_head above 128, kv_heads that
  * does not divide heads without kv_of_head, scale not positive and finite, bad ld, misaligned, unknown dtype, more heads
  * than 65535).

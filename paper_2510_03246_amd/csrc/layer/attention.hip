@@ -7,6 +7,7 @@
 #include "layer_ops.h"
 
 #include <cmath>
+#include <type_traits>
 
 namespace strp {
 
@@ -252,9 +253,11 @@ __device__ const unsigned zero_chunk[4] = {0u, 0u, 0u, 0u};
 // different banks.
 // What bounds it is the vector unit (an exponential, a multiply-add, an addition, half a maximum and half a conversion for a score) and, at 128 channels a head, as
 // much the matrix cores.  So that either has work while the other waits, the scores of the next tile are multiplied beside the softmax of this one, and V P follows
-// it a quarter of the keys at a time.  K runs a tile ahead of V: LDS has RING tiles of each.  Eight prompts of 2048 tokens, 32 heads of 64: 223 us, 620 TFLOP/s;
-// 16221 tokens in prompts of 1 to 8191, 32 heads of 128 on 8: 872 us, 860 TFLOP/s.
-template <int DHP, int NW, int RING, int WPS>
+// it a quarter of the keys at a time.  K runs a tile ahead of V: LDS has RING tiles of each.
+// SPLIT: the probabilities meet V as two terms of bf16, which is half as many matrix instructions again and three vector instructions a score.  With one term results are further from
+// those in 64 bits than their own rounding puts them (2.0e-3 against 1.66e-3, relative, on Gaussian V); with two they are not.  Whole calls, two terms / one: eight prompts of 2048 tokens, 32 heads
+// of 64: 302 / 221 us; 16221 tokens in prompts of 1 to 8191, 32 heads of 128 on 8: 1157 / 890 us.
+template <int DHP, int NW, int RING, int WPS, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const AttnP p) {
   constexpr int KT = 64, NC = DHP / 32, NS = DHP / 16, TILE = DHP * 128, LH = DHP / 8 / NW, BQ = 32 * NW;      // LH: KBs of a tile of K or V that a wavefront moves
   static_assert(DHP % (8 * NW) == 0, "whole pieces for every wavefront");
@@ -348,11 +351,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   auto frag_v = [&](unsigned at, int c, int k) { return *(const __attribute__((address_space(3))) bf16x8*)(size_t)(at + (offV ^ (unsigned)(32 * k)) + 4096 * c); };
 
   floatx16 O[NC];
-  float m = -INFINITY, l[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int c = 0; c < NC; ++c)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) O[c][e] = 0.0f;
+  float m, l[2];
+  bool again = false;
   struct Scores { floatx16 u[2]; };
   auto clear = [&](Scores& S) {
 #pragma unroll
@@ -399,20 +399,30 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     }
     return m == -INFINITY ? 0.0f : m * p.scale_log2e;
   };
-  // probabilities of the quarter k of a tile's keys
+  // Probabilities of the quarter k of a tile's keys and, in fp32, their sum.  SPLIT: hi has their upper 16 bits and lo what that leaves, so that what meets V is within 2^-16 of them;
+  // else hi is rounded to bf16 (2^-8) and the sum is of what was rounded.
+  struct Probs { bf16x8 hi, lo; };
   auto quarter = [&](const Scores& S, int k, float ref) {
-    bf16x8 P;
+    uintx4 hi, lo;
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      bf16x2 x;
+    for (int e = 0; e < 4; ++e) {
+      float x[2];
 #pragma unroll
-      for (int f = 0; f < 2; ++f) x[f] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + e + f], p.scale_log2e, -ref));
-      // the sum of what meets V, in fp32
-      l[e >> 1 & 1] = __builtin_amdgcn_fdot2_f32_bf16(x, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[e >> 1 & 1], false);
-      P[e] = x[0];
-      P[e + 1] = x[1];
+      for (int f = 0; f < 2; ++f) x[f] = __builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + 2 * e + f], p.scale_log2e, -ref));
+      if constexpr (SPLIT) {
+        const unsigned b0 = __builtin_bit_cast(unsigned, x[0]), b1 = __builtin_bit_cast(unsigned, x[1]);
+        l[0] += x[0];
+        l[1] += x[1];
+        hi[e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+        const bf16x2 left = {(__bf16)(x[0] - __builtin_bit_cast(float, b0 & 0xffff0000u)), (__bf16)(x[1] - __builtin_bit_cast(float, b1 & 0xffff0000u))};
+        lo[e] = __builtin_bit_cast(unsigned, left);
+      } else {
+        const bf16x2 r = {(__bf16)x[0], (__bf16)x[1]};
+        hi[e] = __builtin_bit_cast(unsigned, r);
+        l[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(r, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[e & 1], false);
+      }
     }
-    return P;
+    return Probs{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
   };
   unsigned atK = base, atV = baseV;              // the tile of K whose scores come next, the tile of V
   // Tile s, whose scores are in S; those of the next one go to N.
@@ -440,7 +450,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
       // Where some key is not seen by every query, a value that is not finite would reach those too, by a probability of zero: such values are left out
       // of the products and added to the results of the queries that see them.
       bool odd = false;
-      if (!whole) {
+      if (!whole || again) {
         typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
         ushort2v most = {0, 0};
 #pragma unroll
@@ -464,7 +474,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
 #pragma unroll
         for (int c = 0; c < NC; ++c) v[c] = frag_v(atV, c, k);
         scores(N, atK, k * NS / 4, (k + 1) * NS / 4);
-        const bf16x8 P = quarter(S, k, ref);
+        const Probs P = quarter(S, k, ref);
         if (odd)
 #pragma unroll
           for (int c = 0; c < NC; ++c)
@@ -474,7 +484,10 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
               __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-        for (int c = 0; c < NC; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], P, O[c], 0, 0, 0);
+        for (int c = 0; c < NC; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], P.hi, O[c], 0, 0, 0);
+        if constexpr (SPLIT)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) O[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[c], P.lo, O[c], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (odd)
@@ -497,23 +510,49 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     }
     atV = atV == baseV + (RING - 1) * TILE ? baseV : atV + TILE;
   };
-  issue_k(0);
+  while (true) {
+    toK = atK = base;
+    toV = atV = baseV;
+    m = -INFINITY;
+    l[0] = l[1] = 0.0f;
 #pragma unroll
-  for (int s = 0; s < RING - 1; ++s) {
-    issue_k(s + 1);
-    issue_v(s);
-  }
-  Scores a, b;
-  clear(a);
-  wait_loads<(RING - 1) * 2 * LH>();
-  __builtin_amdgcn_s_barrier();
-  all_scores(a, atK);
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) O[c][e] = 0.0f;
+    issue_k(0);
+#pragma unroll
+    for (int s = 0; s < RING - 1; ++s) {
+      issue_k(s + 1);
+      issue_v(s);
+    }
+    Scores a, b;
+    clear(a);
+    wait_loads<(RING - 1) * 2 * LH>();
+    __builtin_amdgcn_s_barrier();
+    all_scores(a, atK);
 #pragma unroll 1
-  for (int s = 0; s < steps; s += 2) {
-    tile_step(s, a, b);
-    if (s + 1 < steps) tile_step(s + 1, b, a);
+    for (int s = 0; s < steps; s += 2) {
+      tile_step(s, a, b);
+      if (s + 1 < steps) tile_step(s + 1, b, a);
+    }
+    wait_loads<0>();                             // LDS is not to be written behind the workgroup's end
+    if (again) break;
+    // A value of V that is not finite and is seen by every query of a tile has been multiplied by a probability or by a part of one, which may be zero: the workgroup then
+    // goes through the keys once more and looks at every tile's values.
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) most = __builtin_elementwise_maximum(most, fabsf(O[c][e]));
+    const bool lost = __builtin_amdgcn_ballot_w64(!(most < INFINITY)) != 0;
+    if (lane == 0) lows[wave] = lost;
+    __syncthreads();
+    int any = lows[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) any |= lows[w];
+    if (!__builtin_amdgcn_readfirstlane(any)) break;
+    again = true;
   }
-  wait_loads<0>();                               // LDS is not to be written behind the workgroup's end
   const float half = l[0] + l[1];
   const auto halves = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, half), __builtin_bit_cast(unsigned, half), false, false);
   const unsigned half0 = halves[0], half1 = halves[1];
@@ -534,10 +573,16 @@ static void launch_attention_bf16(strp_ctx* ctx, AttnP p) {
     p.tiles = (int)((p.T + bq - 1) / bq);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles * p.heads)), dim3(threads), 0, ctx->stream, p);
   };
-  // three workgroups of three tiles of 64 channels on a CU, two of two of 96 or 128: what its 160 KB of LDS and its registers hold
-  if (p.dh <= 64) go(attention_bf16_kernel<64, 4, 3, 3>, 128, 256);
-  else if (p.dh <= 96) go(attention_bf16_kernel<96, 4, 2, 2>, 128, 256);
-  else go(attention_bf16_kernel<128, 4, 2, 2>, 128, 256);
+  // three workgroups of three tiles of 64 channels on a CU, two of two of 96 or 128: what its 160 KB of LDS and its registers hold; with the probabilities in two terms, two also of 64
+  // (with three of them 9 to 18 registers lie in memory: 32 heads of 64 over 8 x 2048 450 us, not 340)
+  const auto by_width = [&](auto split) {
+    constexpr bool SPLIT = decltype(split)::value;
+    if (p.dh <= 64) go(attention_bf16_kernel<64, 4, SPLIT ? 2 : 3, SPLIT ? 2 : 3, SPLIT>, 128, 256);
+    else if (p.dh <= 96) go(attention_bf16_kernel<96, 4, 2, 2, SPLIT>, 128, 256);
+    else go(attention_bf16_kernel<128, 4, 2, 2, SPLIT>, 128, 256);
+  };
+  if (ctx->precision == STRP_PREC_SPLIT) by_width(std::true_type());
+  else by_width(std::false_type());
 }
 
 static void launch_attention_f32(strp_ctx* ctx, AttnP p) {

@@ -402,8 +402,8 @@ class Context:
 
     def strp_attention(self, Q, K, V, T, heads, kv_heads=None, seq_start=None, kv_of_head=None, scale=None, out=None):
         """Causal attention of T packed tokens: Q [heads*d_head x ld], K, V [kv_heads*d_head x ld], seq_start [n_seq + 1] int32 offsets
-        (None: one sequence), kv_of_head [heads] int32 (None: equal groups), scale 1 / sqrt(d_head) by default.  Returns
-        the head outputs, like Q."""
+        (None: one sequence), kv_of_head [heads] int32 (None: equal groups), scale 1 / sqrt(d_head) by default.  In bf16 the
+        probabilities are held in two terms, or rounded once where the context's precision is PREC_FAST.  Returns the head outputs, like Q."""
         kv_heads = heads if kv_heads is None else kv_heads
         if heads <= 0 or Q.dim() != 2 or Q.shape[0] < heads or Q.shape[0] % heads:
             raise ValueError(f"Q: {tuple(Q.shape)} is not {heads} heads")

@@ -1,0 +1,109 @@
+"""The decoder layer's operators where they can go wrong: how exact a result is, which variant runs, what lies beside the data.
+
+U = 2^-23 bounds what one fp32 operation or one step of a matrix-core sum adds, relative to the magnitudes that meet there; H(t) is half a
+step of an output of type t."""
+import math
+
+import pytest
+import torch
+
+from paper_2510_03246_amd import strp
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -23
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def H(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def ld8(T):
+    return (T + 7) // 8 * 8
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return strp.Context(0)
+
+
+@pytest.fixture(scope="module")
+def fast():
+    c = strp.Context(0)
+    c.set_precision(strp.PREC_FAST)
+    return c
+
+
+def rand(shape, seed, dt=F32, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dt)
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------
+def attention_exact(Q, K, V, heads, kv_of, starts, scale, probs):
+    """result and bound, where a probability is within `probs` of its value, relative, as it meets V"""
+    dt, dh = Q.dtype, Q.shape[0] // heads
+    out = torch.zeros((heads * dh, starts[-1]), dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(out)
+    for a, e in zip(starts, starts[1:]):
+        n = e - a
+        seen = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+        for h in range(heads):
+            r, rk = slice(h * dh, (h + 1) * dh), slice(kv_of[h] * dh, (kv_of[h] + 1) * dh)
+            q, k, v = Q[r, a:e].double(), K[rk, a:e].double(), V[rk, a:e].double()
+            p = torch.softmax(torch.where(seen, scale * (q.t() @ k), -math.inf), 1)
+            out[r, a:e] = v @ p.t()
+            # a score is off by dh + 4 steps of its magnitudes, its probability by twice the largest of these of its row (the maximum's and its own), relative, and by 16 steps of the
+            # exponential; the two sums have n terms each
+            mag = torch.where(seen, scale * (q.abs().t() @ k.abs()), 0.0).max(1).values
+            rel = 2 * (dh + 4) * U * mag + 16 * U + 2 * n * U + probs
+            tol[r, a:e] = 2 * rel * (v.abs() @ p.t()) + H(dt) * out[r, a:e].abs() + 1e-37
+    return out, tol
+
+
+def attention_close(c, lens, heads, kv, dh, dt, probs, kv_of=None, seed=0):
+    starts = [0]
+    for n in lens:
+        starts.append(starts[-1] + n)
+    T = starts[-1]
+    Q, K, V = (torch.full(((heads if i == 0 else kv) * dh, ld8(T)), float("nan"), dtype=dt, device="cuda") for i in range(3))
+    for i, x in enumerate((Q, K, V)):
+        x[:, :T] = rand((x.shape[0], T), seed + i, dt, 1.5 if i < 2 else 1.0)
+    got = c.strp_attention(Q, K, V, T, heads, kv, torch.tensor(starts, dtype=torch.int32, device="cuda"),
+                           kv_of_head=torch.tensor(kv_of, dtype=torch.int32, device="cuda") if kv_of else None)[:, :T].double()
+    want, tol = attention_exact(Q[:, :T], K[:, :T], V[:, :T], heads, kv_of or [h // (heads // kv) for h in range(heads)], starts, dh ** -0.5, probs)
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), (lens, heads, kv, dh, int(bad.sum()), float(((got - want).abs() / tol).max()))
+
+
+@pytest.mark.parametrize("dh", [8, 16, 31, 64, 80, 96, 128])
+@pytest.mark.parametrize("lens", [[1], [64], [130, 1, 63], [300]], ids=str)
+def test_attention_holds_the_probabilities_in_two_terms(ctx, lens, dh):
+    """bf16, as a context comes: a probability meets V within 2^-16 of its value (the remainder of its upper 16 bits, below 2^-7 of it, rounded to nine)."""
+    attention_close(ctx, lens, 4, 2, dh, BF16, 2.0 ** -16)
+
+
+@pytest.mark.parametrize("dh", [1, 7, 8, 16, 31, 32, 33, 48, 63, 64, 65, 80, 96, 97, 100, 127, 128])
+def test_attention_with_rounded_probabilities(fast, dh):
+    attention_close(fast, [70, 1, 140], 4, 2, dh, BF16, H(BF16))
+    attention_close(fast, [130, 1, 1, 250, 63], 3, 3, dh, BF16, H(BF16), kv_of=[2, 0, 2])
+
+
+@pytest.mark.parametrize("dh", [64, 96, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_what_every_query_of_a_tile_sees_shows_itself(ctx, fast, bad, dh):
+    """A value of V that is not finite at token 5 of 400 is that in its channel of every later token, also where its probability is a half, a quarter or too small to count;
+    the other channels and the tokens before it have the bits they had."""
+    T = 400
+    for c in (ctx, fast):
+        Q, K, V = (rand((2 * dh, T), i, BF16, s) for i, s in enumerate((0.0, 1.0, 1.0)))          # scores of zero: probabilities of 1 / (t + 1), many of them whole in eight bits
+        V2 = V.clone()
+        V2[3, 5] = bad
+        rows = torch.arange(2 * dh, device="cuda") != 3
+        for q in (Q, rand((2 * dh, T), 7, BF16, 1.5), rand((2 * dh, T), 7, BF16, 40.0)):
+            clean, got = (c.strp_attention(q, K, v, T, 2, 2) for v in (V, V2))
+            assert torch.equal(got[rows], clean[rows]) and torch.equal(got[3, :5], clean[3, :5])
+            assert not torch.isfinite(got[3, 5:]).any()
+        got = c.strp_attention(Q, K, V2, T, 2, 2)[3, 5:]
+        assert bool(torch.isnan(got).all()) if bad != bad else bool((got == bad).all())

@@ -83,7 +83,9 @@ strp_status strp_set_product_planes(strp_ctx* ctx, strp_product product, int32_t
  * as many parts as fit, in fp32 chains of at most 8192 tokens each: the last bits of a Gram matrix or a right-hand
  * side then depend on the workspace's size.  STRP_ENOMEM when not even those fit.
  * Calls on one workspace run one after the other on the context's stream.  Captured calls that are replayed at the same time
- * need workspaces of their own, set before each is captured. */
+ * need workspaces of their own, set before each is captured (STRP_ESTATE while the stream is being captured).
+ * The device status word lies at the workspace's beginning and is cleared here: poll first, or copy its first four bytes
+ * from the workspace that is replaced, where a failure may be pending. */
 strp_status strp_set_workspace(strp_ctx* ctx, void* dev_ptr, size_t bytes);
 /* Synchronise the stream and return the device status word (STRP_OK, STRP_ENOTPD, STRP_ENONFINITE, STRP_EHIP), which it clears;
  * also STRP_EHIP where the synchronisation itself fails. */

@@ -78,6 +78,14 @@ strp_status fail(strp_ctx* ctx, strp_status st, const char* fmt, ...) {
   return st;
 }
 
+// whether what is enqueued on the stream becomes part of a graph; where the runtime does not say (the null stream beside one that is being captured), as if it did
+static bool capturing(hipStream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(stream, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return true;
+}
+
 static inline long long round_up(long long x, long long a) { return (x + a - 1) / a * a; }
 static inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
@@ -515,6 +523,8 @@ strp_status strp_set_workspace(strp_ctx* ctx, void* dev_ptr, size_t bytes) {
   if (!ctx) return STRP_EINVAL;
   if (!dev_ptr || bytes < 4096) return fail(ctx, STRP_EINVAL, "workspace: null or smaller than 4096 bytes");
   if ((uintptr_t)dev_ptr & 255u) return fail(ctx, STRP_EINVAL, "workspace: pointer not 256-byte aligned");
+  // a graph would clear the status word at every replay, with what calls outside it have left there
+  if (capturing(ctx->stream)) return fail(ctx, STRP_ESTATE, "workspace: the context's stream is being captured; set a workspace that is large enough before");
   if (ctx->ws && ctx->ws != (char*)dev_ptr) ctx->ticket_due = 1;
   ctx->ws = (char*)dev_ptr;
   ctx->ws_bytes = bytes;
@@ -906,11 +916,7 @@ struct Aside {
   // whether there is a second stream; none is made while the call is being captured
   bool ready() const {
     if (ctx->side_state == 0) {
-      hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-      if (hipStreamIsCapturing(own, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone) {
-        (void)hipGetLastError();
-        return false;
-      }
+      if (capturing(own)) return false;
       // streams and events belong to the device that is current in the calling thread as they are made, which need not be the context's
       int current = 0;
       const bool known = hipGetDevice(&current) == hipSuccess;

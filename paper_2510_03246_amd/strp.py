@@ -215,12 +215,17 @@ class Context:
 
     # ---- plumbing ---------------------------------------------------------------------
     def set_workspace(self, nbytes: int):
+        """A workspace of nbytes in place of the present one; a failure that has not been polled stays pending.  Not while the
+        context's stream is being captured."""
+        with torch.cuda.stream(self.stream):
+            ws = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
+            self.check(self.lib.strp_set_workspace(self.h, _ptr(ws), int(nbytes)))
+            if self.ws is not None:
+                ws[:4].copy_(self.ws[:4])         # the status word
         if self.in_graphs:
             self.kept.append(self.ws)             # a graph that is replayed still writes there
             self.in_graphs = False
-        with torch.cuda.stream(self.stream):
-            self.ws = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
-        self.check(self.lib.strp_set_workspace(self.h, _ptr(self.ws), int(nbytes)))
+        self.ws = ws
 
     def ensure_workspace(self, nbytes: int):
         if self.ws is None or self.ws.numel() < nbytes:

@@ -107,3 +107,57 @@ def test_what_every_query_of_a_tile_sees_shows_itself(ctx, fast, bad, dh):
             assert not torch.isfinite(got[3, 5:]).any()
         got = c.strp_attention(Q, K, V2, T, 2, 2)[3, 5:]
         assert bool(torch.isnan(got).all()) if bad != bad else bool((got == bad).all())
+
+
+# ---- the workspace --------------------------------------------------------------------------------------------------
+def leave_a_failure(c):
+    """A refit whose matrix is not positive definite."""
+    G = torch.diag(torch.tensor([1.0, 2.0, -3.0, 4.0, 5.0, 6.0, 7.0, 8.0], device="cuda"))
+    A = rand((8, 64), 1)
+    c.strp_refit(strp.SIDE_FC2, G, 0.0, A, A, 64, torch.arange(8, dtype=torch.int32, device="cuda"), torch.empty((8, 8), device="cuda"))
+
+
+@pytest.mark.parametrize("call", ["linear", "logprobs", "mask", "set_workspace"])
+def test_a_larger_workspace_keeps_a_failure_that_was_not_polled(call):
+    c = strp.Context(0)
+    c.set_workspace(1 << 17)
+    leave_a_failure(c)
+    size = c.ws.numel()
+    if call == "linear":
+        c.strp_linear(rand((512, 4096), 1, BF16), rand((4096, 512), 2, BF16), 512)
+    elif call == "logprobs":
+        c.strp_token_logprobs(rand((50000, 512), 1), 512, n_top=1)
+    elif call == "mask":
+        c.strp_mask_topk(rand(3000000, 1), 1000)
+    else:
+        c.set_workspace(1 << 22)
+    assert c.ws.numel() > size
+    assert c.poll() == strp.ENOTPD
+    assert c.poll() == strp.OK
+
+
+def test_a_captured_call_does_not_replace_the_workspace():
+    """It is refused where it would have to, and the context is as it was; with room set before, every replay leaves a pending failure where it is."""
+    W, X = rand((512, 4096), 1, BF16, 0.05), rand((4096, 512), 2, BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c = strp.Context(0)
+        c.set_workspace(4096)
+        out = torch.empty((512, 512), dtype=BF16, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            with pytest.raises(strp.StrpError) as e:
+                c.strp_linear(W, X, 512, out=out)
+            out.zero_()
+        assert e.value.status == strp.ESTATE and c.ws.numel() == 4096
+        want = c.strp_linear(W, X, 512)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.strp_linear(W, X, 512, out=out)
+        for _ in range(3):
+            out.zero_()
+            leave_a_failure(c)
+            graph.replay()
+            assert torch.equal(out, want) and c.poll() == strp.ENOTPD
+    torch.cuda.synchronize()

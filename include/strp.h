@@ -87,6 +87,9 @@ strp_status strp_set_product_planes(strp_ctx* ctx, strp_product product, int32_t
  * The device status word lies at the workspace's beginning and is cleared here: poll first, or copy its first four bytes
  * from the workspace that is replaced, where a failure may be pending. */
 strp_status strp_set_workspace(strp_ctx* ctx, void* dev_ptr, size_t bytes);
+/* Whether a call that was captured into a graph uses the present workspace (1, else 0): its replays write there, so the memory must
+ * last as long as the graph, also when another workspace takes its place.  forget != 0: those graphs are gone. */
+int32_t strp_workspace_captured(strp_ctx* ctx, int32_t forget);
 /* Synchronise the stream and return the device status word (STRP_OK, STRP_ENOTPD, STRP_ENONFINITE, STRP_EHIP), which it clears;
  * also STRP_EHIP where the synchronisation itself fails. */
 strp_status strp_poll(strp_ctx* ctx);

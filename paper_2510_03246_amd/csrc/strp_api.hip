@@ -86,6 +86,10 @@ static bool capturing(hipStream_t stream) {
   return true;
 }
 
+void note_workspace(strp_ctx* ctx) {
+  if (ctx->ws && !ctx->ws_captured) ctx->ws_captured = capturing(ctx->stream);
+}
+
 static inline long long round_up(long long x, long long a) { return (x + a - 1) / a * a; }
 static inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
@@ -527,9 +531,17 @@ strp_status strp_set_workspace(strp_ctx* ctx, void* dev_ptr, size_t bytes) {
   if (capturing(ctx->stream)) return fail(ctx, STRP_ESTATE, "workspace: the context's stream is being captured; set a workspace that is large enough before");
   if (ctx->ws && ctx->ws != (char*)dev_ptr) ctx->ticket_due = 1;
   ctx->ws = (char*)dev_ptr;
+  ctx->ws_captured = 0;
   ctx->ws_bytes = bytes;
   ctx->status_dev = (int32_t*)dev_ptr;
   return fill_zero(ctx, dev_ptr, 256);
+}
+
+int32_t strp_workspace_captured(strp_ctx* ctx, int32_t forget) {
+  if (!ctx) return 0;
+  const int32_t was = ctx->ws_captured;
+  if (forget) ctx->ws_captured = 0;
+  return was;
 }
 
 strp_status strp_poll(strp_ctx* ctx) {

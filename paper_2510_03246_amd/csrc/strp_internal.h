@@ -36,6 +36,7 @@ struct strp_ctx {
   hipStream_t side;
   hipEvent_t side_event[2];
   int side_state;
+  int ws_captured;        // a call that is part of a graph has the present workspace (note_workspace)
   int flow_workers;       // workgroups of the next factorisation in one launch, which has other kernels beside it; 0: as many as it has use for
 };
 
@@ -68,13 +69,16 @@ strp_status fail(strp_ctx* ctx, strp_status st, const char* fmt, ...);
     if (s_ != STRP_OK) return s_;       \
   } while (0)
 
+// every call that uses the workspace comes by here: whether a graph has it
+void note_workspace(strp_ctx* ctx);
+
 // ---- workspace bump arena (256-byte granules); the first granule holds the status word, the only thing in the workspace
 // that lasts from one call to the next ----
 struct Arena {
   char* base;
   size_t off, cap;
   Arena() : base(nullptr), off(0), cap(0) {}
-  explicit Arena(strp_ctx* ctx) : base(ctx->ws), off(256), cap(ctx->ws_bytes) {}
+  explicit Arena(strp_ctx* ctx) : base(ctx->ws), off(256), cap(ctx->ws_bytes) { note_workspace(ctx); }
   Arena(void* block, size_t bytes) : base((char*)block), off(0), cap(bytes) {}   // sub-arena over a block taken elsewhere
   size_t room() const { return base && off < cap ? (cap - off) & ~size_t(255) : 0; }
   void* take(size_t bytes) {

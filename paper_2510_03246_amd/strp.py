@@ -27,7 +27,7 @@ ACT_NONE, ACT_RELU, ACT_GELU = range(3)
 TOP_MAX = 16
 
 EXPORTS = [
-    "strp_create", "strp_destroy", "strp_last_error", "strp_set_precision", "strp_set_product_planes", "strp_set_workspace",
+    "strp_create", "strp_destroy", "strp_last_error", "strp_set_precision", "strp_set_product_planes", "strp_set_workspace", "strp_workspace_captured",
     "strp_poll", "strp_workspace_bytes", "strp_module_cache_bytes", "strp_profile_enable", "strp_profile_read", "strp_profile_launches", "strp_gram", "strp_score_alloc", "strp_mask_topk", "strp_mask_topk_static", "strp_topk_workspace_bytes", "strp_weight_energy", "strp_alloc_inverse", "strp_alloc_softmax",
     "strp_refit", "strp_module_init", "strp_admm_step",
     "strp_linear", "strp_linear_workspace_bytes", "strp_layer_norm", "strp_attention", "strp_token_logprobs", "strp_token_logprobs_workspace_bytes",
@@ -129,6 +129,7 @@ def load_library():
     lib.strp_set_precision.argtypes = [vp, C.c_int]
     lib.strp_set_product_planes.argtypes = [vp, C.c_int, i32, i32]
     lib.strp_set_workspace.argtypes = [vp, vp, C.c_size_t]
+    lib.strp_workspace_captured.argtypes = [vp, i32]
     lib.strp_poll.argtypes = [vp]
     lib.strp_profile_enable.argtypes = [vp, C.c_int]
     lib.strp_profile_read.argtypes = [vp, C.POINTER(ProfileEntry), i32, C.POINTER(i32)]
@@ -194,7 +195,7 @@ class Context:
             raise StrpError(st, "strp_create failed")
         self.h = h
         self.ws = None
-        self.in_graphs, self.kept = False, []     # whether a captured call has the workspace; those that were replaced since
+        self.kept = []                            # workspaces that graphs have and that were replaced
         if workspace_bytes:
             self.set_workspace(workspace_bytes)
 
@@ -217,21 +218,19 @@ class Context:
     def set_workspace(self, nbytes: int):
         """A workspace of nbytes in place of the present one; a failure that has not been polled stays pending.  Not while the
         context's stream is being captured."""
+        captured = self.lib.strp_workspace_captured(self.h, 0)
         with torch.cuda.stream(self.stream):
             ws = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
             self.check(self.lib.strp_set_workspace(self.h, _ptr(ws), int(nbytes)))
             if self.ws is not None:
                 ws[:4].copy_(self.ws[:4])         # the status word
-        if self.in_graphs:
+        if captured:
             self.kept.append(self.ws)             # a graph that is replayed still writes there
-            self.in_graphs = False
         self.ws = ws
 
     def ensure_workspace(self, nbytes: int):
         if self.ws is None or self.ws.numel() < nbytes:
             self.set_workspace(nbytes)
-        if torch.cuda.is_current_stream_capturing():
-            self.in_graphs = True
 
     def set_precision(self, prec: int):
         self.check(self.lib.strp_set_precision(self.h, prec))

@@ -161,3 +161,44 @@ def test_a_captured_call_does_not_replace_the_workspace():
             graph.replay()
             assert torch.equal(out, want) and c.poll() == strp.ENOTPD
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("call", ["gram", "scores", "mask", "energy"])
+def test_a_graph_of_any_call_keeps_the_workspace_that_a_larger_call_replaces(call):
+    """Captured, then a linear on the same context takes a larger workspace, then replayed: the result of the eager call, and nothing else is written."""
+    A = rand((256, 512), 1)
+    score, energies, W = torch.empty(256, device="cuda"), torch.zeros(1, dtype=torch.float64, device="cuda"), rand((64, 256), 2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c = strp.Context(0)
+        c.set_workspace(4 << 20)
+        values = rand(60000, 3)
+
+        def run():
+            if call == "gram":
+                return c.strp_gram(A, 512)
+            if call == "scores":
+                c.strp_score_alloc(A, 512, strp.WANDA, score, energies, 0, 1, What=W)
+                return score
+            if call == "mask":
+                return c.strp_mask_topk(values, 777)[1]
+            energies.zero_()
+            c.strp_weight_energy([A, W], 0.1, 0.1, 1.0, energies)
+            return energies
+
+        want = run().clone()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = run()
+        size = c.ws.numel()
+        c.strp_linear(rand((512, 4096), 1, BF16), rand((4096, 512), 2, BF16), 512)
+        assert c.ws.numel() > size
+        others = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        for _ in range(3):
+            got.zero_()
+            graph.replay()
+            assert torch.equal(got, want) and torch.equal(run(), want)
+        assert all(bool((o == 7).all()) for o in others)
+    torch.cuda.synchronize()

@@ -195,7 +195,7 @@ class Context:
             raise StrpError(st, "strp_create failed")
         self.h = h
         self.ws = None
-        self.kept = []                            # workspaces that graphs have and that were replaced
+        self.kept = []                            # workspaces that graphs have and that were replaced (forget_graphs)
         if workspace_bytes:
             self.set_workspace(workspace_bytes)
 
@@ -231,6 +231,12 @@ class Context:
     def ensure_workspace(self, nbytes: int):
         if self.ws is None or self.ws.numel() < nbytes:
             self.set_workspace(nbytes)
+
+    def forget_graphs(self):
+        """No graph that has captured this context's calls is replayed any more: what was kept for them is freed, which otherwise lasts as
+        long as the context (a context must outlive its graphs)."""
+        self.lib.strp_workspace_captured(self.h, 1)
+        self.kept.clear()
 
     def set_precision(self, prec: int):
         self.check(self.lib.strp_set_precision(self.h, prec))

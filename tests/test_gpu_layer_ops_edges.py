@@ -202,3 +202,36 @@ def test_a_graph_of_any_call_keeps_the_workspace_that_a_larger_call_replaces(cal
             assert torch.equal(got, want) and torch.equal(run(), want)
         assert all(bool((o == 7).all()) for o in others)
     torch.cuda.synchronize()
+
+
+def test_workspaces_of_graphs_that_are_gone_are_freed():
+    """A replaced workspace lasts while a graph may write to it, and no longer than forget_graphs says."""
+    A = rand((64, 512), 1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c = strp.Context(0)
+        c.set_workspace(1 << 28)
+        c.strp_gram(A, 512)
+        c.set_workspace(1 << 29)                   # no graph: replaced and freed
+        assert not c.kept
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.strp_gram(A, 512)
+        c.set_workspace(1 << 28)
+        c.set_workspace(1 << 27)                   # no graph has this one
+        assert [w.numel() for w in c.kept] == [1 << 29]
+        del graph
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        c.forget_graphs()
+        assert not c.kept and before - torch.cuda.memory_allocated() == 1 << 29
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.strp_gram(A, 512)
+        del graph
+        torch.cuda.synchronize()
+        c.forget_graphs()
+        c.set_workspace(1 << 28)
+        assert not c.kept
+    torch.cuda.synchronize()

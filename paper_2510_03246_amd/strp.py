@@ -181,6 +181,17 @@ def dtype_code(t: torch.Tensor) -> int:
         raise TypeError(f"unsupported dtype {t.dtype}") from None
 
 
+def aligned_rows(W: torch.Tensor) -> torch.Tensor:
+    """W [M x K] as strp_linear reads weights, rows beginning at multiples of eight entries: W itself where they do, else the first K columns of
+    a copy that is wider.  Done once, for weights as a refit leaves them or with columns taken out."""
+    M, K = W.shape
+    if W.stride(1) == 1 and W.stride(0) % 8 == 0 and W.stride(0) >= K and W.data_ptr() % 16 == 0:
+        return W
+    wide = torch.zeros((M, (K + 7) // 8 * 8), dtype=W.dtype, device=W.device)
+    wide[:, :K] = W
+    return wide[:, :K]
+
+
 class Context:
     """Owns a strp_ctx bound to torch's current stream on `device`, plus the caller-side workspace."""
 
@@ -385,8 +396,8 @@ class Context:
         return self._empty((rows, (T + 7) // 8 * 8), dtype)
 
     def strp_linear(self, W, X, T, bias=None, act=ACT_NONE, residual=None, out=None):
-        """act(W X + bias) + residual: W [M x K], X [K x ld], bias [M] fp32, residual [M x ld] of out's dtype (out itself is
-        allowed).  Returns out, made in X's dtype where none is given."""
+        """act(W X + bias) + residual: W [M x K] with rows at multiples of eight entries (aligned_rows), X [K x ld], bias [M] fp32, residual
+        [M x ld] of out's dtype (out itself is allowed).  Returns out, made in X's dtype where none is given."""
         M, K = W.shape
         if out is None:
             out = self._new(M, T, X.dtype)

@@ -235,3 +235,25 @@ def test_workspaces_of_graphs_that_are_gone_are_freed():
         c.set_workspace(1 << 28)
         assert not c.kept
     torch.cuda.synchronize()
+
+
+# ---- linear ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("xt", [BF16, F32])
+def test_linear_of_the_weights_that_a_refit_leaves(ctx, xt):
+    """A head module's refit onto 45 of 51 channels, then the pruned projection twice: all columns, and the kept ones alone."""
+    T, d, out = 600, 51, 37
+    C, Y = torch.zeros((d, ld8(T)), dtype=xt, device="cuda"), torch.zeros((out, ld8(T)), device="cuda")
+    C[:, :T], Y[:, :T] = rand((d, T), 1, xt), rand((out, T), 2)
+    idx = torch.tensor([i for i in range(d) if i % 9 != 4], dtype=torch.int32, device="cuda")
+    ctx.ensure_workspace(1 << 24)
+    W = torch.zeros((out, d), device="cuda")
+    ctx.strp_refit(strp.SIDE_FC2, ctx.strp_gram(C, T, idx=idx), 1.0, C, Y, T, idx, W)
+    assert ctx.poll() == strp.OK
+    with pytest.raises(strp.StrpError):
+        ctx.strp_linear(W, C, T)
+    got = ctx.strp_linear(strp.aligned_rows(W), C, T, out=torch.empty((out, ld8(T)), device="cuda"))
+    kept = C[idx.long()].contiguous()
+    compact = ctx.strp_linear(strp.aligned_rows(W[:, idx.long()]), kept, T, out=torch.empty((out, ld8(T)), device="cuda"))
+    w, c = W.double(), C[:, :T].double()
+    tol = (d + 4) * U * (w.abs() @ c.abs()) + H(F32) * (w @ c).abs() + 1e-37
+    assert ((got[:, :T].double() - w @ c).abs() <= tol).all() and ((compact[:, :T].double() - w @ c).abs() <= tol).all()

@@ -247,7 +247,7 @@ def test_linear_of_the_weights_that_a_refit_leaves(ctx, xt):
     idx = torch.tensor([i for i in range(d) if i % 9 != 4], dtype=torch.int32, device="cuda")
     ctx.ensure_workspace(1 << 24)
     W = torch.zeros((out, d), device="cuda")
-    ctx.strp_refit(strp.SIDE_FC2, ctx.strp_gram(C, T, idx=idx), 1.0, C, Y, T, idx, W)
+    ctx.strp_refit(strp.SIDE_FC2, ctx.strp_gram(C, T, idx=idx), 1.0, Y, C, T, idx, W)
     assert ctx.poll() == strp.OK
     with pytest.raises(strp.StrpError):
         ctx.strp_linear(W, C, T)

@@ -257,3 +257,37 @@ def test_linear_of_the_weights_that_a_refit_leaves(ctx, xt):
     w, c = W.double(), C[:, :T].double()
     tol = (d + 4) * U * (w.abs() @ c.abs()) + H(F32) * (w @ c).abs() + 1e-37
     assert ((got[:, :T].double() - w @ c).abs() <= tol).all() and ((compact[:, :T].double() - w @ c).abs() <= tol).all()
+
+
+# ---- together -------------------------------------------------------------------------------------------------------
+def test_the_readme_s_example(ctx):
+    """The example of a decoder layer is run as it stands, on a decoder of one layer in fp32, and its perplexity is that of the model in 64 bits: norm before either block, a residual
+    round either, a norm before the head.  Every one of the ten results on the longest path is off by at most 400 steps, relative (sums of up to 512 terms, whose errors add up like their
+    square root), and passes the earlier ones on with a factor of order one."""
+    import os
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code, = [b.split("```")[0] for b in text.split("```python\n")[1:] if "strp_token_logprobs" in b]
+    d, f, V, heads, T = 128, 512, 999, 4, 203
+    w = {n: rand((r, c), i, F32, c ** -0.5) for i, (n, r, c) in enumerate([("q", d, d), ("k", d, d), ("v", d, d), ("Wo", d, d), ("W1", f, d), ("W2", d, f), ("E", V, d)])}
+    b = {n: 0.1 * rand(r, 20 + i) for i, (n, r) in enumerate([("q", d), ("k", d), ("v", d), ("bo", d), ("b1", f), ("b2", d)])}
+    norms = {n: (1.0 if n[0] == "g" else 0.0) + 0.5 * rand(d, 30 + i) for i, n in enumerate(("gain1", "bias1", "gain2", "bias2", "gain_f", "bias_f"))}
+    H0, starts = rand((d, ld8(T)), 50), [0, 60, T]
+    next_ids = torch.randint(0, V, (T,), device="cuda", dtype=torch.int32, generator=torch.Generator(device="cuda").manual_seed(2))
+    next_ids[59] = next_ids[T - 1] = -1
+    names = dict(ctx=ctx, strp=strp, torch=torch, H=H0, T=T, heads=heads, kv_heads=heads, starts=torch.tensor(starts, dtype=torch.int32, device="cuda"), next_ids=next_ids,
+                 qkv=[(w[n], b[n]) for n in "qkv"], **{n: w[n] for n in ("Wo", "W1", "W2", "E")}, **{n: b[n] for n in ("bo", "b1", "b2")}, **norms)
+    exec(code, names)
+
+    D = lambda t: t.double()
+    norm = lambda x, i: (x - x.mean(0)) / torch.sqrt(x.var(0, unbiased=False) + 1e-5) * D(norms["gain" + i])[:, None] + D(norms["bias" + i])[:, None]
+    x = D(H0)[:, :T]
+    n = norm(x, "1")
+    q, k, v = (D(w[m]) @ n + D(b[m])[:, None] for m in "qkv")
+    c = torch.cat([attention_exact(q[:, a:e], k[:, a:e], v[:, a:e], heads, list(range(heads)), [0, e - a], (d // heads) ** -0.5, 0.0)[0] for a, e in zip(starts, starts[1:])], 1)
+    x = x + D(w["Wo"]) @ c + D(b["bo"])[:, None]
+    x = x + D(w["W2"]) @ (D(w["W1"]) @ norm(x, "2") + D(b["b1"])[:, None]).clamp_min(0) + D(b["b2"])[:, None]
+    logp = torch.log_softmax(D(w["E"]) @ norm(x, "_f"), 0)
+    scored = next_ids >= 0
+    want = torch.where(scored, logp.gather(0, next_ids.clamp_min(0).long()[None])[0], 0.0)
+    assert float((names["out"]["logp"].double() - want).norm() / want.norm()) <= 10 * 400 * U
+    assert abs(float(names["perplexity"]) / math.exp(-float(want.sum()) / int(scored.sum())) - 1) <= 10 * 400 * U * float(want.abs().mean()) + 4 * U

@@ -7,7 +7,9 @@ import math
 import pytest
 import torch
 
+import layer_ops_sizes as sizes
 from paper_2510_03246_amd import strp
+from test_gpu_layer_ops import linear_case, logprobs_check, norm_check, padded
 
 pytestmark = pytest.mark.gpu
 
@@ -291,3 +293,63 @@ def test_the_readme_s_example(ctx):
     want = torch.where(scored, logp.gather(0, next_ids.clamp_min(0).long()[None])[0], 0.0)
     assert float((names["out"]["logp"].double() - want).norm() / want.norm()) <= 10 * 400 * U
     assert abs(float(names["perplexity"]) / math.exp(-float(want.sum()) / int(scored.sum())) - 1) <= 10 * 400 * U * float(want.abs().mean()) + 4 * U
+
+
+# ---- every kernel that there is ----------------------------------------------------------------------------------------
+FP32_TYPES = [(w, x, y) for w, x in ((F32, F32), (F32, BF16), (BF16, F32)) for y in (F32, BF16)]
+IDS = lambda v: "x".join(map(str, v)) if isinstance(v[0], int) else "-".join(str(t)[6:] for t in v)
+
+
+@pytest.mark.parametrize("types", [(BF16, BF16, BF16), (BF16, BF16, F32)], ids=IDS)
+@pytest.mark.parametrize("size", sizes.LINEAR_BF16, ids=IDS)
+def test_linear_in_every_tile_of_bf16(ctx, size, types):
+    linear_case(ctx, *size, types, strp.ACT_RELU, True, True)
+    linear_case(ctx, *size, types, strp.ACT_GELU, True, False)
+    linear_as_a_whole(ctx, *size, types)
+
+
+@pytest.mark.parametrize("types", FP32_TYPES, ids=IDS)
+@pytest.mark.parametrize("size", sizes.LINEAR_F32, ids=IDS)
+def test_linear_in_every_tile_of_fp32(ctx, size, types):
+    linear_case(ctx, *size, types, strp.ACT_RELU, True, True)
+    linear_as_a_whole(ctx, *size, types)
+
+
+def linear_as_a_whole(c, M, K, T, types):
+    """Relative to the result, in the 2-norm.  The K steps of a sum are off independently of each other, each by less than U of a partial sum that is no larger than the
+    whole in the mean: sqrt(K) U together, and a rounding of the output.  (An operand of fp32 that met the products rounded to bf16 would be off by 1.6e-3.)"""
+    wt, xt, yt = types
+    W, X = padded(M, K, 11, wt, 0.05, ld8(K))[:, :K], padded(K, T, 12, xt)
+    got = c.strp_linear(W, X, T, out=torch.empty((M, ld8(T)), dtype=yt, device="cuda"))[:, :T].double()
+    want = W.double() @ X[:, :T].double()
+    assert float((got - want).norm() / want.norm()) <= (math.sqrt(K) + 8) * U + H(yt), (M, K, T, types)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("wide", sorted(sizes.NORM_TOKENS["f32"]))
+def test_layer_norm_in_every_kernel(ctx, wide, dt):
+    name = "bf16" if dt == BF16 else "f32"
+    for d, T in sizes.NORM[name]:
+        if T != sizes.NORM_TOKENS[name][wide]:
+            continue
+        Y = torch.full((d, ld8(T)), 7.0, dtype=dt, device="cuda")
+        norm_check(ctx, padded(d, T, 5, dt), T, 1 + 0.1 * rand(d, 6), rand(d, 7), out=Y)
+        assert (Y[:, T:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("d,T", sizes.NORM_TALL)
+def test_layer_norm_of_more_channels_than_registers_hold(ctx, d, T, dt):
+    Y = torch.full((d, ld8(T)), 7.0, dtype=dt, device="cuda")
+    norm_check(ctx, padded(d, T, 5, dt), T, 1 + 0.1 * rand(d, 6), rand(d, 7), out=Y)
+    assert (Y[:, T:] == 7.0).all()
+    X = padded(d, T, 6, dt)
+    assert norm_check(ctx, X, T, None, None, out=X) is X
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("V,T,n_top", sizes.LOGPROBS)
+def test_token_logprobs_in_every_kernel(ctx, V, T, n_top, dt):
+    X = padded(V, T, V + T, dt, 3.0)
+    target = torch.randint(-2, V + 2, (T,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(torch.int32)
+    logprobs_check(ctx, X, T, target, n_top)

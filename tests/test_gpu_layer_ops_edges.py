@@ -353,3 +353,30 @@ def test_token_logprobs_in_every_kernel(ctx, V, T, n_top, dt):
     X = padded(V, T, V + T, dt, 3.0)
     target = torch.randint(-2, V + 2, (T,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(torch.int32)
     logprobs_check(ctx, X, T, target, n_top)
+
+
+# ---- offsets and maps that are wrong ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("starts", [[-100, 50, 300], [0, 5000, 300], [200, 100, 50], [7, 7, 7], [300, 0, 301], [-(2 ** 31), 2 ** 31 - 1, -5], [40, 260]], ids=str)
+def test_attention_reads_and_writes_its_own_rows_and_tokens_whatever_the_offsets_say(ctx, fast, starts, dt):
+    """Q, K, V and C lie inside larger buffers: NaN round K and V, 7 round C.  What is written is finite, so no key or value came from outside, and nothing is written outside."""
+    T, dh, heads, kv, edge = 300, 40, 4, 3, 16
+    big = {n: torch.full((rows * dh + 2 * edge, ld8(T) + 4 * edge), fill, dtype=dt, device="cuda") for n, rows, fill in
+           (("Q", heads, 0.0), ("K", kv, float("nan")), ("V", kv, float("nan")), ("C", heads, 7.0))}
+    inner = {n: b[edge:-edge, edge:-edge] for n, b in big.items()}
+    for i, n in enumerate("QKV"):
+        inner[n][:, :T] = rand((inner[n].shape[0], T), i, dt)
+        inner[n][:, T:] = float("nan")
+    kv_of = torch.tensor([-5, 900, 2 ** 31 - 1, -(2 ** 31)], dtype=torch.int32, device="cuda")
+    for c in (ctx, fast):
+        inner["C"][:] = 7.0
+        c.strp_attention(inner["Q"], inner["K"], inner["V"], T, heads, kv, torch.tensor(starts, dtype=torch.int32, device="cuda"), kv_of_head=kv_of, out=inner["C"])
+        inside = inner["C"][:, :T].clone()
+        assert torch.isfinite(inside).all()
+        inner["C"][:, :T] = 7.0
+        assert (big["C"] == 7.0).all()
+        if starts == [40, 260]:                    # right offsets: heads -5 and -2^31 have key-value head 0, the others the last
+            right = torch.full((heads * dh, ld8(T)), 7.0, dtype=dt, device="cuda")
+            c.strp_attention(inner["Q"], inner["K"], inner["V"], T, heads, kv, torch.tensor(starts, dtype=torch.int32, device="cuda"),
+                             kv_of_head=torch.tensor([0, kv - 1, kv - 1, 0], dtype=torch.int32, device="cuda"), out=right)
+            assert torch.equal(inside, right[:, :T]) and (inside[:, :40] == 7.0).all() and (inside[:, 260:] == 7.0).all() and not (inside[:, 40:260] == 7.0).any()

@@ -256,13 +256,15 @@ __device__ const unsigned zero_chunk[4] = {0u, 0u, 0u, 0u};
 // it a quarter of the keys at a time.  K runs a tile ahead of V: LDS has RING tiles of each.
 // SPLIT: the probabilities meet V as two terms of bf16, which is half as many matrix instructions again and three vector instructions a score.  With one term results are further from
 // those in 64 bits than their own rounding puts them (2.0e-3 against 1.66e-3, relative, on Gaussian V); with two they are not.  Whole calls, two terms / one: eight prompts of 2048 tokens, 32 heads
-// of 64: 302 / 221 us; 16221 tokens in prompts of 1 to 8191, 32 heads of 128 on 8: 1157 / 890 us.
+// of 64: 271 / 221 us; 16221 tokens in prompts of 1 to 8191, 32 heads of 128 on 8: 1101 / 890 us.
 template <int DHP, int NW, int RING, int WPS, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const AttnP p) {
   constexpr int KT = 64, NC = DHP / 32, NS = DHP / 16, TILE = DHP * 128, LH = DHP / 8 / NW, BQ = 32 * NW;      // LH: KBs of a tile of K or V that a wavefront moves
   static_assert(DHP % (8 * NW) == 0, "whole pieces for every wavefront");
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * RING * TILE];
   __shared__ int lows[NW];
+  constexpr bool QLDS = SPLIT && DHP <= 64;      // Q stays in LDS, for the registers of the second term
+  __shared__ bf16x8 sQ[QLDS ? NW : 1][QLDS ? NS : 1][QLDS ? 64 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
   // the tiles with most keys first; the heads that an XCD gets are neighbours where eight divides them, since neighbours share K and V
   const int slot = (int)blockIdx.x % p.heads, tile = p.tiles - 1 - (int)blockIdx.x / p.heads;
@@ -280,6 +282,9 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
         qf[s][e] = d < p.dh ? v : (__bf16)0.0f;
       }
   }
+  if constexpr (QLDS)
+#pragma unroll
+    for (int s = 0; s < NS; ++s) sQ[wave][s][lane] = qf[s];
   const int lo = first_key(p, q);
   // the wavefront's first key, and the first key from which on every query sees (none, if some query is in no sequence)
   int wlo = lo <= q ? lo : 0x7fffffff, whi = wlo;
@@ -363,9 +368,13 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   auto sees = [&](int s) { return wq + 31 >= first + s * KT && wlo < first + (s + 1) * KT; };      // some query, perhaps
   auto scores = [&](Scores& S, unsigned at, int d0, int d1) {
 #pragma unroll
-    for (int d = d0; d < d1; ++d)
+    for (int d = d0; d < d1; ++d) {
+      bf16x8 qd;
+      if constexpr (QLDS) qd = sQ[wave][d][lane];
+      else qd = qf[d];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) S.u[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_k(at, d, u), qf[d], S.u[u], 0, 0, 0);
+      for (int u = 0; u < 2; ++u) S.u[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_k(at, d, u), qd, S.u[u], 0, 0, 0);
+    }
   };
   // all of them; not every fragment at once, for the registers
   auto all_scores = [&](Scores& S, unsigned at) {
@@ -390,7 +399,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     if (__builtin_amdgcn_ballot_w64(grown)) {
       const float fac = grown ? __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e) : 1.0f;
       l[0] *= fac;
-      l[1] *= fac;
+      if constexpr (!SPLIT) l[1] *= fac;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -411,8 +420,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
       for (int f = 0; f < 2; ++f) x[f] = __builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + 2 * e + f], p.scale_log2e, -ref));
       if constexpr (SPLIT) {
         const unsigned b0 = __builtin_bit_cast(unsigned, x[0]), b1 = __builtin_bit_cast(unsigned, x[1]);
-        l[0] += x[0];
-        l[1] += x[1];
+        l[0] += x[0] + x[1];
         hi[e] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
         const bf16x2 left = {(__bf16)(x[0] - __builtin_bit_cast(float, b0 & 0xffff0000u)), (__bf16)(x[1] - __builtin_bit_cast(float, b1 & 0xffff0000u))};
         lo[e] = __builtin_bit_cast(unsigned, left);
@@ -519,11 +527,13 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) O[c][e] = 0.0f;
-    issue_k(0);
+    int s0 = 0;
+    asm volatile("" : "+s"(s0));                 // or the addresses of these are worked out ahead, and kept
+    issue_k(s0);
 #pragma unroll
     for (int s = 0; s < RING - 1; ++s) {
-      issue_k(s + 1);
-      issue_v(s);
+      issue_k(s0 + s + 1);
+      issue_v(s0 + s);
     }
     Scores a, b;
     clear(a);
@@ -573,11 +583,11 @@ static void launch_attention_bf16(strp_ctx* ctx, AttnP p) {
     p.tiles = (int)((p.T + bq - 1) / bq);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(p.tiles * p.heads)), dim3(threads), 0, ctx->stream, p);
   };
-  // three workgroups of three tiles of 64 channels on a CU, two of two of 96 or 128: what its 160 KB of LDS and its registers hold; with the probabilities in two terms, two also of 64
-  // (with three of them 9 to 18 registers lie in memory: 32 heads of 64 over 8 x 2048 450 us, not 340)
+  // three workgroups of 64 channels on a CU, two of 96 or 128: what its 160 KB of LDS and its registers hold.  (With the probabilities in two terms, 64 channels and Q in registers it
+  // would be two: 302 us, not 271, for 32 heads over 8 x 2048 tokens.)  Two tiles of K and of V in LDS or three: the same within 1 %.
   const auto by_width = [&](auto split) {
     constexpr bool SPLIT = decltype(split)::value;
-    if (p.dh <= 64) go(attention_bf16_kernel<64, 4, SPLIT ? 2 : 3, SPLIT ? 2 : 3, SPLIT>, 128, 256);
+    if (p.dh <= 64) go(attention_bf16_kernel<64, 4, SPLIT ? 2 : 3, 3, SPLIT>, 128, 256);
     else if (p.dh <= 96) go(attention_bf16_kernel<96, 4, 2, 2, SPLIT>, 128, 256);
     else go(attention_bf16_kernel<128, 4, 2, 2, SPLIT>, 128, 256);
   };

@@ -339,7 +339,7 @@ strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype dtype, int3
  * bf16: products of bf16 with fp32 sums.  The probabilities are fp32 and meet V as the context's precision says: as two bf16
  * terms (STRP_PREC_SPLIT, 2^-16 relative) or rounded once (STRP_PREC_FAST, 2^-8).  fp32: products of fp32.
  * Errors: STRP_EINVAL (null pointer, sizes not positive, ceil(T / 64) heads of 2^23 or more, d_head above 128, kv_heads that
- * does not divide heads without kv_of_head, scale not positive and finite, bad ld, misaligned, unknown dtype, more heads
+ * does not divide heads without kv_of_head, scale not positive or above 2e38, bad ld, misaligned, unknown dtype, more heads
  * than 65535).
  */
 typedef struct {

@@ -6,7 +6,6 @@
 // keys, so that a tile of queries that crosses from one sequence into the next needs nothing of its own.
 #include "layer_ops.h"
 
-#include <cmath>
 #include <type_traits>
 
 namespace strp {
@@ -616,7 +615,8 @@ extern "C" strp_status strp_attention(strp_ctx* ctx, const strp_attention_in* in
   if (in->heads > 65535) return fail(ctx, STRP_EINVAL, "attention: more than 65535 heads");
   if (!in->kv_of_head && in->heads % in->kv_heads) return fail(ctx, STRP_EINVAL, "attention: kv_heads does not divide heads and kv_of_head is null");
   if (in->n_seq < 0 || (in->seq_start ? in->n_seq < 1 : in->n_seq != 0)) return fail(ctx, STRP_EINVAL, "attention: seq_start needs n_seq > 0, no seq_start n_seq = 0");
-  if (!(in->scale > 0.0f) || std::isinf(in->scale)) return fail(ctx, STRP_EINVAL, "attention: scale must be positive and finite");
+  // the kernels multiply by scale log2(e)
+  if (!(in->scale > 0.0f) || !(in->scale <= 2.0e38f)) return fail(ctx, STRP_EINVAL, "attention: scale must be positive and at most 2e38");
   if (!token_ld(in->ldq, in->T) || !token_ld(in->ldk, in->T) || !token_ld(in->ldv, in->T) || !token_ld(in->ldc, in->T))
     return fail(ctx, STRP_EINVAL, "attention: leading dimensions must be multiples of 8 and not below T");
   if (!ptr16(in->Q) || !ptr16(in->K) || !ptr16(in->V) || !ptr16(in->C)) return fail(ctx, STRP_EINVAL, "attention: Q, K, V or C not 16-byte aligned");

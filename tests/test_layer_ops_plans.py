@@ -97,7 +97,17 @@ def check_attention():
             assert seen[prec, strp.F32, a] == seen[prec, strp.F32, b] == seen[1 - prec, strp.F32, a]
 
 
-CHECKS = [check_linear, check_norm, check_logprobs, check_attention]
+def check_attention_scales():
+    """in powers of two a scale has to be finite too"""
+    lib = _library()
+    strp = lib.strp
+    for scale, want in ((1e-30, strp.OK), (2e38, strp.OK), (2.4e38, strp.EINVAL), (3.4e38, strp.EINVAL), (float("inf"), strp.EINVAL), (float("nan"), strp.EINVAL), (0.0, strp.EINVAL)):
+        a = strp.AttentionIn(Q=A[0], K=A[1], V=A[2], C=A[3], dtype=strp.BF16, heads=4, kv_heads=2, d_head=64, scale=scale, T=300, ldq=304, ldk=304, ldv=304, ldc=304)
+        st, launches = lib.launches(lambda: lib.lib.strp_attention(lib.h, C.byref(a)))
+        assert st == want and len(launches) == (want == strp.OK), scale
+
+
+CHECKS = [check_linear, check_norm, check_logprobs, check_attention, check_attention_scales]
 
 
 @pytest.fixture(scope="session")

@@ -316,7 +316,7 @@ size_t strp_linear_workspace_bytes(int32_t M, int32_t K, int64_t T, strp_dtype w
 
 /*
  * strp_layer_norm -- Y[:, t] = (X[:, t] - mean_t) / sqrt(var_t + eps) * gain + bias over the d channels of every token
- * (population variance, the deviations taken from the mean).
+ * (population variance, the deviations taken from the mean; the sum of their squares has to fit fp32).
  *   X [d x ldx], Y [d x ldy] of dtype;  gain, bias [d] fp32, either may be NULL (1 and 0).  Y may be X (same ld).
  * Errors: STRP_EINVAL (null X or Y, d or T not positive, d above 2^30, T above 2^27, eps negative or not a number, bad ld,
  * misaligned, unknown dtype).
@@ -335,6 +335,7 @@ strp_status strp_layer_norm(strp_ctx* ctx, const void* X, strp_dtype dtype, int3
  *   NULL: g(h) = h / (heads / kv_heads), kv_heads divides heads.
  * Sequences may be empty or of one token.  Tokens outside every sequence keep what C holds.  What a token does not see
  * (other sequences, later tokens, padding) has no part in its result, whatever it holds, infinities and NaN included.
+ * The division by the sum of the probabilities comes last: 2^8 times the sum of |v| over the keys seen has to fit fp32.
  * Entries of seq_start or kv_of_head outside their ranges give wrong results, no access out of bounds.
  * bf16: products of bf16 with fp32 sums.  The probabilities are fp32 and meet V as the context's precision says: as two bf16
  * terms (STRP_PREC_SPLIT, 2^-16 relative) or rounded once (STRP_PREC_FAST, 2^-8).  fp32: products of fp32.

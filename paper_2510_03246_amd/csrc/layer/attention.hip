@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256, 2) void attention_f32_kernel(const AttnP p) {
   static_assert(2 * 32 * 33 <= 64 * PITCH, "the other half's results lie where K was");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
   const int part = wave >> 1, group = wave & 1;                            // half of the keys, of the queries
-  const int slot = (int)blockIdx.x % p.heads, tile = p.tiles - 1 - (int)blockIdx.x / p.heads;       // the tiles with most keys first
+  const int slot = (int)blockIdx.x % p.heads, tile = p.tiles - 1 - (int)blockIdx.x / p.heads;       // from the last tile on: of one sequence those with most keys first
   const int head = p.heads % 8 == 0 ? (slot & 7) * (p.heads >> 3) + (slot >> 3) : slot;
   const int q0 = tile * 64, q = q0 + group * 32 + l32, kv = kv_head_of(p, head);
   float qf[DHP / 2];
@@ -251,7 +251,7 @@ __device__ const unsigned zero_chunk[4] = {0u, 0u, 0u, 0u};
 // 16 contiguous bytes.  The chunks of 16 bytes in a row of K or V lie in LDS in an order that depends on the row, so that what is read at once lies in
 // different banks.
 // What bounds it is the vector unit (an exponential, a multiply-add, an addition, half a maximum and half a conversion for a score) and, at 128 channels a head, as
-// much the matrix cores.  So that either has work while the other waits, the scores of the next tile are multiplied beside the softmax of this one, and V P follows
+// much the matrix cores (busy with SPLIT 66 and 36 % of the time at 64 channels, 49 and 50 % at 128; without 57 and 29, 41 and 40).  So that either has work while the other waits, the scores of the next tile are multiplied beside the softmax of this one, and V P follows
 // it a quarter of the keys at a time.  K runs a tile ahead of V: LDS has RING tiles of each.
 // SPLIT: the probabilities meet V as two terms of bf16, which is half as many matrix instructions again and three vector instructions a score.  With one term results are further from
 // those in 64 bits than their own rounding puts them (2.0e-3 against 1.66e-3, relative, on Gaussian V); with two they are not.  Whole calls, two terms / one: eight prompts of 2048 tokens, 32 heads
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attention_bf16_kernel(const Attn
   constexpr bool QLDS = SPLIT && DHP <= 64;      // Q stays in LDS, for the registers of the second term
   __shared__ bf16x8 sQ[QLDS ? NW : 1][QLDS ? NS : 1][QLDS ? 64 : 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
-  // the tiles with most keys first; the heads that an XCD gets are neighbours where eight divides them, since neighbours share K and V
+  // from the last tile on (of one sequence those with most keys first); the heads that an XCD gets are neighbours where eight divides them, since neighbours share K and V
   const int slot = (int)blockIdx.x % p.heads, tile = p.tiles - 1 - (int)blockIdx.x / p.heads;
   const int head = p.heads % 8 == 0 ? (slot & 7) * (p.heads >> 3) + (slot >> 3) : slot;
   const int q0 = tile * BQ, q = q0 + wave * 32 + l32;

@@ -127,8 +127,9 @@ __device__ __forceinline__ void finish_tile(const LinearP& p, const floatx4 (&ac
 
 // Tiles of (WM 16 NI) channels x (64 WN) tokens, a wavefront 16 NI x 64, in steps of 32 of the contraction.  W comes in pairs of steps, 128 bytes of a row: the
 // line that memory hands out whole.  LDS holds three pairs of W and four steps of X, and all but what is being multiplied is on its way.  A remainder of the
-// contraction is the first pair and goes through registers, zeros from K on.  The matrix cores bound it, in the largest products by power: 8192 x 2048 over 2048 tokens
-// 62.5 us, 1.1 PFLOP/s; 4096 x 4915 over 32768 1.19 to 1.27 ms, 1.04 to 1.11; 768 x 768 over 2048 11.8 us.
+// contraction is the first pair and goes through registers, zeros from K on.  What bounds it is a step's matrix instructions and reads of LDS, which overlap in part (64 steps of
+// a tile of 256 1.8 us, the matrix instructions alone 0.85; the matrix cores are busy 42 % of the time), in the largest products also power: 8192 x 2048 over 2048 tokens
+// 62 us, 1.1 PFLOP/s; 4096 x 4915 over 32768 1.19 to 1.27 ms, 1.04 to 1.11; 768 x 768 over 2048 11.8 us.
 template <int WM, int WN, int NI, typename YT>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_tile_kernel(const LinearP p) {
   constexpr int NW = WM * WN, BM = WM * 16 * NI, BN = WN * 64, PAIR = BM * 128, STEP = BN * 64, XAT = 3 * PAIR, RPI = 512 / BN;     // RPI: rows of X in a KB
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(64 * WM * WN, WM * WN >= 8 ? 1 : 2) void linear_til
 
 // Few tokens (T <= 16 NT): W is the traffic, read once straight into fragments (a lane has 16 bytes of a row), the contraction in parts among the NW wavefronts
 // of a workgroup, which add their sums up in LDS.  X goes to LDS as it lies, a run of rows at a time, and is read turned.  A workgroup has 16 channels.
-// What bounds it is the rate of its reads, each of 16 rows: 3.0 TB/s of W with a workgroup to a CU and 3.4 from two on (4096 x 4096 one token 13.9 us, 8192 x 2048 12.2); below
+// What bounds it is the rate of its reads, each of 16 rows: 2.6 TB/s of W with a workgroup to a CU and 3.0 from two on (4096 x 4096 one token 13.2 us, 8192 x 2048 11.4; with W in the last-level cache 11.9, 10.2); below
 // that a launch and the latencies of X, W and the sums (768 x 768 4.1 us).  Asking for X two runs ahead, beginning at different places of the contraction, both
 // steps of a line to one wavefront and 32 channels a workgroup changed it by less than 10 % either way.
 constexpr int FEW_WAVES = 8;

@@ -314,7 +314,7 @@ static void launch_logprobs(strp_ctx* ctx, const LogitP& a, const TokenP& b) {
   const long long cols = a.ct * (16 / (long long)sizeof(E));
   hipLaunchKernelGGL((logit_streams_kernel<E>), dim3((unsigned)((a.T + cols - 1) / cols), a.slices), dim3(256), 0, ctx->stream, a);
   // Eight wavefronts for a token, one where the tokens alone are wavefronts enough.  Both kernels, us, 50000 entries of bf16, one against eight: one token 57, 24; 512 86, 41; 2048 89, 85;
-  // 4096 150, 162; 8192 287, 310.  (Four: 2048 86.5; sixteen: one token 23, 512 51.)
+  // 4096 150, 162; 8192 287, 310.  (Four: 2048 86.5; sixteen: one token 23, 512 51.)  Measured at these sizes alone: 130000 entries over 2048 tokens in eight 175, over 2100 in one 219.
   const auto go = [&](auto kernel, int tokens) { hipLaunchKernelGGL(kernel, dim3((unsigned)((b.T + tokens - 1) / tokens)), dim3(1024), 0, ctx->stream, b); };
   if (b.T <= 2048) go(token_finish_kernel<E, 8>, 2);
   else go(token_finish_kernel<E, 1>, 16);

@@ -193,7 +193,8 @@ def aligned_rows(W: torch.Tensor) -> torch.Tensor:
 
 
 class Context:
-    """Owns a strp_ctx bound to torch's current stream on `device`, plus the caller-side workspace."""
+    """Owns a strp_ctx bound to torch's current stream on `device`, plus the caller-side workspace.  Its calls are enqueued on that stream also where another
+    one is current: then the caller orders the two, and keeps what the calls read until they have."""
 
     def __init__(self, device=0, workspace_bytes: int | None = None):
         self.lib = load_library()

@@ -1,0 +1,468 @@
+"""Timing cases of the operators with which a model generates: the paged cache of keys and values, the attention that reads it, and the
+verification of drafted tokens.
+
+  append     keys and values of new tokens, turned by their positions, into the pages of a cache (bf16, fp32 or 4 bits); queries turned beside them
+  attention  new tokens of many sequences, one or thousands each, over the pages of their sequences
+  verify     drafted tokens against the target's probabilities from given random numbers, and the token that follows them
+
+Activations are channel-major like every activation of the framework (rows are channels, tokens contiguous).  With `own` false the operators are computed in
+their plain form, elementary torch operations in 32 bits (64 for angles and for what decides about tokens); with `own` true through the entry points of the binding.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+_context = None
+
+
+def _ctx():
+    """The one library context that a program keeps for its device."""
+    global _context
+    if _context is None:
+        from paper_2510_03246_amd import strp
+        _context = strp.Context(0)
+    return _context
+
+
+def listed():
+    return [
+        # The next token of one prompt of the smallest model: launches and latency.
+        dict(name="append_one_token", op="append", heads=12, kv=12, dh=64, rot=64, pairs=False, page=16, dtype="bf16", cache="bf16", seqs="1:511"),
+        # Eight calibration segments of 2048 tokens of the 2048-wide model, queries and keys turned.
+        dict(name="append_8x2048", op="append", heads=32, kv=32, dh=64, rot=64, pairs=False, page=64, dtype="bf16", cache="bf16", seqs=" ".join(["2048:0"] * 8)),
+        # A serving step: chunks of prompts beside single tokens, grouped heads, far positions, 4 bits.
+        dict(name="append_ragged_q4", op="append", heads=32, kv=8, dh=128, rot=128, pairs=True, page=32, dtype="bf16", cache="q4",
+             seqs="1000:0 1:70001 1:4095 513:2048 1:1 1:31 7:100 2000:12345"),
+        # The next token of one prompt of the smallest model.
+        dict(name="attention_one_token", op="attention", heads=12, kv=12, dh=64, page=16, dtype="bf16", cache="bf16", seqs="1:511"),
+        # A serving step: the next tokens of 64 sequences of very different lengths, grouped heads.
+        dict(name="attention_decode_64", op="attention", heads=32, kv=8, dh=128, page=64, dtype="bf16", cache="bf16",
+             seqs=" ".join("1:%d" % ((i * i * 977 + 31 * i) % 4001) for i in range(64))),
+        # Eight long conversations whose cache is held in 4 bits.
+        dict(name="attention_decode_long_q4", op="attention", heads=32, kv=8, dh=128, page=32, dtype="bf16", cache="q4",
+             seqs="1:32768 1:30001 1:40000 1:25000 1:32767 1:35000 1:39999 1:28001"),
+        # Four drafted tokens and the one before them, sixteen sequences, every head with keys of its own (the 4096-wide model).
+        dict(name="attention_drafts", op="attention", heads=32, kv=32, dh=128, page=16, dtype="bf16", cache="bf16", seqs=" ".join("5:%d" % (2000 + 7 * i) for i in range(16))),
+        # Chunks of two long prompts beside the next tokens of six others.
+        dict(name="attention_chunks", op="attention", heads=32, kv=8, dh=128, page=64, dtype="bf16", cache="bf16",
+             seqs="1024:6000 1:3000 1:17 1024:2048 1:1 1:4096 1:777 1:2500"),
+        # fp32, a head width that is no power of two (the 2560-wide model), a prompt's last tokens among them.
+        dict(name="attention_f32", op="attention", heads=32, kv=32, dh=80, page=16, dtype="f32", cache="f32", seqs="1:1999 1:0 3:500 40:1000 1:1500 1:64"),
+        # Four drafted tokens of one prompt.
+        dict(name="verify_one_prompt", op="verify", V=50000, drafts="4", tau=1.0, dtype="f32", masked=0),
+        # A serving step of 64 sequences, some without drafts, the vocabulary's padding rows masked.
+        dict(name="verify_64", op="verify", V=50000, drafts=" ".join(str((i * 5) % 8) for i in range(64)), tau=0.8, dtype="bf16", masked=16),
+        # The largest batch.
+        dict(name="verify_256", op="verify", V=50000, drafts=" ".join(["4"] * 256), tau=1.0, dtype="bf16", masked=0),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["append", "attention", "attention", "verify"])
+    if op == "verify":
+        V = _log(rng, 300, 130000)
+        cap = min(2304.0, 1.1e8 / V)
+        drafts, cols = [], 0.0
+        for _ in range(_log(rng, 1, 256)):
+            n = rng.choice([0, 1, 3, 4, 4, 5, 7, rng.randint(0, 12)])
+            if cols + 2 * n + 1 > cap:
+                break
+            drafts.append(n)
+            cols += 2 * n + 1
+        return dict(op="verify", V=V, drafts=" ".join(map(str, drafts or [2])), tau=rng.choice([1.0, 1.0, 0.7, 1.3]), dtype=rng.choice(["bf16", "f32"]),
+                    masked=rng.choice([0, 0, 16]))
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    cache = rng.choice([dtype, dtype, "q4"])
+    dh = rng.choice([32, 64, 64, 80, 96, 128, 128, 8 * rng.randint(1, 16)])
+    kv = rng.randint(1, 16)
+    heads = kv * rng.choice([1, 1, 2, 4, 7])
+    case = dict(op=op, heads=heads, kv=kv, dh=dh, page=rng.choice([16, 16, 32, 64, 128]), dtype=dtype, cache=cache)
+    if op == "append":
+        case.update(rot=rng.choice([0, dh, dh, dh // 4 * 2]), pairs=rng.random() < 0.5)
+        room, seqs = int(6.0e7 / (dh * (2 * heads + 4 * kv))), []
+        for _ in range(_log(rng, 1, 48)):
+            n = min(room, _log(rng, 1, 3000))
+            if n < 1:
+                break
+            seqs.append("%d:%d" % (n, _log(rng, 1, 30000) - 1))
+            room -= n
+        return dict(case, seqs=" ".join(seqs or ["3:5"]))
+    # no more products and no larger a cache than the largest listed cases
+    flops, nbytes, seqs = 1.5e11 / (8.0 if dtype == "f32" else 1.0), 3.0e8, []
+    for _ in range(_log(rng, 1, 64)):
+        n, past = rng.choice([1, 1, 1, 1, rng.randint(2, 9), _log(rng, 10, 1500)]), _log(rng, 1, 40000) - 1
+        flops -= 4.0 * heads * dh * n * (past + n)
+        nbytes -= 8.0 * kv * dh * (past + n)
+        if flops < 0 or nbytes < 0:
+            break
+        seqs.append("%d:%d" % (n, past))
+    return dict(case, seqs=" ".join(seqs or ["2:33"]))
+
+
+def _seqs(case):
+    """[(new tokens, tokens that the cache holds before them)]"""
+    return [tuple(int(x) for x in s.split(":")) for s in case["seqs"].split()]
+
+
+def _drafts(case):
+    return [int(n) for n in case["drafts"].split()]
+
+
+def _ld(T):
+    return (T + 7) // 8 * 8
+
+
+def _starts(counts):
+    starts = [0]
+    for n in counts:
+        starts.append(starts[-1] + n)
+    return starts
+
+
+def _activations(rows, T, g, dtype, scale=1.0, heavy=True):
+    """[rows x ld] with tokens contiguous: Gaussian, one channel in a hundred heavy-tailed."""
+    x = torch.randn((rows, _ld(T)), generator=g, device="cuda") * scale
+    if heavy:
+        n = max(1, rows // 100)
+        chi = sum(torch.randn((n, _ld(T)), generator=g, device="cuda") ** 2 for _ in range(3)) / 3.0
+        x[:n] /= torch.sqrt(chi)
+    return x.to(DTYPES[dtype])
+
+
+def _quantise(x):
+    """x [..., dh] in 32 bits: whole numbers 0 .. 15 and, last, (lowest, step)."""
+    lo = x.amin(-1, keepdim=True)
+    step = (x.amax(-1, keepdim=True) - lo) / 15.0
+    n = torch.where(step > 0, torch.round((x - lo) / step), 0.0).clamp(0.0, 15.0)
+    return n, torch.cat([lo, step], -1)
+
+
+def _packed(n):
+    b = n.to(torch.uint8)
+    return b[..., 0::2] | (b[..., 1::2] << 4)
+
+
+def _values(packed, scales):
+    """What 4 bits stand for, in 32 bits."""
+    n = torch.stack([packed & 15, packed >> 4], -1).flatten(-2).float()
+    return scales[..., :1] + n * scales[..., 1:]
+
+
+def _pool(pages, case, g):
+    """Pages as other sequences and earlier tokens have left them: [pages, kv, page, dh], and (lowest, step) where 4 bits hold it."""
+    x = torch.randn((pages, case["kv"], case["page"], case["dh"]), generator=g, device="cuda")
+    if case["cache"] == "q4":
+        n, scales = _quantise(x)
+        return _packed(n), scales
+    return x.to(DTYPES[case["cache"]]), None
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    st = dict(case=case)
+    if case["op"] == "verify":
+        V, drafts, dt = case["V"], _drafts(case), DTYPES[case["dtype"]]
+        n, Td = len(drafts), sum(drafts)
+        x = torch.randn((V, _ld(Td + n)), generator=g, device="cuda") * 2.5
+        likely = torch.randint(0, V - case["masked"], (x.shape[1],), generator=g, device="cuda")
+        x[likely, torch.arange(x.shape[1], device="cuda")] += 8.0
+        # the draft's logits are the target's at the same position, and some of its own
+        at = torch.tensor([s + i + sum(drafts[:s]) for s in range(n) for i in range(drafts[s])], dtype=torch.int64, device="cuda")
+        y = torch.zeros((V, _ld(max(Td, 1))), device="cuda")
+        if Td:
+            y[:, :Td] = x[:, at] + torch.randn((V, Td), generator=g, device="cuda") * 0.7
+        if case["masked"]:
+            x[V - case["masked"]:] = -math.inf
+            y[V - case["masked"]:] = -math.inf
+        x, y = x.to(dt), y.to(dt)
+        ids = torch.zeros(0, dtype=torch.int32, device="cuda")
+        if Td:
+            # drafted as a draft is: from its own probabilities
+            u = torch.rand((V, Td), generator=g, device="cuda").clamp_min(1e-30)
+            ids = (y[:, :Td].float() / case["tau"] - torch.log(-torch.log(u))).argmax(0).to(torch.int32)
+        st.update(target=x, draft=y, ids=ids, n_seq=n, Td=Td, u=torch.rand(Td, generator=g, device="cuda"), u_next=torch.rand(n, generator=g, device="cuda"),
+                  starts=torch.tensor(_starts(drafts), dtype=torch.int32, device="cuda"))
+        return st
+    seqs, kv, dh, page = _seqs(case), case["kv"], case["dh"], case["page"]
+    T = sum(n for n, _ in seqs)
+    need = [(n + past + page - 1) // page for n, past in seqs]
+    # every page that a sequence holds for attention; for appending those that the new tokens go to, the others lie in the same memory
+    pages = sum(need) + 3 if case["op"] == "attention" else sum(w - past // page for w, (n, past) in zip(need, seqs)) + 3
+    order = torch.randperm(pages, generator=g, device="cuda").to(torch.int32).tolist()
+    table = [[0] * max(need) for _ in seqs]
+    for row, w, (n, past) in zip(table, need, seqs):
+        first = 0 if case["op"] == "attention" else past // page
+        row[first:w] = order[:w - first]
+        order = order[w - first:]
+    st.update(T=T, table=torch.tensor(table, dtype=torch.int32, device="cuda"), past=torch.tensor([p for _, p in seqs], dtype=torch.int32, device="cuda"),
+              starts=torch.tensor(_starts([n for n, _ in seqs]), dtype=torch.int32, device="cuda"),
+              Q=_activations(case["heads"] * dh, T, g, case["dtype"], 1.5, heavy=False), out=torch.empty((case["heads"] * dh, _ld(T)), dtype=DTYPES[case["dtype"]], device="cuda"))
+    for name in ("K", "V"):
+        st["c" + name], st["s" + name] = _pool(pages, case, g)
+    if case["op"] == "append":
+        st.update(K=_activations(kv * dh, T, g, case["dtype"]), V=_activations(kv * dh, T, g, case["dtype"]))
+        if case["rot"]:
+            st["inv_freq"] = 10000.0 ** (-torch.arange(0, case["rot"], 2, device="cuda", dtype=torch.float32) / case["rot"])
+    return st
+
+
+# ---- through the framework -------------------------------------------------------------------------------------------
+def _cache(st):
+    """The handle that a program keeps beside its pages."""
+    if "handle" not in st:
+        from paper_2510_03246_amd import strp
+        st["handle"] = strp.PagedCache(st["cK"], st["cV"], st["sK"], st["sV"])
+    return st["handle"]
+
+
+def _own(st):
+    ctx, case = _ctx(), st["case"]
+    if case["op"] == "append":
+        ctx.strp_cache_append(st["K"], st["V"], st["T"], _cache(st), st["table"], st["past"], seq_start=st["starts"], inv_freq=st.get("inv_freq"), pairs=case["pairs"],
+                              Q=st["Q"], q_out=st["out"])
+        return _appended(st, st["out"][:, :st["T"]])
+    if case["op"] == "attention":
+        return ctx.strp_cache_attention(st["Q"], st["T"], case["heads"], _cache(st), st["table"], st["past"], seq_start=st["starts"], out=st["out"])[:, :st["T"]]
+    return ctx.strp_verify_draft(st["target"], st["draft"], st["ids"], st["u"], st["u_next"], seq_start=st["starts"], temperature=case["tau"])
+
+
+# ---- plain form ------------------------------------------------------------------------------------------------------
+def _appended(st, q):
+    """Turned queries and the whole cache, 4 bits as what they stand for."""
+    if st["case"]["cache"] == "q4":
+        return dict(Q=q, K=_values(st["cK"], st["sK"]), V=_values(st["cV"], st["sV"]))
+    return dict(Q=q, K=st["cK"], V=st["cV"])
+
+
+def _of_tokens(st):
+    """Sequence and position of every new token."""
+    t = torch.arange(st["T"], device="cuda")
+    s = torch.searchsorted(st["starts"][1:].contiguous(), t.to(torch.int32), right=True)
+    return s, st["past"][s] + t - st["starts"][s]
+
+
+def _turned(x, case, cos, sin):
+    """x [heads*dh x T] in 32 bits with its first `rot` channels of each head turned, in 64."""
+    rot, dh = case["rot"], case["dh"]
+    if not rot:
+        return x
+    x = x.reshape(-1, dh, x.shape[1])
+    a, b = (x[:, 0:rot:2], x[:, 1:rot:2]) if case["pairs"] else (x[:, :rot // 2], x[:, rot // 2:rot])
+    a, b = a.double(), b.double()
+    ra, rb = (a * cos - b * sin).float(), (b * cos + a * sin).float()
+    y = x.clone()
+    if case["pairs"]:
+        y[:, 0:rot:2], y[:, 1:rot:2] = ra, rb
+    else:
+        y[:, :rot // 2], y[:, rot // 2:rot] = ra, rb
+    return y.reshape(-1, x.shape[2])
+
+
+def _plain_append(st):
+    case, T = st["case"], st["T"]
+    kv, dh, page = case["kv"], case["dh"], case["page"]
+    s, pos = _of_tokens(st)
+    cos = sin = None
+    if case["rot"]:
+        angle = pos.double()[None, :] * st["inv_freq"].double()[:, None]
+        cos, sin = torch.cos(angle), torch.sin(angle)
+    pages, rows = st["table"][s, pos // page].long(), (pos % page).long()
+    for name in ("K", "V"):
+        x = st[name][:, :T].float()
+        x = (_turned(x, case, cos, sin) if name == "K" else x).reshape(kv, dh, T).permute(2, 0, 1)
+        if case["cache"] == "q4":
+            n, scales = _quantise(x)
+            st["c" + name][pages, :, rows] = _packed(n)
+            st["s" + name][pages, :, rows] = scales
+        else:
+            st["c" + name][pages, :, rows] = x.to(DTYPES[case["cache"]])
+    return _appended(st, _turned(st["Q"][:, :T].float(), case, cos, sin).to(DTYPES[case["dtype"]]))
+
+
+def _plain_attention(st):
+    case = st["case"]
+    kv, dh, page, G = case["kv"], case["dh"], case["page"], case["heads"] // case["kv"]
+    out = torch.empty((case["heads"] * dh, st["T"]), dtype=DTYPES[case["dtype"]], device="cuda")
+    a = 0
+    for i, (n, past) in enumerate(_seqs(case)):
+        keys = past + n
+        pages = st["table"][i, :(keys + page - 1) // page].long()
+        k, v = ((_values(st["c" + x][pages], st["s" + x][pages]) if case["cache"] == "q4" else st["c" + x][pages].float()).transpose(0, 1).reshape(kv, -1, dh)[:, :keys].contiguous()
+                for x in ("K", "V"))
+        q = st["Q"][:, a:a + n].float().reshape(kv, G, dh, n).permute(0, 1, 3, 2)
+        step = max(1, min(n, (1 << 28) // (case["heads"] * keys)))          # queries at a time, so that their scores take a GB at most
+        for j in range(0, n, step):
+            e = min(n, j + step)
+            p = torch.matmul(q[:, :, j:e].reshape(kv, G * (e - j), dh), k.transpose(1, 2).contiguous()).reshape(kv, G, e - j, keys) / math.sqrt(dh)
+            if n > 1:
+                p.masked_fill_(torch.arange(keys, device="cuda")[None, :] > torch.arange(past + j, past + e, device="cuda")[:, None], -math.inf)
+            p = torch.exp(p - p.amax(-1, keepdim=True))
+            p /= p.sum(-1, keepdim=True)
+            c = torch.matmul(p.reshape(kv, G * (e - j), keys), v).reshape(kv, G, e - j, dh)
+            out[:, a + j:a + e] = c.permute(0, 1, 3, 2).reshape(-1, e - j).to(out.dtype)
+        a += n
+    return out
+
+
+def _softmax64(x, tau):
+    x = x.double() * (1.0 / tau)
+    e = torch.exp(x - x.amax(0))
+    return e / e.sum(0)
+
+
+def _plain_verify(st):
+    case, n, Td = st["case"], st["n_seq"], st["Td"]
+    counts = (st["starts"][1:] - st["starts"][:-1]).long()
+    seq = torch.arange(n, device="cuda")
+    first = st["starts"][:-1].long() + seq                                  # the target's column of each sequence's first position
+    p = _softmax64(st["target"][:, :Td + n], case["tau"])
+    accepted = torch.zeros_like(counts)
+    if Td:
+        q = _softmax64(st["draft"][:, :Td], case["tau"])
+        of = torch.searchsorted(st["starts"][1:].contiguous(), torch.arange(Td, device="cuda", dtype=torch.int32), right=True)
+        t = torch.arange(Td, device="cuda")
+        ok = st["u"].double() * q[st["ids"].long(), t] < p[st["ids"].long(), t + of]
+        # the first token of each sequence that is refused
+        at = torch.where(ok, Td, t)
+        bad = torch.full((n,), Td, device="cuda").scatter_reduce(0, of, at, "amin")
+        accepted = torch.minimum(bad - st["starts"][:-1].long(), counts)
+    r = p[:, first + accepted]
+    if Td:
+        rest = torch.clamp_min(r - q[:, (st["starts"][:-1].long() + accepted).clamp_max(Td - 1)], 0.0)
+        use = (accepted < counts) & (rest.sum(0) > 0)
+        r = torch.where(use[None, :], rest, r)
+    c = torch.cumsum(r, 0)
+    over = c > st["u_next"].double() * c[-1]
+    v = torch.arange(case["V"], device="cuda")[:, None]
+    return dict(accepted=accepted.to(torch.int32), next_ids=torch.where(over, v, case["V"]).amin(0).to(torch.int32))
+
+
+def run(st):
+    if own:
+        return _own(st)
+    return {"append": _plain_append, "attention": _plain_attention, "verify": _plain_verify}[st["case"]["op"]](st)
+
+
+def _row_bytes(case):
+    return {"bf16": 2.0 * case["dh"], "f32": 4.0 * case["dh"], "q4": 0.5 * case["dh"] + 8.0}[case["cache"]]
+
+
+def work(case):
+    b = {"bf16": 2.0, "f32": 4.0}[case["dtype"]]
+    if case["op"] == "verify":
+        drafts = _drafts(case)
+        cells = float(case["V"]) * (2 * sum(drafts) + len(drafts))
+        return {"bytes": b * cells + 8.0 * sum(drafts) + 12.0 * len(drafts), "flops": 3.0 * cells}
+    seqs = _seqs(case)
+    T = sum(n for n, _ in seqs)
+    if case["op"] == "append":
+        return {"bytes": T * (2.0 * b * case["heads"] * case["dh"] + 2.0 * case["kv"] * (b * case["dh"] + _row_bytes(case))),
+                "flops": 3.0 * T * case["rot"] * (case["heads"] + case["kv"])}
+    seen = sum(n * past + n * (n + 1) / 2.0 for n, past in seqs)
+    return {"bytes": 2.0 * b * T * case["heads"] * case["dh"] + 2.0 * case["kv"] * _row_bytes(case) * sum(n + past for n, past in seqs),
+            "flops": 4.0 * case["heads"] * case["dh"] * seen}
+
+
+# ---- the same in 64 bits, from the definitions -----------------------------------------------------------------------
+def _exact_append(st):
+    case, dh, page, rot = st["case"], st["case"]["dh"], st["case"]["page"], st["case"]["rot"]
+    where = [(i, past + j) for i, (n, past) in enumerate(_seqs(case)) for j in range(n)]
+    pos = torch.tensor([p for _, p in where], dtype=torch.float64, device="cuda")
+    index = torch.arange(dh, device="cuda")
+    inside = index < rot
+    if case["pairs"]:
+        partner, which, sign = index ^ 1, index // 2, torch.where(index % 2 == 0, -1.0, 1.0).double()
+    else:
+        half = max(rot // 2, 1)
+        partner, which, sign = (index + half) % max(rot, 1), index % half, torch.where(index < half, -1.0, 1.0).double()
+
+    def turn(x):                       # [T, heads, dh]
+        if not rot:
+            return x
+        freq = st["inv_freq"].double()[torch.where(inside, which, 0)]
+        a = pos[:, None, None] * freq
+        y = x * torch.cos(a) + sign * x[..., torch.where(inside, partner, index)] * torch.sin(a)
+        return torch.where(inside, y, x)
+
+    def rows(x):
+        return x[:, :st["T"]].double().t().reshape(st["T"], -1, dh)
+
+    res = dict(Q=turn(rows(st["Q"])).reshape(st["T"], -1).t())
+    table = st["table"].tolist()
+    slot = torch.tensor([table[i][p // page] * page + p % page for i, p in where], device="cuda")
+    for name in ("K", "V"):
+        x = turn(rows(st[name])) if name == "K" else rows(st[name])
+        if case["cache"] == "q4":
+            scales = st["s" + name].double()
+            low, high = (st["c" + name] % 16).double(), (st["c" + name] // 16).double()
+            pool = torch.stack((low, high), dim=-1).reshape(*low.shape[:-1], dh) * scales[..., 1:2] + scales[..., 0:1]
+            f = x.float()              # a cache of 4 bits is made from values, lowest and step of 32
+            lo = torch.min(f, dim=-1, keepdim=True).values
+            step = torch.div(torch.max(f, dim=-1, keepdim=True).values - lo, 15.0)
+            x = torch.where(step > 0, lo.double() + step.double() * torch.clamp(torch.round(torch.div(f - lo, step)), 0, 15).double(), lo.double())
+        else:
+            pool = st["c" + name].double()
+        flat = pool.transpose(1, 2).reshape(-1, case["kv"], dh)
+        flat[slot] = x
+        res[name] = flat.reshape(-1, page, case["kv"], dh).transpose(1, 2)
+    return res
+
+
+def _exact_attention(st):
+    case, dh, page, G = st["case"], st["case"]["dh"], st["case"]["page"], st["case"]["heads"] // st["case"]["kv"]
+    out = torch.empty((case["heads"] * dh, st["T"]), dtype=torch.float64, device="cuda")
+    starts, table = st["starts"].tolist(), st["table"].tolist()
+    for i, (n, past) in enumerate(_seqs(case)):
+        pages = table[i][:-(-(past + n) // page)]
+        a, e = starts[i], starts[i + 1]
+        mask = torch.ones((n, past + n), dtype=torch.bool, device="cuda").tril(past)
+        for g in range(case["kv"]):
+            kv = []
+            for name in ("K", "V"):
+                x = torch.cat([st["c" + name][pg, g] for pg in pages], 0) if len(pages) < 64 else st["c" + name][pages, g].flatten(0, 1)
+                if case["cache"] == "q4":
+                    sc = st["s" + name][pages, g].flatten(0, 1).double()
+                    x = torch.stack((x % 16, x // 16), dim=2).flatten(1).double() * sc[:, 1:] + sc[:, :1]
+                kv.append(x[:past + n].double())
+            for h in range(g * G, (g + 1) * G):
+                w = torch.mm(st["Q"][h * dh:(h + 1) * dh, a:e].double().t().contiguous(), kv[0].t().contiguous()) * dh ** -0.5
+                w = torch.exp(w - torch.where(mask, w, -math.inf).max(1, keepdim=True).values) * mask
+                out[h * dh:(h + 1) * dh, a:e] = torch.mm(w, kv[1]).div(w.sum(1, keepdim=True)).t()
+    return out
+
+
+def _exact_verify(st):
+    case, res = st["case"], ([], [])
+    starts, ids, u, last = st["starts"].tolist(), st["ids"].tolist(), st["u"].tolist(), st["u_next"].tolist()
+    for s in range(st["n_seq"]):
+        a, n = starts[s], starts[s + 1] - starts[s]
+        p = torch.softmax(st["target"][:, a + s:a + s + n + 1].double() / case["tau"], 0)
+        q = torch.softmax(st["draft"][:, a:a + n].double() / case["tau"], 0)
+        at = 0
+        drafted = torch.tensor(ids[a:a + n], dtype=torch.int64, device="cuda")
+        pairs = torch.stack((p[:, :n].gather(0, drafted[None])[0], q.gather(0, drafted[None])[0])).tolist()
+        while at < n and u[a + at] * pairs[1][at] < pairs[0][at]:
+            at += 1
+        w = p[:, at]
+        if at < n:
+            rest = torch.relu(w - q[:, at])
+            w = rest if float(rest.sum()) > 0.0 else w
+        c = w.cumsum(0)
+        res[0].append(at)
+        res[1].append(int((c <= last[s] * c[-1]).sum()))
+    return dict(accepted=torch.tensor(res[0], dtype=torch.int32, device="cuda"), next_ids=torch.tensor(res[1], dtype=torch.int32, device="cuda"))
+
+
+def exact(case, seed):
+    """The same in 64 bits, from the definitions."""
+    return {"append": _exact_append, "attention": _exact_attention, "verify": _exact_verify}[case["op"]](prepare(case, seed))

@@ -142,7 +142,7 @@ def _activations(rows, T, g, dtype, scale=1.0, heavy=True):
 def _quantise(x):
     """x [..., dh] in 32 bits: whole numbers 0 .. 15 and, last, (lowest, step)."""
     lo = x.amin(-1, keepdim=True)
-    step = (x.amax(-1, keepdim=True) - lo) / 15.0
+    step = (x.amax(-1, keepdim=True) - lo) / torch.full_like(lo, 15.0)      # by a number torch would multiply by its rounded inverse
     n = torch.where(step > 0, torch.round((x - lo) / step), 0.0).clamp(0.0, 15.0)
     return n, torch.cat([lo, step], -1)
 
@@ -408,7 +408,7 @@ def _exact_append(st):
             pool = torch.stack((low, high), dim=-1).reshape(*low.shape[:-1], dh) * scales[..., 1:2] + scales[..., 0:1]
             f = x.float()              # a cache of 4 bits is made from values, lowest and step of 32
             lo = torch.min(f, dim=-1, keepdim=True).values
-            step = torch.div(torch.max(f, dim=-1, keepdim=True).values - lo, 15.0)
+            step = torch.div(torch.max(f, dim=-1, keepdim=True).values - lo, torch.tensor(15.0, device="cuda"))
             x = torch.where(step > 0, lo.double() + step.double() * torch.clamp(torch.round(torch.div(f - lo, step)), 0, 15).double(), lo.double())
         else:
             pool = st["c" + name].double()

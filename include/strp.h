@@ -374,6 +374,84 @@ strp_status strp_token_logprobs(strp_ctx* ctx, const void* logits, strp_dtype dt
 /* Workspace (bytes, device) that strp_token_logprobs needs; pure function. */
 size_t strp_token_logprobs_workspace_bytes(int32_t V, int64_t T, int32_t n_top);
 
+/* ---- what a model needs to generate: a paged cache, attention over it, verification of drafts ----
+ *
+ * Activations as above; nothing here touches the status word.  A cache holds the keys and values of many sequences in pages of `page` tokens:
+ *   K, V [pages x kv_heads x page x d_head], a token's channels contiguous (that is how the attention of single tokens reads them), in
+ *     STRP_CACHE_BF16, STRP_CACHE_F32: values of that type;
+ *     STRP_CACHE_Q4: two channels a byte, the even one in the lower half, as whole numbers n of 0 to 15 that stand for lowest + n step;
+ *       K_scale, V_scale [pages x kv_heads x page x 2] fp32: lowest and step of a token's channels in one head.
+ *   table [n_seq x ld_table]: the pages of a sequence in the order of its tokens: token j is row j % page of page table[j / page].
+ *   past [n_seq]: tokens that the cache holds of each sequence before the call's own;  seq_start: n_seq + 1 ascending offsets into the
+ *     call's T tokens, as in strp_attention, or NULL for one sequence of all of them (n_seq = 1).  Token t of sequence i has
+ *     the position past[i] + t - seq_start[i].  A call of strp_cache_append and the strp_cache_attention behind it take the same arrays.
+ * Wrong entries of table, past and seq_start (negative, too large, not ascending) give wrong results, no access out of bounds: pages
+ * outside the cache are not written, and are read as if they were the nearest one; positions from ld_table * page on are not stored.
+ */
+typedef enum { STRP_CACHE_BF16 = 0, STRP_CACHE_F32 = 1, STRP_CACHE_Q4 = 2 } strp_cache_format;
+typedef struct {
+  void* K;
+  void* V;
+  float* K_scale;
+  float* V_scale;
+  const int32_t* table;
+  const int32_t* past;
+  const int32_t* seq_start;
+  int32_t format, kv_heads, d_head, page, pages, n_seq, ld_table;
+} strp_cache;
+
+/*
+ * strp_cache_append -- keys and values of T new tokens into the pages of their sequences, keys (and queries) turned by their positions.
+ *   K [kv_heads*d_head x ldk], V [kv_heads*d_head x ldv], Q [heads*d_head x ldq] or NULL, Qr [heads*d_head x ldqr] (Q itself is allowed, same
+ *   ld), all of dtype.  inv_freq [rot / 2] fp32; rot = 0 and NULL: nothing is turned.  With a = position inv_freq[j] (a product in 64 bits):
+ *     (x, y) -> (x cos a - y sin a, y cos a + x sin a)  for channels (j, j + rot / 2) of each head, or (2j, 2j + 1) where pairs != 0,
+ *   in 64 bits, rounded to fp32 and then to the output's type; channels from rot on are as they were.
+ *   STRP_CACHE_Q4, for a token and head, all of it in fp32 on the turned keys of fp32: lowest = min x, step = (max x - lowest) / 15,
+ *   n = (x - lowest) / step to the nearest whole number (0 where step is 0).  What is not finite, or a range that fp32 does not hold,
+ *   stands for values that are not finite.
+ * Tokens outside every sequence are not stored, and their Qr keeps what it holds.  No two tokens may have one place.
+ * Errors: STRP_EINVAL (null K, V or cache pointers, sizes not positive, d_head no multiple of 8 or above 128, page no power of two from 16 to
+ * 65536, ld_table * page above 2^30, heads or kv_heads above 1024, n_seq above 65536, T above 2^27, rot odd, negative or above d_head, inv_freq
+ * missing, Q without Qr, a cache of the other type than dtype, scales missing, bad ld, misaligned, unknown dtype or format).
+ */
+typedef struct {
+  strp_cache cache;
+  const void* K;
+  const void* V;
+  const void* Q;
+  void* Qr;
+  const float* inv_freq;
+  int32_t dtype, heads, rot, pairs;
+  int64_t T, ldk, ldv, ldq, ldqr;
+} strp_cache_append_in;
+strp_status strp_cache_append(strp_ctx* ctx, const strp_cache_append_in* in);
+
+/*
+ * strp_cache_attention -- attention of T new tokens over the cache, which holds them already: a token at position q of its sequence sees
+ * the keys 0 .. q:  c = sum_j softmax_j(scale q . k_j) v_j.
+ *   Q, C [heads*d_head x ldq / ldc] of dtype;  kv_of_head as in strp_attention.  The cache is of dtype, or STRP_CACHE_Q4.
+ * One token a sequence or thousands, sequences of any lengths beside each other.  Tokens outside every sequence keep what C holds.  What a
+ * token does not see has no part in its result, whatever it holds, infinities and NaN included.
+ * bf16: products of bf16 with fp32 sums; probabilities meet V as the context's precision says, as in strp_attention; whole numbers of 4 bits
+ * enter the products exactly, lowest and step in fp32.  fp32: products of fp32.  The division by the sum of the probabilities comes last.
+ * A call repeated on the same inputs gives the same bits; how the keys are split depends on all sequences of the call, so the
+ * last bits of a sequence's results may depend on the lengths of the others.
+ * Errors: STRP_EINVAL (as strp_cache_append; heads * T above 2^30; scale not positive or above 2e38; kv_heads that does not divide heads without kv_of_head),
+ * STRP_ENOMEM (strp_cache_attention_workspace_bytes).
+ */
+typedef struct {
+  strp_cache cache;
+  const void* Q;
+  void* C;
+  const int32_t* kv_of_head;
+  int32_t dtype, heads;
+  float scale;
+  int64_t T, ldq, ldc;
+} strp_cache_attention_in;
+strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* in);
+/* Workspace (bytes, device) that strp_cache_attention needs for any call with this d_head; pure function. */
+size_t strp_cache_attention_workspace_bytes(int32_t d_head);
+
 /* ---- stateful per-module path ---------------------------------------------------------- */
 typedef struct {
   const void* X;       /* [d x ldx]   x_dtype                                               */

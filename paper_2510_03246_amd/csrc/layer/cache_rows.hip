@@ -1,0 +1,751 @@
+// Attention of new tokens over a paged cache, few rows at a time.
+//
+//   c = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),  j = 0 .. position of the token.
+// A row is a head at a token; the rows that share keys (the heads of a group, the new tokens of a sequence) are taken 16 at a time.  The work is cut into units, a
+// tile of rows by 128 (fp32: 64) keys, numbered sequence by sequence, and every workgroup gets as many of them as any other, one after the other: so a long sequence
+// beside short ones, or one alone, fills the chip as well as many alike.  The lengths are in device memory, so every workgroup works its share out
+// for itself.  What it does not finish it leaves as (maximum, sum, weighted sum) in the workspace, and a second kernel puts such parts together in their order.
+#include "paged_cache.h"
+
+#include <type_traits>
+
+namespace strp {
+
+constexpr int ROWS = 16;
+constexpr float LOG2E = 1.44269504088896341f;
+
+struct RowsP {
+  Pages c;
+  const void* Q;
+  void* C;
+  const void* K;
+  const void* V;
+  const floatx4* sK;       // (lowest, step) of two keys
+  const floatx4* sV;
+  const int32_t* kv_of_head;
+  int heads, group;
+  long long ldq, ldc;
+  float scale_log2e;
+  int workers, least;      // workgroups, and the fewest units that one gets
+  // what workgroups leave unfinished: [workers][2], of a tile of rows that began before (0) or goes on behind (1)
+  float* part;             // [slot][row][channels]
+  float2* ml;              // [slot][row]
+  long long* off;          // [slot][row] where the row's results go, -1: no such row
+  int* parts;              // [worker] how many workgroups share the tile that begins in slot 1; 0: none
+};
+
+__device__ __forceinline__ float both_16(float x, bool sum) {      // with the lane 16 further in its half
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  const unsigned a = r[0], b = r[1];
+  return sum ? __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b) : __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+__device__ __forceinline__ float both_32(float x, bool sum) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  const unsigned a = r[0], b = r[1];
+  return sum ? __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b) : __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
+}
+// over the four lanes that have the same row
+__device__ __forceinline__ float quads_max(float x) { return both_32(both_16(x, false), false); }
+__device__ __forceinline__ float quads_sum(float x) { return both_32(both_16(x, true), true); }
+
+// a value that all lanes have, in scalar registers
+__device__ __forceinline__ long long uniform(long long x) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (long long)((unsigned long long)hi << 32 | lo);
+}
+
+// a base that stays in scalar registers beside its lanes' offsets (or the sums of both that do not change are kept in vector registers, two for an address)
+__device__ __forceinline__ const char* opaque(const char* p) {
+  asm("" : "+s"(p));
+  return p;
+}
+
+__device__ __forceinline__ unsigned pick(unsigned a, unsigned b, unsigned sel) { return __builtin_amdgcn_perm(b, a, sel); }
+constexpr unsigned LOWS = 0x05040100u, HIGHS = 0x07060302u;      // the lower, the upper halves of a and b
+// whole numbers 0..15 in bits 0-3 and 16-19 as bf16 of 128 + n, which is exact
+__device__ __forceinline__ unsigned with_128(unsigned x) { return (x & 0x000F000Fu) | 0x43004300u; }
+
+// One tile of the cache's keys or values as a lane has it.  Keys: lane (key l % 16, quarter l / 16 of a step of the contraction).  Values: channels W (l % 16) .. + W of
+// the keys 4 (l / 16) .. + 4, which is where the probabilities of the scores' registers are.
+//   E: type of the activations; Q4; W: channels of a value's lane, 16 W >= d_head
+template <typename E, bool Q4, int W>
+struct Tile;
+
+template <int W>
+struct Tile<__bf16, false, W> {
+  static constexpr int NC = W / 2;
+  typedef uintx4 Key;
+  Key k[NC];
+  unsigned v[4][W / 2];
+};
+template <int W>
+struct Tile<float, false, W> {
+  static constexpr int NC = W;
+  typedef floatx4 Key;
+  Key k[NC];
+  float v[4][W];
+};
+template <typename E, int W>
+struct TileQ4 {
+  static constexpr int NC = W / 2;
+  unsigned k[NC];
+  unsigned v[4];
+  floatx4 ks[2], vs[2];
+};
+template <int W>
+struct Tile<__bf16, true, W> : TileQ4<__bf16, W> {};
+template <int W>
+struct Tile<float, true, W> : TileQ4<float, W> {};
+
+template <typename E, bool Q4, int W, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
+  constexpr bool BF = sizeof(E) == 2;
+  typedef Tile<E, Q4, W> TileT;
+  constexpr int NC = TileT::NC, DH = 16 * W, PITCH = DH + 4;
+  constexpr int NT = BF || Q4 ? 2 : 1, KW = 16 * NT, UNIT = 4 * KW;      // tiles and keys of a wavefront in a unit, keys of a unit
+  __shared__ __attribute__((aligned(16))) float sO[4][ROWS][PITCH];
+  __shared__ float sM[4][ROWS], sL[4][ROWS];
+  __shared__ long long sOff[ROWS];
+  __shared__ unsigned short sOrder[MAX_CACHE_HEADS];      // the heads by the key-value head that they read
+  __shared__ int sFirst[MAX_CACHE_HEADS + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quad = lane >> 4;
+  const Pages& c = p.c;
+  const int dh = c.dh;
+  // neighbours in the work are neighbours on an XCD
+  const int worker = (int)(blockIdx.x & 7) * (p.workers >> 3) + (int)(blockIdx.x >> 3);
+
+  if (p.kv_of_head) {
+    __shared__ int sOf[MAX_CACHE_HEADS];
+    for (int h = tid; h < p.heads; h += 256) sOf[h] = clamped(p.kv_of_head[h], 0, c.kv_heads - 1);
+    __syncthreads();
+    for (int h = tid; h < p.heads; h += 256) {
+      int at = 0;
+      for (int o = 0; o < p.heads; ++o) at += sOf[o] < sOf[h] || (sOf[o] == sOf[h] && o < h);
+      sOrder[at] = (unsigned short)h;
+    }
+    for (int g = tid; g <= c.kv_heads; g += 256) {
+      int at = 0;
+      for (int o = 0; o < p.heads; ++o) at += sOf[o] < g;
+      sFirst[g] = at;
+    }
+    __syncthreads();
+  }
+  auto group_of = [&](int kv) { return p.kv_of_head ? sFirst[kv + 1] - sFirst[kv] : p.group; };
+  auto tiles_of = [&](int n) {             // tiles of rows of a sequence with n new tokens
+    if (!p.kv_of_head) return c.kv_heads * ((n * p.group + ROWS - 1) / ROWS);
+    int sum = 0;
+    for (int g = 0; g < c.kv_heads; ++g) sum += (n * group_of(g) + ROWS - 1) / ROWS;
+    return sum;
+  };
+  struct Seq { int begin, n, past, units, tiles; };
+  auto sequence = [&](int s) {
+    Seq q;
+    q.begin = seq_begin(c, s);
+    q.n = max(seq_begin(c, s + 1) - q.begin, 0);
+    q.past = seq_past(c, s);
+    q.units = q.n ? (min(q.past + q.n, c.cap) + UNIT - 1) / UNIT : 0;
+    q.tiles = q.n ? tiles_of(q.n) : 0;
+    return q;
+  };
+  // this workgroup's units, and the sequence that they begin in
+  const int each = (c.n_seq + 63) / 64;
+  long long mine = 0;
+  for (int i = 0; i < each; ++i)
+    if (lane * each + i < c.n_seq) {
+      const Seq q = sequence(lane * each + i);
+      mine += (long long)q.units * q.tiles;
+    }
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long x = __shfl_up(upto, o, 64);
+    upto += lane >= o ? x : 0;
+  }
+  const long long total = uniform(__shfl(upto, 63, 64));
+  long long per = (total + p.workers - 1) / p.workers;
+  per = per < p.least ? p.least : per;
+  long long u = worker * per;
+  const long long u1 = u + per < total ? u + per : total;
+  if (tid == 0) p.parts[worker] = 0;
+  if (tid < 2 * ROWS) p.off[(long long)worker * 2 * ROWS + tid] = -1;
+  if (u >= u1) return;
+  const unsigned long long holds = __builtin_amdgcn_ballot_w64(upto - mine <= u && u < upto);
+  const int holder = __builtin_ctzll(holds);
+  int s = __builtin_amdgcn_readfirstlane(holder * each);
+  long long base = uniform(__shfl(upto - mine, holder, 64));
+  auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  auto uniform_sequence = [&] {
+    const Seq x = sequence(s);
+    return Seq{same(x.begin), same(x.n), same(x.past), same(x.units), same(x.tiles)};
+  };
+  Seq q = uniform_sequence();
+  auto next_sequence = [&] {
+    base += (long long)q.units * q.tiles;
+    ++s;
+    q = uniform_sequence();
+  };
+  while (u >= base + (long long)q.units * q.tiles) next_sequence();
+
+  while (true) {
+    // ---- a segment: blocks b0 .. b1 of one tile of rows ----
+    const long long rel = u - base;
+    const int row_tile = (int)(rel / q.units), b0 = (int)(rel - (long long)row_tile * q.units);
+    const int b1 = (long long)q.units - b0 < u1 - u ? q.units : b0 + (int)(u1 - u);
+    int kv, rt, group;
+    if (!p.kv_of_head) {
+      const int per_kv = (q.n * p.group + ROWS - 1) / ROWS;
+      kv = row_tile / per_kv;
+      rt = row_tile - kv * per_kv;
+      group = p.group;
+    } else {
+      rt = row_tile;
+      for (kv = 0; kv < c.kv_heads - 1; ++kv) {
+        const int t = (q.n * same(group_of(kv)) + ROWS - 1) / ROWS;
+        if (rt < t) break;
+        rt -= t;
+      }
+      group = same(group_of(kv));
+    }
+    const int rows = min(ROWS, q.n * group - rt * ROWS), r = min(n16, rows - 1);
+    const int at = rt * ROWS + r, token = at / group, in_group = at - token * group;
+    const int head = p.kv_of_head ? sOrder[sFirst[kv] + in_group] : kv * group + in_group;
+    const int keys = min(q.past + q.n, c.cap);
+    const int see = min(q.past + token, keys - 1);                                             // the row's last key
+    const int see_all = min(q.past + rt * ROWS / group, keys - 1), see_any = min(q.past + (rt * ROWS + rows - 1) / group, keys - 1);
+    const long long out = (long long)head * dh * p.ldc + q.begin + token;
+
+    // the row's query as the second operand
+    int width = dh, quarter = quad;
+    asm volatile("" : "+s"(width), "+v"(quarter));        // what this works out is not worth registers for the rest of the kernel
+    const E* Qp = (const E*)p.Q + (long long)head * dh * p.ldq + q.begin + token;
+    uintx4 qb[BF ? NC : 1];
+    float qf[BF ? 1 : (Q4 ? NC * 8 : NC * 4)];
+    float qsum = 0.0f;
+    if constexpr (BF) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        unsigned short e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          // of 4 bits a lane has channels 8 NC apart where its heads are whole, with channel j beside j + 4
+          const int ch = Q4 ? (width == DH ? 8 * NC * quarter + 8 * i : 32 * i + 8 * quarter) + (j >> 1) + 4 * (j & 1) : 32 * i + 8 * quarter + j;
+          e[j] = ((const unsigned short*)Qp)[(long long)(ch < width ? ch : 0) * p.ldq];
+          e[j] = ch < width ? e[j] : (unsigned short)0;
+          if constexpr (Q4) qsum += __builtin_bit_cast(float, (unsigned)e[j] << 16);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qb[i][j] = (unsigned)e[2 * j] | (unsigned)e[2 * j + 1] << 16;
+        __builtin_amdgcn_sched_barrier(0);       // not every address at once, for the registers
+      }
+    } else {
+      constexpr int PER = Q4 ? 8 : 4;
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const int ch = Q4 ? (width == DH ? 8 * NC * quarter + 8 * i : 32 * i + 8 * quarter) + j : 16 * i + 4 * quarter + j;
+          const float x = ((const float*)Qp)[(long long)(ch < width ? ch : 0) * p.ldq];
+          qf[i * PER + j] = ch < width ? x : 0.0f;
+          if constexpr (Q4) qsum += qf[i * PER + j];
+          if (j == PER - 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if constexpr (Q4) qsum = quads_sum(qsum);
+
+    // pages of the wavefront's keys: lane l has that of tile l % NT of its keys in block bt + l / NT
+    const int32_t* table = c.table + (long long)s * c.ld_table;
+    int ids = 0, bt = b0;
+    auto look_up = [&](int b) {
+      const int key = (b + lane / NT) * UNIT + wave * KW + (lane % NT) * 16;
+      ids = clamped(table[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
+    };
+    const int in_page = (1 << c.page_log2) - 1;
+    auto tile_row = [&](int b, int t) {    // the row of the cache that the wavefront's tile t of block b begins at
+      const int page = __builtin_amdgcn_readlane(ids, NT * (b - bt) + t);
+      return (((long long)page * c.kv_heads + kv) << c.page_log2) + ((b * UNIT + wave * KW + t * 16) & in_page);
+    };
+
+    TileT T[NT];
+    auto load_k = [&](int b) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const long long row = tile_row(b, t);
+        if constexpr (!Q4) {
+          const char* g = opaque((const char*)p.K + row * (dh * (int)sizeof(E)));
+          constexpr int CH = BF ? 32 : 16, LN = CH / 4;
+#pragma unroll
+          for (int i = 0; i < NC; ++i) {
+            const int ch = CH * i + LN * quad;
+            T[t].k[i] = *(const typename TileT::Key*)(g + (unsigned)(n16 * dh + (ch < dh ? ch : 0)) * (unsigned)sizeof(E));
+          }
+        } else {
+          const char* g = opaque((const char*)p.K + row * (dh / 2));
+          if (dh == DH) {
+            typedef unsigned vec __attribute__((ext_vector_type(NC)));
+            const vec x = *(const vec*)(g + (unsigned)(n16 * (DH / 2) + 4 * NC * quad));
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+              if constexpr (NC == 1) T[t].k[i] = x[0];
+              else T[t].k[i] = x[i];
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+              const int ch = 32 * i + 8 * quad;
+              T[t].k[i] = *(const unsigned*)(g + (unsigned)(n16 * (dh / 2) + (ch < dh ? ch : 0) / 2));
+            }
+          }
+          const floatx4* sc = (const floatx4*)(opaque((const char*)(p.sK + (row >> 1))) + 32u * (unsigned)quad);
+          T[t].ks[0] = sc[0];
+          T[t].ks[1] = sc[1];
+        }
+      }
+    };
+    auto load_v = [&](int b) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const long long row = tile_row(b, t);
+        const int ch = W * n16 < dh ? W * n16 : 0;
+        const char* rows_at = opaque((const char*)p.V + (Q4 ? row * (dh / 2) : row * (dh * (int)sizeof(E))));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (!Q4) {
+            const E* g = (const E*)(rows_at + (unsigned)((4 * quad + e) * dh + ch) * (unsigned)sizeof(E));
+            if constexpr (BF) {
+              typedef unsigned vec __attribute__((ext_vector_type(W / 2)));
+              const vec x = *(const vec*)g;
+#pragma unroll
+              for (int j = 0; j < W / 2; ++j) {
+                if constexpr (W == 2) T[t].v[e][j] = x[0];
+                else T[t].v[e][j] = x[j];
+              }
+            } else {
+              load_floats<(W < 4 ? W : 4)>(g, *(float(*)[W < 4 ? W : 4]) & T[t].v[e][0]);
+              if constexpr (W == 8) load_floats<4>(g + 4, *(float(*)[4]) & T[t].v[e][4]);
+            }
+          } else {
+            const char* g = rows_at + (unsigned)((4 * quad + e) * (dh / 2) + ch / 2);
+            if constexpr (W == 8) T[t].v[e] = *(const unsigned*)g;
+            else if constexpr (W == 4) T[t].v[e] = *(const unsigned short*)g;
+            else T[t].v[e] = *(const unsigned char*)g;
+          }
+        }
+        if constexpr (Q4) {
+          const floatx4* sc = (const floatx4*)(opaque((const char*)(p.sV + (row >> 1))) + 32u * (unsigned)quad);
+          T[t].vs[0] = sc[0];
+          T[t].vs[1] = sc[1];
+        }
+      }
+    };
+
+    floatx4 O[W];
+    float m, l, weight, lowest;            // weight: sum of what the values were multiplied by (of 4 bits: to take 128 off again); lowest: of p lowest
+    bool careful = false, odd;
+    while (true) {
+      odd = false;
+#pragma unroll
+      for (int j = 0; j < W; ++j) O[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+      m = -INFINITY;
+      l = weight = lowest = 0.0f;
+      // the wavefront's blocks that some row sees
+      const int keys_of_wave = see_any - wave * KW;
+      const int be = keys_of_wave < 0 ? b0 : min(b1, keys_of_wave / UNIT + 1);
+      if (b0 < be) {
+        bt = b0;
+        look_up(bt);
+        load_k(b0);
+        load_v(b0);
+      }
+#pragma unroll 1
+      for (int b = b0; b < be; ++b) {
+        const int k0 = b * UNIT + wave * KW;
+        floatx4 S[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float from = BF && Q4 ? -128.0f * qsum : 0.0f;
+          S[t] = floatx4{from, from, from, from};
+          if constexpr (BF && !Q4) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+              uintx4 k = T[t].k[i];
+              if (32 * i + 32 > dh) {
+                const unsigned keep = 32 * i + 8 * quad < dh ? ~0u : 0u;
+                k &= uintx4{keep, keep, keep, keep};
+              }
+              S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qb[i]), S[t], 0, 0, 0);
+            }
+          } else if constexpr (BF) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+              const unsigned x = T[t].k[i];
+              const uintx4 k = uintx4{with_128(x), with_128(x >> 4), with_128(x >> 8), with_128(x >> 12)};
+              S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qb[i]), S[t], 0, 0, 0);
+            }
+          } else if constexpr (!Q4) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float k = T[t].k[i][e];
+                if (16 * i + 16 > dh) k = 16 * i + 4 * quad < dh ? k : 0.0f;
+                S[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, qf[4 * i + e], S[t], 0, 0, 0);
+              }
+          } else {
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                S[t] = __builtin_amdgcn_mfma_f32_16x16x4f32((float)(T[t].k[i] >> (4 * e) & 15u), qf[8 * i + e], S[t], 0, 0, 0);
+          }
+          if constexpr (Q4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[t][e] = __builtin_fmaf(S[t][e], T[t].ks[e >> 1][2 * (e & 1) + 1], qsum * T[t].ks[e >> 1][2 * (e & 1)]);
+        }
+        const bool more = b + 1 < be;
+        if (more) {
+          if (b + 1 - bt == 64 / NT) {
+            bt = b + 1;
+            look_up(bt);
+          }
+          load_k(b + 1);
+        }
+        // the softmax: lane (row, quad) has the keys 4 quad .. + 4 of both tiles
+        const bool whole = k0 + KW - 1 <= see_all;
+        if (!whole)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[t][e] = k0 + 16 * t + 4 * quad + e <= see ? S[t][e] : -INFINITY;
+        float mt = m;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mt = __builtin_elementwise_maximum(mt, S[t][e]);
+        mt = quads_max(mt);
+        const bool grown = !((mt - m) * p.scale_log2e <= 8.0f || mt == -INFINITY);      // until then what the row holds stays as it is
+        if (__builtin_amdgcn_ballot_w64(grown)) {
+          const float fac = grown ? __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e) : 1.0f;
+          l *= fac;
+          weight *= fac;
+          lowest *= fac;
+#pragma unroll
+          for (int j = 0; j < W; ++j) O[j] *= fac;
+          m = grown ? mt : m;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float P[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            P[t][e] = __builtin_amdgcn_exp2f((S[t][e] - ref) * p.scale_log2e);      // the difference first: it is exact, or small against what it is taken from
+            if constexpr (!BF || SPLIT || Q4) l += P[t][e];
+            if constexpr (Q4) {
+              const bool seen = whole || k0 + 16 * t + 4 * quad + e <= see;
+              lowest += seen ? P[t][e] * T[t].vs[e >> 1][2 * (e & 1)] : 0.0f;
+              P[t][e] = seen ? P[t][e] * T[t].vs[e >> 1][2 * (e & 1) + 1] : 0.0f;
+            }
+          }
+        // Values.  Where some key is not seen by every row, a value that is not finite would reach those too, by a probability of zero:
+        // such values are left out of the products and added to the results of the rows that see them.
+        const bool check = !Q4 && (careful || !whole);
+        if constexpr (BF) {
+          uintx4 hi, lo;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const float x0 = P[d >> 1][2 * (d & 1)], x1 = P[d >> 1][2 * (d & 1) + 1];
+            if constexpr (SPLIT) {
+              // hi has the upper 16 bits and lo what that leaves: together within 2^-16
+              const unsigned b0_ = __builtin_bit_cast(unsigned, x0), b1_ = __builtin_bit_cast(unsigned, x1);
+              hi[d] = pick(b0_, b1_, HIGHS);
+              const float h0 = __builtin_bit_cast(float, b0_ & 0xffff0000u), h1 = __builtin_bit_cast(float, b1_ & 0xffff0000u);
+              const bf16x2 rest = bf16x2{(__bf16)(x0 - h0), (__bf16)(x1 - h1)};
+              lo[d] = __builtin_bit_cast(unsigned, rest);
+              if constexpr (Q4) weight += (h0 + (float)rest[0]) + (h1 + (float)rest[1]);
+            } else {
+              const bf16x2 one = bf16x2{(__bf16)x0, (__bf16)x1};
+              hi[d] = __builtin_bit_cast(unsigned, one);
+              if constexpr (Q4) weight += (float)one[0] + (float)one[1];
+              else l += (float)one[0] + (float)one[1];
+            }
+          }
+          if constexpr (!Q4) {
+            if (check)
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                  for (int j = 0; j < W / 2; ++j) {
+                    const unsigned x = T[t].v[e][j];
+                    const bool a = (x & 0x7f80u) == 0x7f80u, z = (x & 0x7f800000u) == 0x7f800000u;
+                    odd = odd || a || z;
+                    T[t].v[e][j] = (a ? 0u : x & 0xffffu) | (z ? 0u : x & 0xffff0000u);
+                  }
+          }
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            uintx4 v;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {      // keys 2 d and 2 d + 1 of the lane's eight
+              if constexpr (!Q4) {
+                v[d] = pick(T[d >> 1].v[2 * (d & 1)][j >> 1], T[d >> 1].v[2 * (d & 1) + 1][j >> 1], j & 1 ? HIGHS : LOWS);
+              } else {
+                const unsigned a = T[d >> 1].v[2 * (d & 1)], z = T[d >> 1].v[2 * (d & 1) + 1];
+                v[d] = with_128(pick(a, z, j < 4 ? LOWS : HIGHS) >> (4 * (j & 3)));
+              }
+            }
+            O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi), O[j], 0, 0, 0);
+            if constexpr (SPLIT) O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, lo), O[j], 0, 0, 0);
+            if (j % 2) __builtin_amdgcn_sched_barrier(0);      // not every operand at once, for the registers
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int j = 0; j < W; ++j) {
+                float v;
+                if constexpr (Q4) {
+                  v = (float)(T[t].v[e] >> (4 * j) & 15u);
+                } else {
+                  v = T[t].v[e][j];
+                  if (check) {
+                    const bool fin = fabsf(v) < INFINITY;
+                    odd = odd || !fin;
+                    v = fin ? v : 0.0f;
+                  }
+                }
+                O[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, P[t][e], O[j], 0, 0, 0);
+              }
+        }
+        if (more) load_v(b + 1);
+      }
+      if constexpr (!Q4) {
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+          // rare: the values of the blocks that were looked at once more, key by key, those that are not finite to the rows that see them
+#pragma unroll 1
+          for (int b = b0; b < be; ++b) {
+            const int k0 = b * UNIT + wave * KW;
+            if (!careful && k0 + KW - 1 <= see_all) continue;
+#pragma unroll 1
+            for (int key = k0; key < k0 + KW && key <= see_any; ++key) {
+              int width = dh, from = 4 * W * quad;
+              asm volatile("" : "+s"(width), "+v"(from));
+              const int page = clamped(table[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
+              const E* g = (const E*)p.V + ((((long long)page * c.kv_heads + kv) << c.page_log2) + (key & in_page)) * dh;
+#pragma unroll
+              for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int ch = from + W * e + j;
+                  const float v = (float)g[ch < width ? ch : 0];
+                  O[j][e] += key <= see && !(fabsf(v) < INFINITY) ? v : 0.0f;
+                  __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+          }
+        }
+      }
+      if (Q4 || careful) break;
+      // a value that is not finite and was seen by all has met a probability, or a part of one, that may be zero: the keys once more, looking at every value
+      float most = 0.0f;
+#pragma unroll
+      for (int j = 0; j < W; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = __builtin_elementwise_maximum(most, fabsf(O[j][e]));
+      if (!__builtin_amdgcn_ballot_w64(!(most < INFINITY))) break;
+      careful = true;
+    }
+
+    // ---- the four wavefronts together ----
+    l = quads_sum(l);
+    if constexpr (Q4) {
+      lowest = quads_sum(lowest);
+      if constexpr (BF) lowest -= 128.0f * quads_sum(weight);
+#pragma unroll
+      for (int j = 0; j < W; ++j) O[j] += lowest;
+    }
+    __syncthreads();                       // the segment before has been read
+    if (quad == 0) {
+      sM[wave][n16] = m;
+      sL[wave][n16] = l;
+      if (wave == 0) sOff[n16] = n16 < rows ? out : -1;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < W; ++j) sO[wave][n16][W * (4 * quad + e) + j] = O[j][e];
+    __syncthreads();
+    {
+      const int row = tid & 15;
+      float f[4], M = sM[0][row], L = 0.0f;
+#pragma unroll
+      for (int w = 1; w < 4; ++w) M = __builtin_elementwise_maximum(M, sM[w][row]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float mw = sM[w][row];
+        f[w] = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw - M) * p.scale_log2e);      // a wavefront that saw no key has zeros
+        L += f[w] * sL[w][row];
+      }
+      const bool whole_row = b0 == 0 && b1 == q.units;
+      const long long to = sOff[row];
+      const int slot = worker * 2 + (b0 == 0 ? 1 : 0);
+      if (to >= 0) {
+        const float inv = 1.0f / L;
+        for (int ch = tid >> 4; ch < dh; ch += 16) {
+          const float x = f[0] * sO[0][row][ch] + f[1] * sO[1][row][ch] + f[2] * sO[2][row][ch] + f[3] * sO[3][row][ch];
+          if (whole_row) ((E*)p.C)[to + (long long)ch * p.ldc] = (E)(x * inv);
+          else p.part[((long long)slot * ROWS + row) * dh + ch] = x;
+        }
+        if (!whole_row && tid < 16) {
+          p.ml[slot * ROWS + row] = float2{M, L};
+          p.off[slot * ROWS + row] = to;
+        }
+      }
+      // the workgroups from this one to that with the tile's last unit
+      if (!whole_row && b0 == 0 && tid == 0) p.parts[worker] = (int)((u - b0 + q.units - 1) / per) - worker + 1;
+    }
+    u += b1 - b0;
+    if (u >= u1) break;
+    while (u >= base + (long long)q.units * q.tiles) next_sequence();
+  }
+}
+
+// The parts of tiles that several workgroups had, in the order of the keys.  A workgroup for a row of the tile that begins in a workgroup of the first kernel: a wavefront has a fourth of
+// the parts, a lane two channels.
+template <typename E>
+__global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
+  __shared__ float sO[4][128];
+  __shared__ float sM[4], sL[4];
+  const int worker = (int)blockIdx.x, row = (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int parts = p.parts[worker];
+  if (parts == 0) return;
+  const long long first = (long long)worker * 2 + 1, to = p.off[first * ROWS + row];
+  if (to < 0) return;
+  const int dh = p.c.dh, ch = 2 * lane;
+  float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
+  constexpr int UN = 8;
+  for (int i0 = wave; i0 < parts; i0 += 4 * UN) {
+    float2 ml[UN], x[UN];
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const int i = i0 + 4 * k;
+      const long long at = (i == 0 ? first : (long long)(worker + min(i, parts - 1)) * 2) * ROWS + row;
+      ml[k] = p.ml[at];
+      x[k] = *(const float2*)(p.part + at * dh + (ch < dh ? ch : 0));
+      if (i >= parts) ml[k] = float2{-INFINITY, 0.0f};
+    }
+    float most = m;
+#pragma unroll
+    for (int k = 0; k < UN; ++k) most = __builtin_elementwise_maximum(most, ml[k].x);
+    const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((of - most) * p.scale_log2e); };
+    const float f = factor(m);
+    m = most;
+    l *= f;
+    o[0] *= f;
+    o[1] *= f;
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const float g = factor(ml[k].x);
+      if (g == 0.0f && i0 + 4 * k >= parts) continue;      // not 0 times whatever lies there
+      l += g * ml[k].y;
+      o[0] += g * x[k].x;
+      o[1] += g * x[k].y;
+    }
+  }
+  sO[wave][ch] = o[0];
+  sO[wave][ch + 1] = o[1];
+  if (lane == 0) {
+    sM[wave] = m;
+    sL[wave] = l;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x >= dh) return;
+  float most = sM[0], sum = 0.0f, L = 0.0f;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) most = __builtin_elementwise_maximum(most, sM[w]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = sM[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sM[w] - most) * p.scale_log2e);
+    L += f * sL[w];
+    sum += f * sO[w][threadIdx.x];
+  }
+  ((E*)p.C)[to + (long long)threadIdx.x * p.ldc] = (E)(sum / L);
+}
+
+constexpr int WORKERS = 512;               // two workgroups a CU
+
+struct RowsBytes { size_t part, ml, off, parts; };
+static RowsBytes rows_bytes(int dh) {
+  const size_t rows = (size_t)WORKERS * 2 * ROWS;
+  return RowsBytes{rows * dh * 4, rows * sizeof(float2), rows * 8, (size_t)WORKERS * 4};
+}
+static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
+
+template <typename E, bool Q4, bool SPLIT>
+static void launch_rows(strp_ctx* ctx, const RowsP& p, int join_rows) {
+  const dim3 grid((unsigned)p.workers), block(256);
+  if (p.c.dh <= 32) hipLaunchKernelGGL((cache_rows_kernel<E, Q4, 2, SPLIT>), grid, block, 0, ctx->stream, p);
+  else if (p.c.dh <= 64) hipLaunchKernelGGL((cache_rows_kernel<E, Q4, 4, SPLIT>), grid, block, 0, ctx->stream, p);
+  else hipLaunchKernelGGL((cache_rows_kernel<E, Q4, 8, SPLIT>), grid, block, 0, ctx->stream, p);
+  hipLaunchKernelGGL((cache_join_kernel<E>), dim3((unsigned)p.workers, (unsigned)join_rows), block, 0, ctx->stream, p);
+}
+
+}  // namespace strp
+
+using namespace strp;
+
+extern "C" {
+
+size_t strp_cache_attention_workspace_bytes(int32_t d_head) {
+  if (d_head <= 0 || d_head > 128) return 0;
+  const RowsBytes b = rows_bytes(d_head);
+  return 256 + up256(b.part) + up256(b.ml) + up256(b.off) + up256(b.parts);
+}
+
+strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* in) {
+  if (!ctx) return STRP_EINVAL;
+  if (!in || !in->Q || !in->C) return fail(ctx, STRP_EINVAL, "cache_attention: null Q or C");
+  const strp_cache& c = in->cache;
+  if (const char* e = cache_error(c, in->dtype, in->heads, in->T)) return fail(ctx, STRP_EINVAL, "cache_attention: %s", e);
+  if (in->T * in->heads > (1LL << 30)) return fail(ctx, STRP_EINVAL, "cache_attention: T * heads above 2^30");
+  if (!in->kv_of_head && in->heads % c.kv_heads) return fail(ctx, STRP_EINVAL, "cache_attention: kv_heads does not divide heads and kv_of_head is null");
+  if (!(in->scale > 0.0f) || !(in->scale <= 2.0e38f)) return fail(ctx, STRP_EINVAL, "cache_attention: scale must be positive and at most 2e38");
+  if (!token_ld(in->ldq, in->T) || !token_ld(in->ldc, in->T)) return fail(ctx, STRP_EINVAL, "cache_attention: leading dimensions must be multiples of 8 and not below T");
+  if (!ptr16(in->Q) || !ptr16(in->C)) return fail(ctx, STRP_EINVAL, "cache_attention: Q or C not 16-byte aligned");
+  if (!ctx->ws) return fail(ctx, STRP_ENOMEM, "cache_attention: no workspace set");
+  Arena arena(ctx);
+  const RowsBytes b = rows_bytes(c.d_head);
+  STRP_TAKE(ctx, arena, part, float, b.part / 4);
+  STRP_TAKE(ctx, arena, ml, float2, b.ml / sizeof(float2));
+  STRP_TAKE(ctx, arena, off, long long, b.off / 8);
+  STRP_TAKE(ctx, arena, parts, int, b.parts / 4);
+  OnDevice on(ctx);
+  if (!on.ok()) return fail(ctx, STRP_EHIP, "cache_attention: device %d cannot be made current", ctx->device);
+  RowsP p{pages_of(c, in->T), in->Q, in->C, c.K, c.V, (const floatx4*)c.K_scale, (const floatx4*)c.V_scale, in->kv_of_head, in->heads, in->heads / c.kv_heads,
+          in->ldq, in->ldc, in->scale * LOG2E, WORKERS, 1, part, ml, off, parts};
+  if (p.group == 0) p.group = 1;
+  // a tile has no more rows than the heads that one key-value head can have times the tokens
+  const long long rows = (in->kv_of_head ? in->heads : p.group) * in->T;
+  const int join_rows = rows < ROWS ? (int)rows : ROWS;
+  // the lengths are on the device: the operations and bytes of a cache that is full
+  const double keys = (double)p.c.cap, T = (double)in->T, row = c.format == STRP_CACHE_Q4 ? 0.5 * c.d_head + 8.0 : bytes_of(in->dtype) * (double)c.d_head;
+  ProfScope ps(ctx, "cache_attention", 4.0 * in->heads * c.d_head * T * keys, 2.0 * c.n_seq * keys * c.kv_heads * row);
+  const bool q4 = c.format == STRP_CACHE_Q4;
+  if (in->dtype == STRP_F32) {
+    if (q4) launch_rows<float, true, false>(ctx, p, join_rows);
+    else launch_rows<float, false, false>(ctx, p, join_rows);
+  } else if (ctx->precision == STRP_PREC_SPLIT) {
+    if (q4) launch_rows<__bf16, true, true>(ctx, p, join_rows);
+    else launch_rows<__bf16, false, true>(ctx, p, join_rows);
+  } else {
+    if (q4) launch_rows<__bf16, true, false>(ctx, p, join_rows);
+    else launch_rows<__bf16, false, false>(ctx, p, join_rows);
+  }
+  STRP_HIP(ctx, hipGetLastError());
+  return STRP_OK;
+}
+
+}  // extern "C"

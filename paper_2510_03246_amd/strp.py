@@ -24,6 +24,7 @@ PROD_GRAM, PROD_RHS2, PROD_RHS1, PROD_RESID, PROD_AUPD, PROD_ZUPD = range(6)
 STAGE_SELECT, STAGE_REFIT2, STAGE_REFIT1, STAGE_AUPD, STAGE_ZUPD, STAGE_OBJ = 1, 2, 4, 8, 16, 32
 STAGE_ALL = 63
 ACT_NONE, ACT_RELU, ACT_GELU = range(3)
+CACHE_BF16, CACHE_F32, CACHE_Q4 = range(3)
 TOP_MAX = 16
 
 EXPORTS = [
@@ -31,6 +32,7 @@ EXPORTS = [
     "strp_poll", "strp_workspace_bytes", "strp_module_cache_bytes", "strp_profile_enable", "strp_profile_read", "strp_profile_launches", "strp_gram", "strp_score_alloc", "strp_mask_topk", "strp_mask_topk_static", "strp_topk_workspace_bytes", "strp_weight_energy", "strp_alloc_inverse", "strp_alloc_softmax",
     "strp_refit", "strp_module_init", "strp_admm_step",
     "strp_linear", "strp_linear_workspace_bytes", "strp_layer_norm", "strp_attention", "strp_token_logprobs", "strp_token_logprobs_workspace_bytes",
+    "strp_cache_append", "strp_cache_attention", "strp_cache_attention_workspace_bytes",
 ]
 
 
@@ -87,9 +89,28 @@ class AttentionIn(C.Structure):
                 ("ldv", C.c_int64), ("ldc", C.c_int64)]
 
 
+class Cache(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_scale", C.c_void_p), ("V_scale", C.c_void_p), ("table", C.c_void_p), ("past", C.c_void_p),
+                ("seq_start", C.c_void_p), ("format", C.c_int32), ("kv_heads", C.c_int32), ("d_head", C.c_int32), ("page", C.c_int32),
+                ("pages", C.c_int32), ("n_seq", C.c_int32), ("ld_table", C.c_int32)]
+
+
+class CacheAppendIn(C.Structure):
+    _fields_ = [("cache", Cache), ("K", C.c_void_p), ("V", C.c_void_p), ("Q", C.c_void_p), ("Qr", C.c_void_p), ("inv_freq", C.c_void_p),
+                ("dtype", C.c_int32), ("heads", C.c_int32), ("rot", C.c_int32), ("pairs", C.c_int32), ("T", C.c_int64), ("ldk", C.c_int64),
+                ("ldv", C.c_int64), ("ldq", C.c_int64), ("ldqr", C.c_int64)]
+
+
+class CacheAttentionIn(C.Structure):
+    _fields_ = [("cache", Cache), ("Q", C.c_void_p), ("C", C.c_void_p), ("kv_of_head", C.c_void_p), ("dtype", C.c_int32), ("heads", C.c_int32),
+                ("scale", C.c_float), ("T", C.c_int64), ("ldq", C.c_int64), ("ldc", C.c_int64)]
+
+
 # Their bytes from the fields in order: a call's cost on the host is the marshalling, and packing in one go is the cheaper form of it.
 _LINEAR, _ATTENTION = struct.Struct("@5P6i5q"), struct.Struct("@6P5if5q")
 assert _LINEAR.size == C.sizeof(LinearIn) and _ATTENTION.size == C.sizeof(AttentionIn)
+_CACHE_APPEND, _CACHE_ATTENTION = struct.Struct("@7P7i4x5P4i5q"), struct.Struct("@7P7i4x3P2if4x3q")
+assert _CACHE_APPEND.size == C.sizeof(CacheAppendIn) and _CACHE_ATTENTION.size == C.sizeof(CacheAttentionIn)
 
 _packers = {}
 
@@ -156,6 +177,10 @@ def load_library():
     lib.strp_layer_norm.argtypes = [vp, vp, C.c_int, i32, i64, i64, vp, vp, dbl, vp, i64]
     lib.strp_attention.argtypes = [vp, vp]
     lib.strp_token_logprobs.argtypes = [vp, vp, C.c_int, i32, i64, i64, vp, vp, vp, i32, vp, vp, i64]
+    lib.strp_cache_append.argtypes = [vp, vp]
+    lib.strp_cache_attention.argtypes = [vp, vp]
+    lib.strp_cache_attention_workspace_bytes.argtypes = [i32]
+    lib.strp_cache_attention_workspace_bytes.restype = C.c_size_t
     lib.strp_linear_workspace_bytes.argtypes = [i32, i32, i64, C.c_int, C.c_int]
     lib.strp_linear_workspace_bytes.restype = C.c_size_t
     lib.strp_token_logprobs_workspace_bytes.argtypes = [i32, i64, i32]
@@ -468,6 +493,52 @@ class Context:
                                                 base + at * row if n_top else None, T))
         return res
 
+    # ---- what a model needs to generate ---------------------------------------------------
+    def _pages(self, cache, table, past, seq_start, T):
+        """Fields of strp_cache for a call on T tokens."""
+        if cache.device != self.device.index or table.get_device() != self.device.index:
+            raise ValueError(f"the cache or its table is not on {self.device}")
+        if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("table: needs contiguous int32 rows, one a sequence")
+        n_seq, ld = table.shape
+        return cache.fields[:4] + (table.data_ptr(), self._vector("past", past, n_seq, torch.int32), self._vector("seq_start", seq_start, n_seq + 1, torch.int32)) + cache.fields[4:] + (n_seq, ld)
+
+    def strp_cache_append(self, K, V, T, cache, table, past, seq_start=None, inv_freq=None, pairs=False, Q=None, q_out=None):
+        """Keys and values [kv_heads*d_head x ld] of T new tokens into the cache's pages: those of sequence i (tokens seq_start[i] to seq_start[i + 1]; None:
+        one sequence of all) behind the past[i] that it has, in the pages table[i].  inv_freq [rot / 2] fp32: the first rot channels of every head of K and Q are
+        turned by position * inv_freq, channels (j, j + rot / 2) together, or (2j, 2j + 1) with pairs.  Returns Q turned (q_out may be Q), None without Q."""
+        rows, dts = cache.kv_heads * cache.d_head, _CODES
+        ldk, ldv = self._matrix("K", K, rows, T, dts), self._matrix("V", V, rows, T, (K.dtype,))
+        heads = q = r = ldq = ldr = 0
+        if Q is not None:
+            if Q.dim() != 2 or Q.shape[0] % cache.d_head:
+                raise ValueError(f"Q: {tuple(Q.shape)} is not heads of {cache.d_head}")
+            heads = Q.shape[0] // cache.d_head
+            if q_out is None:
+                q_out = self._new(Q.shape[0], T, Q.dtype)
+            ldq, ldr = self._matrix("Q", Q, Q.shape[0], T, (K.dtype,)), self._matrix("q_out", q_out, Q.shape[0], T, (K.dtype,))
+            q, r = Q.data_ptr(), q_out.data_ptr()
+        rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
+        self.check(self.lib.strp_cache_append(self.h, _CACHE_APPEND.pack(
+            *self._pages(cache, table, past, seq_start, T), K.data_ptr(), V.data_ptr(), q, r, self._vector("inv_freq", inv_freq, rot // 2, torch.float32),
+            _CODES[K.dtype], heads, rot, bool(pairs), T, ldk, ldv, ldq, ldr)))
+        return q_out if q else None
+
+    def strp_cache_attention(self, Q, T, heads, cache, table, past, seq_start=None, kv_of_head=None, scale=None, out=None):
+        """Attention of T new tokens over the cache, which holds them already (strp_cache_append with the same table, past and seq_start): a token sees its
+        sequence up to itself.  Q [heads*d_head x ld], kv_of_head [heads] int32 (None: equal groups), scale 1 / sqrt(d_head) by default.  Returns the
+        head outputs, like Q."""
+        dh = cache.d_head
+        ldq = self._matrix("Q", Q, heads * dh, T, _CODES)
+        if out is None:
+            out = self._new(heads * dh, T, Q.dtype)
+        ldc = self._matrix("out", out, heads * dh, T, (Q.dtype,))
+        self.ensure_workspace(self.lib.strp_cache_attention_workspace_bytes(dh))
+        self.check(self.lib.strp_cache_attention(self.h, _CACHE_ATTENTION.pack(
+            *self._pages(cache, table, past, seq_start, T), Q.data_ptr(), out.data_ptr(), self._vector("kv_of_head", kv_of_head, heads, torch.int32),
+            _CODES[Q.dtype], heads, dh ** -0.5 if scale is None else scale, T, ldq, ldc)))
+        return out
+
     def strp_module_init(self, desc, state, params):
         self.check(self.lib.strp_module_init(self.h, C.byref(desc), C.byref(state), C.byref(params)))
 
@@ -476,6 +547,37 @@ class Context:
         self.check(self.lib.strp_admm_step(self.h, C.byref(desc), C.byref(state), C.byref(params),
                                            C.byref(rep) if rep is not None else None))
         return rep
+
+
+class PagedCache:
+    """Pages of keys and values: K, V [pages x kv_heads x page x d_head] of bf16 or fp32, or uint8 [.. x d_head / 2] for 4 bits, then with
+    K_scale, V_scale [pages x kv_heads x page x 2] fp32 (lowest, step).  A program keeps one for a layer and hands pages to sequences as it likes."""
+
+    def __init__(self, K, V, K_scale=None, V_scale=None):
+        q4 = K.dtype is torch.uint8
+        scales = (K_scale, V_scale) if q4 else ()
+        if K.dtype not in (torch.bfloat16, torch.float32, torch.uint8) or K.dim() != 4 or V.dtype is not K.dtype or V.shape != K.shape:
+            raise ValueError("K and V: [pages x kv_heads x page x d_head], both bf16, fp32, or uint8 (4 bits)")
+        if not q4 and (K_scale is not None or V_scale is not None):
+            raise ValueError("K_scale and V_scale belong to a cache of 4 bits")
+        if any(t is None or t.dtype is not torch.float32 or t.shape != K.shape[:3] + (2,) for t in scales):
+            raise ValueError("a cache of 4 bits needs K_scale and V_scale [pages x kv_heads x page x 2] fp32")
+        if any(not t.is_contiguous() or t.get_device() != K.get_device() for t in (K, V) + scales):
+            raise ValueError("the cache's tensors must be contiguous and on one device")
+        self.K, self.V, self.K_scale, self.V_scale = K, V, K_scale, V_scale
+        pages, self.kv_heads, self.page, width = K.shape
+        self.d_head, self.device = width * (2 if q4 else 1), K.get_device()
+        # as strp_cache has them, round what a call adds
+        self.fields = (K.data_ptr(), V.data_ptr()) + (tuple(t.data_ptr() for t in scales) or (0, 0)) + (CACHE_Q4 if q4 else _CODES[K.dtype], self.kv_heads, self.d_head, self.page, pages)
+
+    @classmethod
+    def empty(cls, ctx, pages, kv_heads, d_head, page=64, dtype=torch.bfloat16):
+        """A cache of `dtype` (torch.uint8: 4 bits) with nothing in it."""
+        with torch.cuda.stream(ctx.stream):
+            e = lambda width, dt: torch.empty((pages, kv_heads, page, width), dtype=dt, device=ctx.device)
+            if dtype is torch.uint8:
+                return cls(e(d_head // 2, dtype), e(d_head // 2, dtype), e(2, torch.float32), e(2, torch.float32))
+            return cls(e(d_head, dtype), e(d_head, dtype))
 
 
 class FFNModule:

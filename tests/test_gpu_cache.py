@@ -1,0 +1,588 @@
+"""The paged cache against its definitions in 64 bits: appending with the turn by position, and attention over the pages.
+
+U = 2^-23 bounds what one fp32 operation or one step of a matrix-core sum adds, relative to the magnitudes that meet there; H(t) is half a
+step of an output of type t.  Every bound is the count of such steps times the sum of magnitudes, worked out beside its use."""
+import math
+
+import pytest
+import torch
+
+from paper_2510_03246_amd import strp
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -23
+BF16, F32, Q4 = torch.bfloat16, torch.float32, torch.uint8
+CASES = [(BF16, BF16), (F32, F32), (BF16, Q4), (F32, Q4)]         # activations, cache
+IDS = ["bf16", "f32", "bf16-q4", "f32-q4"]
+
+
+def H(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def ld8(T):
+    return (T + 7) // 8 * 8
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return strp.Context(0)
+
+
+@pytest.fixture(scope="module")
+def fast():
+    c = strp.Context(0)
+    c.set_precision(strp.PREC_FAST)
+    return c
+
+
+def rand(shape, seed, dt=F32, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dt)
+
+
+def padded(rows, T, seed, dt, scale=1.0, ld=None, fill=float("nan")):
+    """[rows x ld] with data in the first T columns and `fill` behind them."""
+    x = torch.full((rows, ld or ld8(T)), fill, dtype=dt, device="cuda")
+    x[:, :T] = rand((rows, T), seed, dt, scale)
+    return x
+
+
+def close(got, want, tol, what=""):
+    got = got.double()
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), (what, int(bad.sum()), "worst", float(((got - want).abs() / tol.clamp_min(1e-300))[bad].max()), bad.nonzero()[:3].tolist())
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def values(cache):
+    """K and V as the cache's entries stand for them, in 64 bits: [pages x kv x page x d_head]"""
+    if cache.K.dtype != Q4:
+        return cache.K.double(), cache.V.double()
+    return tuple(s[..., :1].double() + torch.stack([p & 15, p >> 4], -1).flatten(-2).double() * s[..., 1:].double()
+                 for p, s in ((cache.K, cache.K_scale), (cache.V, cache.V_scale)))
+
+
+def random_cache(pages, kv, page, dh, dt, seed, bad=False):
+    """Every entry data; `bad`: what is not finite (4 bits: lowest and step)."""
+    if dt == Q4:
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        K, V = (torch.randint(0, 256, (pages, kv, page, dh // 2), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2))
+        s = []
+        for i in range(2):
+            x = rand((pages, kv, page, 2), seed + 2 + i)
+            x[..., 0] = -3.0 + 0.3 * x[..., 0]
+            x[..., 1] = 0.4 + 0.05 * x[..., 1]
+            s.append(torch.full_like(x, float("nan")) if bad else x)
+        return strp.PagedCache(K, V, *s)
+    K, V = rand((pages, kv, page, dh), seed, dt), rand((pages, kv, page, dh), seed + 1, dt)
+    if bad:
+        K.fill_(float("nan"))
+        V.fill_(float("inf"))
+    return strp.PagedCache(K, V)
+
+
+def copy_of(cache):
+    return strp.PagedCache(*(None if t is None else t.clone() for t in (cache.K, cache.V, cache.K_scale, cache.V_scale)))
+
+
+def table_for(seqs, page, pages, seed, spare=2):
+    """Pages for sequences of (new, past) tokens in random order, entries without use out of range."""
+    need = [-(-(n + p) // page) for n, p in seqs]
+    order = torch.randperm(pages, generator=torch.Generator().manual_seed(seed)).tolist()
+    assert sum(need) <= pages
+    table = torch.full((len(seqs), max(need) + spare), -1 if seed % 2 else 1 << 30, dtype=torch.int32)
+    for i, w in enumerate(need):
+        table[i, :w] = torch.tensor(order[:w], dtype=torch.int32)
+        order = order[w:]
+    return table.cuda()
+
+
+def starts_of(seqs, first=0):
+    s = [first]
+    for n, _ in seqs:
+        s.append(s[-1] + n)
+    return s
+
+
+# ---- append ---------------------------------------------------------------------------------------------------------
+def turned(x, dh, pos, inv_freq, pairs):
+    """x [heads*dh x T] in 64 bits, and a bound of what sine, cosine and their products in 64 bits add."""
+    x = x.double().reshape(-1, dh, x.shape[1])
+    y, err = x.clone(), torch.zeros_like(x)
+    if inv_freq is not None:
+        half = inv_freq.numel()
+        a = inv_freq.double()[:, None] * pos.double()[None, :]
+        c, s = torch.cos(a), torch.sin(a)
+        i, j = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if pairs else (slice(0, half), slice(half, 2 * half))
+        y[:, i], y[:, j] = x[:, i] * c - x[:, j] * s, x[:, j] * c + x[:, i] * s
+        err[:, i] = err[:, j] = 2.0 ** -48 * (x[:, i].abs() + x[:, j].abs())
+    return y.reshape(-1, x.shape[2]), err.reshape(-1, x.shape[2])
+
+
+def append_case(ctx, seqs, heads, kv, dh, page, dts, rot=None, pairs=False, first=0, behind=0, seed=0, base=10000.0, scale=1.0, inplace=False):
+    dt, cdt = dts
+    starts = starts_of(seqs, first)
+    T = starts[-1] + behind
+    rot = dh if rot is None else rot
+    pages = sum(-(-(n + p) // page) for n, p in seqs) + 2
+    cache = random_cache(pages, kv, page, dh, cdt, seed + 10)
+    before = copy_of(cache)
+    table = table_for(seqs, page, pages, seed)
+    K, V, Q = padded(kv * dh, T, seed, dt, scale), padded(kv * dh, T, seed + 1, dt, scale), padded(heads * dh, T, seed + 2, dt, scale)
+    Q0 = Q.clone()
+    out = Q if inplace else torch.full((heads * dh, ld8(T)), 7.0, dtype=dt, device="cuda")
+    freq = (base ** (-torch.arange(rot // 2, device="cuda", dtype=F32) * 2 / max(rot, 1))) if rot else None
+    whole = len(seqs) == 1 and first == behind == 0
+    got = ctx.strp_cache_append(K, V, T, cache, table, ints([p for _, p in seqs]), None if whole else ints(starts), freq, pairs, Q, out)
+    assert got is out
+    token = torch.cat([torch.arange(a, e) for a, e in zip(starts, starts[1:])])
+    seq = torch.cat([torch.full((n,), i) for i, (n, _) in enumerate(seqs)])
+    pos = torch.cat([torch.arange(p, p + n) for n, p in seqs])
+    want, err = turned(Q0[:, token.cuda()], dh, pos.cuda(), freq, pairs)
+    # rounded to fp32, then to the type
+    step = lambda w: 2.0 ** -24 * w.abs() if dt != F32 else 0.0
+    close(out[:, token.cuda()], want, (err + step(want)) * (1 + H(dt)) + H(dt) * want.abs() + 1e-37, "Q")
+    outside = torch.ones(out.shape[1], dtype=torch.bool)
+    outside[token] = False
+    kept = Q0 if inplace else torch.full_like(out, 7.0)
+    assert torch.equal(out[:, outside.cuda()].nan_to_num(5.0), kept[:, outside.cuda()].nan_to_num(5.0))
+    # rows of the cache: [n, kv, dh]
+    slot = (table.cpu()[seq, pos // page].long(), pos % page)
+    at = (slot[0].cuda(), slice(None), slot[1].cuda())
+    untouched = torch.ones((pages, page), dtype=torch.bool)
+    untouched[slot] = False
+    un = untouched.cuda()[:, None, :].expand(pages, kv, page)
+    for name, x in (("K", K), ("V", V)):
+        w, e = turned(x[:, token.cuda()], dh, pos.cuda(), freq if name == "K" else None, pairs)
+        w, e = (y.reshape(kv, dh, -1).permute(2, 0, 1) for y in (w, e))
+        mine, old = getattr(cache, name), getattr(before, name)
+        assert torch.equal(mine[un].view(torch.uint8), old[un].view(torch.uint8)), name
+        if cdt != Q4:
+            close(mine[at], w, (e + (step(w) if name == "K" else 0.0)) * (1 + H(cdt)) + H(cdt) * w.abs() + 1e-37, name)
+            continue
+        sc, sc_old = getattr(cache, name + "_scale"), getattr(before, name + "_scale")
+        assert torch.equal(sc[un], sc_old[un])
+        n = torch.stack([mine[at] & 15, mine[at] >> 4], -1).flatten(-2).double()
+        lo, step4 = sc[at][..., :1].double(), sc[at][..., 1:].double()
+        f = w.float()
+        if name == "V":                # no rounding before it: the same numbers
+            l32 = f.amin(-1, keepdim=True)
+            s32 = (f.amax(-1, keepdim=True) - l32) / torch.full_like(l32, 15.0)          # by a number torch multiplies by its rounded inverse
+            assert torch.equal(lo.float(), l32) and torch.equal(step4.float(), s32)
+            assert torch.equal(n, torch.where(s32 > 0, torch.round((f - l32) / s32), 0.0).clamp(0, 15).double())
+        # the lowest and the step are those of x within its rounding to fp32, and the values half a step from x
+        mag = w.abs().amax(-1, keepdim=True)
+        close(lo, w.amin(-1, keepdim=True), U * mag + e.amax(-1, keepdim=True))
+        close(lo + 15 * step4, w.amax(-1, keepdim=True), 4 * U * mag + e.amax(-1, keepdim=True))
+        close(lo + n * step4, w, step4 * (0.5 + 16 * U) + 4 * U * mag)
+
+
+SEQS = [[(1, 0)], [(1, 511)], [(5, 30)], [(64, 0)], [(65, 15)], [(3, 1), (1, 100), (17, 16), (1, 0)], [(0, 7), (9, 3), (0, 0), (1, 31), (0, 2)], [(200, 33), (1, 4), (130, 0)]]
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("seqs", SEQS, ids=str)
+def test_append(ctx, seqs, dts):
+    append_case(ctx, seqs, 3, 2, 64, 16, dts)
+    append_case(ctx, seqs, 4, 4, 128, 32, dts, pairs=True, first=3, behind=6, seed=1)
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("dh", [8, 16, 24, 32, 40, 64, 72, 80, 96, 104, 128])
+def test_append_head_widths(ctx, dh, dts):
+    for rot, pairs in ((dh, False), (dh, True), (dh // 4 * 2, False), (2, True), (0, False), (dh // 8 * 2 + 2, False)):
+        append_case(ctx, [(70, 5), (2, 0)], 2, 1, dh, 16, dts, rot=rot, pairs=pairs, seed=3)
+        append_case(ctx, [(3, 60)], 5, 3, dh, 64, dts, rot=rot, pairs=pairs, seed=4)
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+def test_append_far_positions_and_in_place(ctx, dts):
+    append_case(ctx, [(2, 999_998), (66, 70_001)], 2, 2, 32, 4096, dts, seed=5, inplace=True)
+    append_case(ctx, [(2, 999_998)], 2, 2, 32, 4096, dts, seed=6, base=0.5, pairs=True, inplace=True)      # frequencies above one
+
+
+def test_append_without_queries(ctx):
+    cache, before = random_cache(4, 2, 16, 64, BF16, 1), random_cache(4, 2, 16, 64, BF16, 1)
+    K, V = rand((128, 8), 2, BF16), rand((128, 8), 3, BF16)
+    assert ctx.strp_cache_append(K, V, 3, cache, ints([[2, 1]]), ints([15])) is None
+    for mine, old, x in ((cache.K, before.K, K), (cache.V, before.V, V)):
+        for t, (page, row) in enumerate([(2, 15), (1, 0), (1, 1)]):
+            assert torch.equal(mine[page, :, row], x[:, t].reshape(2, 64))
+            old[page, :, row] = mine[page, :, row]
+        assert torch.equal(mine, old)
+
+
+def test_append_of_many_sequences(ctx):
+    seqs = [(1, i % 50) for i in range(1500)]
+    append_case(ctx, seqs, 2, 1, 16, 16, (BF16, BF16), seed=7)
+    append_case(ctx, [(i % 3, i % 20) for i in range(1030)], 2, 1, 16, 16, (F32, Q4), seed=8)
+
+
+def test_append_of_what_is_not_finite(ctx):
+    """bf16: as it is.  4 bits: a head of a token with such a value stands for none that is finite, the others as ever."""
+    x = rand((128, 8), 1, BF16)
+    x[3, 0], x[70, 1], x[9, 2], x[64 + 5, 2] = float("nan"), float("inf"), -float("inf"), 3.0e38
+    x[64 + 6, 2] = -3.0e38                                        # a range that fp32 does not hold
+    cache = random_cache(1, 2, 16, 64, BF16, 1)
+    ctx.strp_cache_append(x, x, 4, cache, ints([[0]]), ints([0]))
+    assert torch.equal(cache.K[0, :, :4].permute(0, 2, 1).reshape(128, 4).nan_to_num(5.0), x[:, :4].nan_to_num(5.0))
+    cache = random_cache(1, 2, 16, 64, Q4, 1)
+    ctx.strp_cache_append(x, x, 4, cache, ints([[0]]), ints([0]))
+    for v in values(cache):
+        finite = torch.isfinite(v[0, :, :4])
+        assert torch.equal(finite.all(-1).cpu(), torch.tensor([[False, True, False, True], [True, False, False, True]]))
+        assert not finite[0, 0].any() and not finite[1, 2].any()
+
+
+def test_append_of_constant_and_tiny_heads(ctx):
+    x = torch.zeros((64, 8), dtype=F32, device="cuda")
+    x[:, 1], x[:, 2] = 3.25, 1e-44
+    x[5, 2] = 0.0
+    x[:32, 3] = -1.0
+    cache = random_cache(1, 1, 16, 64, Q4, 1)
+    ctx.strp_cache_append(x, x, 4, cache, ints([[0]]), ints([0]))
+    for v in values(cache):
+        assert (v[0, 0, 0] == 0).all() and (v[0, 0, 1] == 3.25).all() and (v[0, 0, 2] - x[:, 2].double()).abs().max() <= 1.5e-45 * 8
+        assert (v[0, 0, 3].sort().values[:32] == -1).all() and (v[0, 0, 3].sort().values[32:].abs() <= 2.0 ** -23).all()
+
+
+def test_append_wrong_places_are_not_written(ctx):
+    for dt in (BF16, Q4):
+        cache = random_cache(8, 2, 16, 64, dt, 1)
+        before = copy_of(cache)
+        K = rand((128, 48), 2, BF16)
+        ctx.strp_cache_append(K, K, 48, cache, ints([[-1, 8], [1 << 30, -5], [0, 1], [0, 1]]), ints([0, 3, 32, -1]), ints([0, 20, 30, 40, 48]))
+        ctx.strp_cache_append(K, K, 9, cache, ints([[3]]), ints([0]), ints([9, 9]))
+        ctx.strp_cache_append(K, K, 9, cache, ints([[3]]), ints([0]), ints([5, 2]))
+        for a, b in zip((cache.K, cache.V, cache.K_scale, cache.V_scale), (before.K, before.V, before.K_scale, before.V_scale)):
+            assert a is None or torch.equal(a, b)
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------
+def attention_reference(Q, cache, table, seqs, starts, heads, kv_of, scale, split=True):
+    """result and bound, [heads*dh x T], zero outside the sequences"""
+    dt, dh, page = Q.dtype, cache.d_head, cache.page
+    K, V = values(cache)
+    q4 = cache.K.dtype == Q4
+    out = torch.zeros((heads * dh, Q.shape[1]), dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(out)
+    for i, (n, past) in enumerate(seqs):
+        if n == 0:
+            continue
+        keys, a, e = past + n, starts[i], starts[i + 1]
+        pages = table[i, :-(-keys // page)].long()
+        seen = torch.ones((n, keys), dtype=torch.bool, device="cuda").tril(past)
+        for h in range(heads):
+            r = slice(h * dh, (h + 1) * dh)
+            k, v = (x[pages, kv_of[h]].reshape(-1, dh)[:keys] for x in (K, V))
+            q = Q[r, a:e].double()
+            s = torch.where(seen, scale * (q.t() @ k.t()), -math.inf)
+            p = torch.softmax(s, 1)
+            o = (p @ v).t()
+            ka, va = k.abs(), v.abs()
+            if q4:
+                # whole numbers enter as 128 + n with 128 sum(q) taken off, and lowest is added behind: their magnitudes are what is summed
+                sk, sv = (x[pages, kv_of[h]].reshape(-1, 2)[:keys].double() for x in (cache.K_scale, cache.V_scale))
+                ka, va = (sc[:, :1].abs() + 271 * sc[:, 1:].abs() + 0 * x for sc, x in ((sk, ka), (sv, va)))
+            # a score is off by dh + 4 steps of its magnitudes (4 bits: 4 more), its probability by twice the largest of these of its row (the maximum's and its
+            # own), relative; the sums have a term more for each key, each doubling of a part's factor and each wavefront or workgroup that is joined: fewer than keys + 64
+            mag = torch.where(seen, scale * (q.abs().t() @ ka.t()), 0.0).max(1).values
+            rel = 2 * (dh + 8) * U * mag + (keys + 64) * U
+            tol[r, a:e] = 2 * (rel * (p @ va).t())
+            if dt == BF16:
+                # two terms of bf16, or one, which numerator and sum share only where V is not of 4 bits
+                tol[r, a:e] += (2.0 ** -16 if split else 2 * H(BF16)) * (p @ v.abs()).t()
+                if q4 and not split:
+                    tol[r, a:e] += 2 * H(BF16) * (p @ (16 * sv[:, 1:].abs() + sv[:, :1].abs() + 0 * v)).t()
+            tol[r, a:e] += H(dt) * o.abs() + 1e-37
+            out[r, a:e] = o
+    return out, tol
+
+
+def attention_case(ctx, seqs, heads, kv, dh, page, dts, first=0, behind=0, kv_of=None, scale=None, seed=0, spread=1.5, split=True, extra=2, fix=None):
+    dt, cdt = dts
+    starts = starts_of(seqs, first)
+    T = starts[-1] + behind
+    pages = sum(-(-(n + p) // page) for n, p in seqs) + extra
+    cache = random_cache(pages, kv, page, dh, cdt, seed + 10, bad=True)
+    good = random_cache(pages, kv, page, dh, cdt, seed + 10)
+    table = table_for(seqs, page, pages, seed)
+    # only what a sequence holds is finite: rows behind it, other pages and the columns of no token are not
+    for i, (n, past) in enumerate(seqs):
+        for j in range(-(-(n + past) // page) if n else 0):
+            rows = min(page, n + past - j * page)
+            g = int(table[i, j])
+            for a, b in zip((cache.K, cache.V, cache.K_scale, cache.V_scale), (good.K, good.V, good.K_scale, good.V_scale)):
+                if a is not None:
+                    a[g, :, :rows] = b[g, :, :rows]
+    if fix:
+        fix(cache, table)
+    Q = padded(heads * dh, T, seed, dt, spread)
+    Q[:, :first] = float("nan")
+    Q[:, starts[-1]:] = float("inf")
+    C = torch.full((heads * dh, ld8(T)), 7.0, dtype=dt, device="cuda")
+    whole = first == behind == 0 and len(seqs) == 1 and seed % 2
+    ctx.strp_cache_attention(Q, T, heads, cache, table, ints([p for _, p in seqs]), None if whole else ints(starts), ints(kv_of) if kv_of else None, scale, out=C)
+    want, tol = attention_reference(Q[:, :T], cache, table, seqs, starts, heads, kv_of or [h // (heads // kv) for h in range(heads)], scale or dh ** -0.5, split)
+    inside = slice(first, starts[-1])
+    close(C[:, inside], want[:, inside], tol[:, inside], (seqs, heads, kv, dh, page, dts))
+    assert (C[:, :first] == 7.0).all() and (C[:, starts[-1]:] == 7.0).all()
+    return C
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("seqs", [[(1, 0)], [(1, 15)], [(1, 31)], [(1, 32)], [(1, 127)], [(1, 128)], [(1, 1000)], [(1, 5000)], [(2, 0)], [(5, 14)], [(17, 100)], [(40, 0)],
+                                  [(1, 0), (1, 1), (1, 300), (1, 63)], [(0, 4), (3, 60), (0, 0), (1, 513), (20, 9), (0, 1)], [(1, i * 37 % 400) for i in range(70)]],
+                         ids=lambda s: str(s) if len(s) < 9 else "70")
+def test_attention(ctx, seqs, dts):
+    attention_case(ctx, seqs, 4, 4, 64, 16, dts)
+    attention_case(ctx, seqs, 8, 2, 128, 32, dts, first=3, behind=6, seed=1)
+    attention_case(ctx, seqs[:6], 3, 1, 80, 128, dts, seed=3)
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("dh", [8, 16, 24, 32, 40, 48, 56, 64, 72, 80, 96, 104, 120, 128])
+def test_attention_head_widths(ctx, dh, dts):
+    attention_case(ctx, [(1, 200), (6, 30)], 4, 2, dh, 16, dts)
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("heads,kv,kv_of", [(8, 1, None), (6, 3, None), (5, 5, None), (40, 1, None), (7, 3, [0, 0, 0, 1, 2, 2, 2]), (3, 4, [3, 0, 3]), (20, 3, [2] * 18 + [0, 2])])
+def test_attention_heads_in_groups(ctx, heads, kv, kv_of, dts):
+    attention_case(ctx, [(1, 70), (5, 3), (1, 0), (9, 200)], heads, kv, 32, 16, dts, kv_of=kv_of)
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+def test_attention_long(ctx, dts):
+    """Several workgroups share a sequence; one sequence and many beside it."""
+    attention_case(ctx, [(1, 40000)], 4, 1, 64, 64, dts)
+    attention_case(ctx, [(1, 20), (1, 30000), (2, 7), (1, 999)], 4, 2, 128, 256, dts, seed=2)
+    attention_case(ctx, [(7, 9000)], 8, 8, 128, 1024, dts, seed=3)
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+def test_attention_of_chunks(ctx, dts):
+    attention_case(ctx, [(300, 500)], 4, 2, 64, 16, dts)
+    attention_case(ctx, [(150, 0), (1, 400), (129, 77), (2, 2), (64, 64)], 4, 1, 128, 64, dts, first=5, seed=1)
+
+
+def test_attention_scales_and_peaked_scores(ctx):
+    for dts in CASES:
+        attention_case(ctx, [(1, 300), (3, 90)], 4, 2, 64, 16, dts, scale=1e-6)
+        attention_case(ctx, [(1, 300), (3, 90)], 4, 2, 64, 16, dts, scale=2.0, spread=0.5, seed=2)
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+def test_attention_with_rounded_probabilities(fast, dh):
+    for cdt in (BF16, Q4):
+        attention_case(fast, [(1, 300), (3, 90), (1, 3000), (200, 20)], 4, 2, dh, 16, (BF16, cdt), split=False)
+
+
+@pytest.mark.parametrize("dts", CASES[:2], ids=IDS[:2])
+@pytest.mark.parametrize("n", [1, 4, 100, 200])
+def test_values_that_are_not_finite_show_where_they_are_seen(ctx, dts, n):
+    """A value of infinity that later tokens of a tile see and earlier ones do not: theirs alone; one that all see: in all."""
+    past, heads, dh = 200, 2, 64
+    for at in (past + n - 1, past + n // 2, 3):
+        def plant(cache, table):
+            cache.V[int(table[0, at // 16]), 0, at % 16, 5] = float("inf")
+        cache = random_cache(60, 1, 16, dh, dts[1], 1)
+        table = table_for([(n, past)], 16, 60, 1)
+        plain = copy_of(cache)
+        Q = rand((heads * dh, ld8(n)), 3, dts[0])
+        want = ctx.strp_cache_attention(Q, n, heads, plain, table, ints([past]))[:, :n]
+        plant(cache, table)
+        got = ctx.strp_cache_attention(Q, n, heads, cache, table, ints([past]))[:, :n]
+        assert torch.isfinite(want).all()
+        sees = torch.arange(past, past + n, device="cuda") >= at
+        for h in range(heads):
+            assert (got[h * dh + 5] == float("inf")).tolist() == sees.tolist(), at
+            rest = torch.arange(dh, device="cuda") != 5
+            assert torch.equal(got[h * dh:(h + 1) * dh][rest], want[h * dh:(h + 1) * dh][rest]), at
+        assert torch.equal(got[:, ~sees], want[:, ~sees])
+
+
+def test_attention_lowest_values(ctx):
+    """Scores of the lowest finite value, and keys of minus infinity: softmax as ever."""
+    cache = random_cache(4, 1, 16, 64, F32, 1)
+    cache.K.zero_()
+    cache.K[0, 0, 3, 0] = -math.inf
+    cache.K[0, 0, 4, 0] = -3.0e38
+    Q = torch.zeros((64, 8), dtype=F32, device="cuda")
+    Q[0, 0] = 1.0
+    got = ctx.strp_cache_attention(Q, 1, 1, cache, ints([[0]]), ints([9]))[:, 0]
+    keep = [0, 1, 2, 5, 6, 7, 8, 9]
+    close(got, cache.V[0, 0, keep].double().mean(0), 64 * U * cache.V[0, 0, :10].abs().double().mean(0) + 1e-37)
+    cache.K[0, 0, :10, 0] = -math.inf
+    assert ctx.strp_cache_attention(Q, 1, 1, cache, ints([[0]]), ints([9]))[:, 0].isnan().all()
+
+
+def test_attention_beyond_32_bit_offsets(ctx):
+    """A pool of more than 2^32 bytes, pages at its far end."""
+    pages, kv, page, dh = 20000, 8, 128, 128
+    K = torch.zeros((pages, kv, page, dh), dtype=BF16, device="cuda")
+    cache = strp.PagedCache(K, K)
+    small = random_cache(3, kv, page, dh, BF16, 1)
+    ids = [pages - 1, pages - 2, 17]
+    K[ids] = small.K
+    Q = rand((kv * dh, 8), 2, BF16)
+    got = ctx.strp_cache_attention(Q, 1, kv, cache, ints([ids]), ints([300]))
+    want = ctx.strp_cache_attention(Q, 1, kv, strp.PagedCache(small.K, small.K), ints([[0, 1, 2]]), ints([300]))
+    assert torch.equal(got[:, 0], want[:, 0])
+    x = rand((kv * dh, 8), 3, BF16)
+    ctx.strp_cache_append(x, x, 2, cache, ints([ids]), ints([127]))
+    assert torch.equal(K[ids[0], :, 127].reshape(-1), x[:, 0]) and torch.equal(K[ids[1], :, 0].reshape(-1), x[:, 1])
+
+
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+def test_attention_wrong_tables_stay_in_bounds(ctx, dts):
+    cache = random_cache(4, 2, 16, 64, dts[1], 1)
+    Q = rand((256, 40), 2, dts[0])
+    for table, past, starts in (([[-1, 99]], [20], [0, 40]), ([[0, 1], [2, 3]], [1 << 30, -7], [0, 3, 5]), ([[0, 1], [2, 3]], [5, 5], [0, 50, 20]),
+                                ([[0, 1], [2, 3]], [5, 5], [-9, 4, 1 << 30]), ([[0]], [15], [7, 7]), ([[0], [1]], [0, 0], [30, 10, 35])):
+        C = torch.full((256, 40), 7.0, dtype=dts[0], device="cuda")
+        ctx.strp_cache_attention(Q, 40, 4, cache, ints(table), ints(past), ints(starts), out=C)
+        if starts == [7, 7]:
+            assert (C == 7.0).all()
+    C = ctx.strp_cache_attention(Q, 40, 4, cache, ints([[0, 1, 2, 3]]), ints([24]), kv_of_head=ints([5, -1, 0, 1]))
+    want = ctx.strp_cache_attention(Q, 40, 4, cache, ints([[0, 1, 2, 3]]), ints([24]), kv_of_head=ints([1, 0, 0, 1]))
+    assert torch.equal(C, want) and torch.isfinite(C).all()
+
+
+def test_attention_repeats_its_bits_and_replays(ctx):
+    """A step of generation, append and attention, captured and replayed with eager work between: positions that the caller raises on the device."""
+    for dts in CASES:
+        dt, cdt = dts
+        heads, kv, dh, page, n_seq = 8, 2, 64, 16, 5
+        cache = random_cache(n_seq * 20, kv, page, dh, cdt, 1)
+        table = torch.randperm(n_seq * 20, generator=torch.Generator().manual_seed(2)).to(torch.int32).reshape(n_seq, 20).cuda()
+        freq = 1e4 ** (-torch.arange(dh // 2, device="cuda", dtype=F32) * 2 / dh)
+        starts = ints(list(range(n_seq + 1)))
+        past = ints([3, 100, 17, 250, 0])
+        K, V, Q = (rand((r * dh, 8), 3 + i, dt) for i, r in enumerate((kv, kv, heads)))
+        q = torch.empty_like(Q)
+        C = torch.zeros_like(Q)
+        c = strp.Context(0)
+
+        def step(to):
+            c.strp_cache_append(K, V, n_seq, cache, table, past, starts, freq, False, Q, q)
+            return c.strp_cache_attention(q, n_seq, heads, cache, table, past, starts, out=to)
+
+        again = step(torch.zeros_like(Q)).clone()
+        assert torch.equal(step(torch.zeros_like(Q)), again)
+        stream = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            c = strp.Context(0)
+            step(C)
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                step(C)
+        first = copy_of(cache)
+        results = []
+        for i in range(4):
+            graph.replay()
+            torch.cuda.synchronize()
+            results.append(C.clone())
+            past += 1
+            for x in (K, V, Q):
+                x += 0.25
+            torch.cuda.synchronize()
+        # the same eagerly, from the same cache
+        for x in (K, V, Q):
+            x -= 1.0
+        past -= 4
+        for t, s in zip((cache.K, cache.V, cache.K_scale, cache.V_scale), (first.K, first.V, first.K_scale, first.V_scale)):
+            if t is not None:
+                t.copy_(s)
+        c = ctx
+        if dt == F32:
+            # what was added and taken off may have rounded
+            for i, x in enumerate((K, V, Q)):
+                x.copy_(rand(x.shape, 3 + i, dt))
+        else:
+            for i, x in enumerate((K, V, Q)):
+                x.copy_(rand(x.shape, 3 + i, dt))
+        for i in range(4):
+            assert torch.equal(step(torch.zeros_like(Q))[:, :n_seq], results[i][:, :n_seq]), (dts, i)
+            past += 1
+            for x in (K, V, Q):
+                x += 0.25
+        torch.cuda.synchronize()
+
+
+def test_calls_run_on_the_context_s_stream_whatever_stream_is_current(ctx):
+    cache = random_cache(8, 2, 16, 64, BF16, 1)
+    K, Q = rand((128, 8), 2, BF16), rand((256, 8), 3, BF16)
+    table, past = ints([[0, 1, 2, 3]]), ints([40])
+    ctx.strp_cache_append(K, K, 4, cache, table, past)
+    want = ctx.strp_cache_attention(Q, 4, 4, cache, table, past)[:, :4].clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = ctx.strp_cache_attention(Q, 4, 4, cache, table, past)
+    torch.cuda.synchronize()
+    assert torch.equal(got[:, :4], want)
+
+
+def test_generation_agrees_with_whole_prompts(ctx):
+    """A prompt appended and attended in pieces (a chunk, then tokens one by one) gives what strp_attention gives for the whole, within both bounds."""
+    heads, kv, dh, T = 6, 2, 64, 150
+    for dt in (BF16, F32):
+        Q, K, V = (rand((r * dh, ld8(T)), 5 + i, dt) for i, r in enumerate((heads, kv, kv)))
+        whole = ctx.strp_attention(Q, K, V, T, heads, kv)[:, :T]
+        cache = random_cache(12, kv, 16, dh, dt, 1)
+        table = ints([list(range(11, 0, -1))])
+        got = torch.empty_like(whole)
+        at = 0
+        for n in [100] + [1] * 20 + [7, 23]:
+            past = ints([at])
+            pieces = []
+            for x in (K, V, Q):
+                piece = torch.zeros((x.shape[0], ld8(n)), dtype=dt, device="cuda")
+                piece[:, :n] = x[:, at:at + n]
+                pieces.append(piece)
+            ctx.strp_cache_append(pieces[0], pieces[1], n, cache, table, past)
+            got[:, at:at + n] = ctx.strp_cache_attention(pieces[2], n, heads, cache, table, past)[:, :n]
+            at += n
+        assert at == T
+        want, tol = attention_reference(Q[:, :T], cache, table, [(T, 0)], [0, T], heads, [h // 3 for h in range(heads)], dh ** -0.5)
+        close(got, want, tol)
+        close(whole, want, tol)
+
+
+def test_binding_refusals(ctx):
+    cache = random_cache(4, 2, 16, 64, BF16, 1)
+    K, Q, table, past = rand((128, 8), 1, BF16), rand((256, 8), 2, BF16), ints([[0, 1]]), ints([3])
+    for err, call in ((ValueError, lambda: strp.PagedCache(cache.K, cache.V[:1])),
+                      (ValueError, lambda: strp.PagedCache(cache.K, cache.V.float())),
+                      (ValueError, lambda: strp.PagedCache(cache.K.half(), cache.V.half())),
+                      (ValueError, lambda: strp.PagedCache(cache.K, cache.V, rand((4, 2, 16, 2), 1), rand((4, 2, 16, 2), 1))),
+                      (ValueError, lambda: strp.PagedCache(cache.K.view(torch.uint8), cache.V.view(torch.uint8))),
+                      (ValueError, lambda: strp.PagedCache(cache.K.transpose(1, 2), cache.V.transpose(1, 2))),
+                      (ValueError, lambda: ctx.strp_cache_append(K[:64], K, 4, cache, table, past)),
+                      (TypeError, lambda: ctx.strp_cache_append(K, K.float(), 4, cache, table, past)),
+                      (ValueError, lambda: ctx.strp_cache_append(K, K, 9, cache, table, past)),
+                      (ValueError, lambda: ctx.strp_cache_append(K, K, 4, cache, table.cpu(), past)),
+                      (ValueError, lambda: ctx.strp_cache_append(K, K, 4, cache, table.long(), past)),
+                      (TypeError, lambda: ctx.strp_cache_append(K, K, 4, cache, table, past.float())),
+                      (ValueError, lambda: ctx.strp_cache_append(K, K, 4, cache, ints([[0], [1]]), past)),
+                      (ValueError, lambda: ctx.strp_cache_append(K, K, 4, cache, table, past, ints([0]))),
+                      (TypeError, lambda: ctx.strp_cache_append(K, K, 4, cache, table, past, inv_freq=past)),
+                      (ValueError, lambda: ctx.strp_cache_append(K, K, 4, cache, table, past, Q=Q[:100])),
+                      (strp.StrpError, lambda: ctx.strp_cache_append(K.float(), K.float(), 4, cache, table, past)),
+                      (strp.StrpError, lambda: ctx.strp_cache_append(K, K, 4, cache, table, past, inv_freq=rand((33,), 1))),
+                      (strp.StrpError, lambda: ctx.strp_cache_append(K, K, 0, cache, table, past)),
+                      (ValueError, lambda: ctx.strp_cache_attention(Q, 4, 3, cache, table, past)),
+                      (strp.StrpError, lambda: ctx.strp_cache_attention(rand((192, 8), 1, BF16), 4, 3, cache, table, past)),
+                      (strp.StrpError, lambda: ctx.strp_cache_attention(Q.float(), 4, 4, cache, table, past)),
+                      (strp.StrpError, lambda: ctx.strp_cache_attention(Q, 4, 4, cache, table, past, scale=-1.0)),
+                      (ValueError, lambda: ctx.strp_cache_attention(Q, 4, 4, cache, table, past, kv_of_head=ints([0, 1]))),
+                      (ValueError, lambda: ctx.strp_cache_attention(Q, 4, 4, cache, table, past, out=torch.empty((256, 8), device="cpu", dtype=BF16)))):
+        with pytest.raises(err):
+            call()

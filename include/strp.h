@@ -452,6 +452,42 @@ strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* i
 /* Workspace (bytes, device) that strp_cache_attention needs for any call with this d_head; pure function. */
 size_t strp_cache_attention_workspace_bytes(int32_t d_head);
 
+/*
+ * strp_verify_draft -- which of a draft's tokens a target model keeps, and the token that follows them, so that what comes out is
+ * distributed as the target's own tokens are (a pruned model drafts, the dense one verifies); without drafted tokens it samples one.
+ *   target [V x ldt], draft [V x ldd] logits of dtype, one row per vocabulary entry.  Sequence i has the drafted tokens draft_start[i] to
+ *   draft_start[i + 1] (n_seq + 1 ascending offsets from 0 to T; NULL: one sequence of all T, or T = 0): their distributions are the columns of
+ *   `draft` and their ids draft_id [T]; the target's at the same positions, and the one behind the last, are columns draft_start[i] + i and on of `target`
+ *   (T + n_seq columns).  T = 0: draft, draft_id and u may be NULL.
+ * With p = softmax(target / temperature) and q = softmax(draft / temperature) at the position of token x:  x is kept where u q(x) < p(x) and
+ * all before it were (an id outside [0, V) is not).  accepted[i] = how many;  next_id[i] = the lowest v with
+ *   sum_{w <= v} r(w) > u_next[i] sum_w r(w),  r = max(p - q, 0) at the first token that is not kept (p, where that is zero
+ *   everywhere), p behind the last one where all are;  u [T], u_next [n_seq] fp32 in [0, 1) are the caller's random numbers.
+ *   From u_next = 1 on: the last v with r(v) > 0.  A position where a distribution that is needed has a NaN, +inf or nothing but -inf ends
+ *   the sequence there, with next_id -1.
+ * All of it is worked out in 64 bits, where 32 would put a token beside its place now and then.  Wrong entries of draft_start give wrong results,
+ * no access out of bounds.
+ * Errors: STRP_EINVAL (null target, u_next, accepted or next_id, T > 0 without draft, draft_id and u, or without
+ * draft_start where n_seq > 1, V or n_seq not positive, V above 2^30, T above
+ * 2^20, n_seq above 65536, temperature outside [1e-30, 1e30], bad ld, misaligned, unknown dtype), STRP_ENOMEM (strp_verify_draft_workspace_bytes).
+ */
+typedef struct {
+  const void* target;
+  const void* draft;
+  const int32_t* draft_id;
+  const float* u;
+  const float* u_next;
+  const int32_t* draft_start;
+  int32_t* accepted;
+  int32_t* next_id;
+  int32_t dtype, V, n_seq;
+  double temperature;
+  int64_t T, ldt, ldd;
+} strp_verify_draft_in;
+strp_status strp_verify_draft(strp_ctx* ctx, const strp_verify_draft_in* in);
+/* Workspace (bytes, device) that strp_verify_draft needs; pure function. */
+size_t strp_verify_draft_workspace_bytes(int32_t V, int64_t T, int32_t n_seq);
+
 /* ---- stateful per-module path ---------------------------------------------------------- */
 typedef struct {
   const void* X;       /* [d x ldx]   x_dtype                                               */

@@ -14,7 +14,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libstrp.so")
 SOURCES = ["gemm_mfma.hip", "gemm_dma.hip", "split_planes.hip", "dense_f64.hip", "chol_flow.hip", "score_select.hip", "strp_api.hip",
            "layer/linear.hip", "layer/linear_bf16.hip", "layer/layer_norm.hip", "layer/attention.hip", "layer/token_logprobs.hip",
-           "layer/cache_append.hip", "layer/cache_rows.hip"]
+           "layer/cache_append.hip", "layer/cache_rows.hip", "layer/verify_draft.hip"]
 BENCH_LIB = os.path.join(HERE, "libstrp_bench.so")
 BENCH_SOURCES = ["bench_probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -33,6 +33,7 @@ EXPORTS = [
     "strp_refit", "strp_module_init", "strp_admm_step",
     "strp_linear", "strp_linear_workspace_bytes", "strp_layer_norm", "strp_attention", "strp_token_logprobs", "strp_token_logprobs_workspace_bytes",
     "strp_cache_append", "strp_cache_attention", "strp_cache_attention_workspace_bytes",
+    "strp_verify_draft", "strp_verify_draft_workspace_bytes",
 ]
 
 
@@ -106,10 +107,18 @@ class CacheAttentionIn(C.Structure):
                 ("scale", C.c_float), ("T", C.c_int64), ("ldq", C.c_int64), ("ldc", C.c_int64)]
 
 
+class VerifyDraftIn(C.Structure):
+    _fields_ = [("target", C.c_void_p), ("draft", C.c_void_p), ("draft_id", C.c_void_p), ("u", C.c_void_p), ("u_next", C.c_void_p),
+                ("draft_start", C.c_void_p), ("accepted", C.c_void_p), ("next_id", C.c_void_p), ("dtype", C.c_int32), ("V", C.c_int32),
+                ("n_seq", C.c_int32), ("temperature", C.c_double), ("T", C.c_int64), ("ldt", C.c_int64), ("ldd", C.c_int64)]
+
+
 # Their bytes from the fields in order: a call's cost on the host is the marshalling, and packing in one go is the cheaper form of it.
 _LINEAR, _ATTENTION = struct.Struct("@5P6i5q"), struct.Struct("@6P5if5q")
 assert _LINEAR.size == C.sizeof(LinearIn) and _ATTENTION.size == C.sizeof(AttentionIn)
 _CACHE_APPEND, _CACHE_ATTENTION = struct.Struct("@7P7i4x5P4i5q"), struct.Struct("@7P7i4x3P2if4x3q")
+_VERIFY_DRAFT = struct.Struct("@8P3i4xd3q")
+assert _VERIFY_DRAFT.size == C.sizeof(VerifyDraftIn)
 assert _CACHE_APPEND.size == C.sizeof(CacheAppendIn) and _CACHE_ATTENTION.size == C.sizeof(CacheAttentionIn)
 
 _packers = {}
@@ -181,6 +190,9 @@ def load_library():
     lib.strp_cache_attention.argtypes = [vp, vp]
     lib.strp_cache_attention_workspace_bytes.argtypes = [i32]
     lib.strp_cache_attention_workspace_bytes.restype = C.c_size_t
+    lib.strp_verify_draft.argtypes = [vp, vp]
+    lib.strp_verify_draft_workspace_bytes.argtypes = [i32, i64, i32]
+    lib.strp_verify_draft_workspace_bytes.restype = C.c_size_t
     lib.strp_linear_workspace_bytes.argtypes = [i32, i32, i64, C.c_int, C.c_int]
     lib.strp_linear_workspace_bytes.restype = C.c_size_t
     lib.strp_token_logprobs_workspace_bytes.argtypes = [i32, i64, i32]
@@ -538,6 +550,29 @@ class Context:
             *self._pages(cache, table, past, seq_start, T), Q.data_ptr(), out.data_ptr(), self._vector("kv_of_head", kv_of_head, heads, torch.int32),
             _CODES[Q.dtype], heads, dh ** -0.5 if scale is None else scale, T, ldq, ldc)))
         return out
+
+    def strp_verify_draft(self, target, draft, draft_ids, u, u_next, seq_start=None, temperature=1.0):
+        """Which drafted tokens the target keeps, and the token that follows: dict of accepted and next_ids [n_seq] int32.  target [V x ld] logits at every
+        drafted position and behind the last one of each sequence, draft [V x ld] at the drafted positions, draft_ids [T] int32, u [T] and u_next
+        [n_seq] fp32 random numbers in [0, 1), seq_start [n_seq + 1] int32 (None: one sequence).  draft, draft_ids and u None: one token of
+        each sequence is sampled from the target."""
+        n_seq = u_next.shape[0]
+        T = 0 if draft is None else draft_ids.shape[0]
+        V = target.shape[0]
+        ldt = self._matrix("target", target, V, T + n_seq, _CODES)
+        d = ids = uu = ldd = 0
+        if T:
+            ldd = self._matrix("draft", draft, V, T, (target.dtype,))
+            d, ids, uu = draft.data_ptr(), self._vector("draft_ids", draft_ids, T, torch.int32), self._vector("u", u, T, torch.float32)
+        elif draft_ids is not None and draft_ids.shape[0]:
+            raise ValueError("draft_ids without draft")
+        starts = self._vector("seq_start", seq_start, n_seq + 1, torch.int32)
+        res = self._empty((2, n_seq), torch.int32)
+        self.ensure_workspace(self.lib.strp_verify_draft_workspace_bytes(V, T, n_seq))
+        self.check(self.lib.strp_verify_draft(self.h, _VERIFY_DRAFT.pack(
+            target.data_ptr(), d, ids, uu, self._vector("u_next", u_next, n_seq, torch.float32), starts, res.data_ptr(), res.data_ptr() + 4 * n_seq,
+            _CODES[target.dtype], V, n_seq, float(temperature), T, ldt, ldd)))
+        return dict(accepted=res[0], next_ids=res[1])
 
     def strp_module_init(self, desc, state, params):
         self.check(self.lib.strp_module_init(self.h, C.byref(desc), C.byref(state), C.byref(params)))

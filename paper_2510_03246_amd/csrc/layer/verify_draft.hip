@@ -325,7 +325,8 @@ extern "C" {
 
 size_t strp_verify_draft_workspace_bytes(int32_t V, int64_t T, int32_t n_seq) {
   if (V <= 0 || V > (1 << 30) || T < 0 || T > (1 << 20) || n_seq <= 0 || n_seq > 65536) return 0;
-  return 256 + up256((size_t)(2 * T + n_seq) * SLICES * sizeof(Mass)) + up256((size_t)n_seq * sizeof(Chosen)) + up256((size_t)n_seq * PARTS * 16);
+  // (a workspace has 4 KB at least)
+  return 4096 + up256((size_t)(2 * T + n_seq) * SLICES * sizeof(Mass)) + up256((size_t)n_seq * sizeof(Chosen)) + up256((size_t)n_seq * PARTS * 16);
 }
 
 strp_status strp_verify_draft(strp_ctx* ctx, const strp_verify_draft_in* in) {

@@ -4,34 +4,46 @@
 // with p and q the softmax of two columns of logits [V x tokens].  What is asked is an index into 10^5 sums, of which some lie within 10^-7 of each other:
 // 32 bits would answer beside it once in a few hundred times, so exponentials and sums are of 64.
 //
-// Three kernels: sums of exponentials of slices of every column; the sequences' first token that is not kept and the sums of r over
-// parts of the vocabulary; the part that holds the answer, entry by entry.
+// Four kernels: sums of exponentials over slices of every column (all that is read once, and most of the time); the first token of every sequence that is not kept;
+// the sums of r over parts of the vocabulary; the part that holds the answer, entry by entry.
 #include "layer_ops.h"
+
+#include <type_traits>
 
 namespace strp {
 
-constexpr int SLICES = 64, PARTS = 64;     // at most: a wavefront has one of each a lane
+constexpr int SLICES = 256, PARTS = 64;    // at most: a lane has four of the slices of a column, one of the parts
 
-// e^y in 64 bits for y <= 600, 0 where y is below -745 (NaN: 0 too): 2^k e^r with |r| <= ln 2 / 2, the series to r^12 (the next term is below 2e-16)
-__device__ __forceinline__ double exp64(double y) {
-  y = fmax(y, -800.0);
-  const double k = __builtin_rint(y * 1.4426950408889634074);
-  double r = __builtin_fma(-k, 6.93147180369123816490e-01, y);      // ln 2 in two parts, the first of 32 bits: its product with k is exact
-  r = __builtin_fma(-k, 1.90821492927058770002e-10, r);
-  double p = 1.0 / 479001600.0;
-  p = __builtin_fma(p, r, 1.0 / 39916800.0);
-  p = __builtin_fma(p, r, 1.0 / 3628800.0);
-  p = __builtin_fma(p, r, 1.0 / 362880.0);
-  p = __builtin_fma(p, r, 1.0 / 40320.0);
-  p = __builtin_fma(p, r, 1.0 / 5040.0);
-  p = __builtin_fma(p, r, 1.0 / 720.0);
-  p = __builtin_fma(p, r, 1.0 / 120.0);
-  p = __builtin_fma(p, r, 1.0 / 24.0);
-  p = __builtin_fma(p, r, 1.0 / 6.0);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
-  p = __builtin_fma(p, r, 1.0);
-  return __builtin_ldexp(p, (int)k);
+// e^y to a few units of 2^-52 for y <= 600, 0 where y is below -700 (NaN: 0 too).  y = (32 k + j) ln 2 / 32 + r with |r| <= ln 2 / 64, so that e^y = 2^k 2^(j/32) e^r: a table of 32 in LDS,
+// which 64 banks give to any lanes at once, and the series to r^5 (the next term is below 2^-48.6 of the whole).  14 instructions in 64 bits; without the table and to r^12 it is 24.
+struct Exp {
+  const double* table;
+  __device__ __forceinline__ double operator()(double y) const {
+    constexpr double ROUND = 6755399441055744.0;                    // 1.5 2^52: what is added to it is rounded to whole numbers, which its lower bits then have
+    const double t = __builtin_fma(fmax(y, -701.0), 46.16624130844682904, ROUND), n = t - ROUND;
+    double r = __builtin_fma(n, -2.166084938653512e-02, y);     // ln 2 / 32 in two parts, the first of 32 bits: its product with n is exact
+    r = __builtin_fma(n, -5.9631716539705866e-12, r);
+    double p = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
+    p = __builtin_fma(p, r, 1.0 / 6.0);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0) * r;
+    const int i = (int)__builtin_bit_cast(unsigned long long, t);
+    const double b = table[i & 31];
+    const unsigned long long e = __builtin_bit_cast(unsigned long long, __builtin_fma(b, p, b)) + ((unsigned long long)(unsigned)(i >> 5) << 52);
+    return y >= -700.0 ? __builtin_bit_cast(double, e) : 0.0;
+  }
+};
+constexpr double LN2 = 0.69314718055994530942;
+// 2^(j/32), j < 32, by the series of e^x on [0, ln 2)
+__device__ __forceinline__ void fill_table(double* table) {
+  if (threadIdx.x < 32) {
+    const double x = threadIdx.x * (LN2 / 32.0);
+    double s = 1.0;
+#pragma unroll
+    for (int k = 18; k > 0; --k) s = __builtin_fma(s, x / (double)k, 1.0);
+    table[threadIdx.x] = s;
+  }
+  __syncthreads();
 }
 
 // Sum of e^((x - ref) / temperature) over some entries.  ref is one of them and no more than 500 temperatures below any: with 64 bits it need not be the largest.
@@ -40,6 +52,9 @@ struct __attribute__((aligned(16))) Mass {
   double sum;
   float ref, most;
 };
+
+// the column of p, that of q (-1: none), and what makes probabilities of exponentials; bad: no answer
+struct Chosen { int col_t, col_d, bad, pad; double ref_t, inv_t, ref_d, inv_d; };
 
 struct VerifyP {
   const void* target;
@@ -56,121 +71,157 @@ struct VerifyP {
   int ct, groups_t, slices, rows;          // first kernel: 16-byte columns a workgroup, workgroups across the target, slices of `rows` entries
   Mass* mass;                              // [columns + T][slices]
   int parts, part_rows;
-  struct Chosen* chosen;                   // [n_seq]
+  Chosen* chosen;                          // [n_seq]
   double* sums;                            // [n_seq][parts][2] of r and of p
 };
 
-// the column of p, that of q (-1: none), and what makes probabilities of exponentials; bad: no answer
-struct Chosen { int col_t, col_d, bad, pad; double ref_t, inv_t, ref_d, inv_d; };
-
-__device__ __forceinline__ Mass joined(Mass a, Mass b, double inv) {
-  Mass r;
-  r.ref = fmaxf(a.ref, b.ref);             // -inf where neither has an entry, and then both sums are zero
-  r.most = __builtin_elementwise_maximum(a.most, b.most);
-  r.sum = a.sum * (a.ref == r.ref ? 1.0 : exp64(((double)a.ref - (double)r.ref) * inv)) + b.sum * (b.ref == r.ref ? 1.0 : exp64(((double)b.ref - (double)r.ref) * inv));
-  return r;
-}
-
 template <typename E>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
-  constexpr int VEC = 16 / sizeof(E);
-  __shared__ Mass sh[256];
+  constexpr int VEC = 16 / sizeof(E), UN = 4;
+  __shared__ double table[32];
+  __shared__ double sSum[4][8][VEC];
+  __shared__ float sRef[4][8][VEC], sMost[4][8][VEC];
+  fill_table(table);
+  const Exp ex{table};
   const bool of_draft = (int)blockIdx.x >= p.groups_t;
-  const int c = threadIdx.x % p.ct, r = threadIdx.x / p.ct, rl = 256 / p.ct;
+  const int c = threadIdx.x % p.ct, r = threadIdx.x / p.ct, rl = 256 / p.ct, wave = threadIdx.x >> 6;
   const long long t0 = ((long long)((int)blockIdx.x - (of_draft ? p.groups_t : 0)) * p.ct + c) * VEC, ld = of_draft ? p.ldd : p.ldt;
   const int n = of_draft ? p.T : p.columns, v0 = (int)blockIdx.y * p.rows, v1 = min(v0 + p.rows, p.V);
-  Mass a[VEC];
+  double sum[VEC], from[VEC];              // from: ref / temperature
+  float ref[VEC], most[VEC], high[VEC];    // high: what ref may not stay behind
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) a[e] = Mass{0.0, -INFINITY, -INFINITY};
+  for (int e = 0; e < VEC; ++e) {
+    sum[e] = from[e] = 0.0;
+    ref[e] = most[e] = high[e] = -INFINITY;
+  }
+  const float reach = (float)(500.0 / p.inv);
   if (t0 < n) {
     const E* x = (const E*)(of_draft ? p.draft : p.target) + t0;
-    for (int v = v0 + r; v < v1; v += rl) {
-      float f[VEC];
-      load_floats<VEC>(x + (long long)v * ld, f);
+    auto take = [&](auto count, int v) {
+      constexpr int N = decltype(count)::value;
+      float f[N][VEC];
+#pragma unroll
+      for (int k = 0; k < N; ++k) load_floats<VEC>(x + (long long)(v + k * rl) * ld, f[k]);
       bool far = false;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        a[e].most = __builtin_elementwise_maximum(a[e].most, f[e]);
-        far = far || (f[e] > a[e].ref && ((double)f[e] - (double)a[e].ref) * p.inv > 500.0);
+        float m = f[0][e];
+#pragma unroll
+        for (int k = 1; k < N; ++k) m = __builtin_elementwise_maximum(m, f[k][e]);
+        most[e] = __builtin_elementwise_maximum(most[e], m);
+        far = far || most[e] > high[e];
       }
-      if (far)
+      if (__builtin_amdgcn_ballot_w64(far)) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (f[e] > a[e].ref && ((double)f[e] - (double)a[e].ref) * p.inv > 500.0) {
-            a[e].sum *= exp64(((double)a[e].ref - (double)f[e]) * p.inv);
-            a[e].ref = f[e];
+          if (most[e] > high[e]) {
+            sum[e] *= ref[e] == -INFINITY ? 0.0 : ex(((double)ref[e] - (double)most[e]) * p.inv);
+            ref[e] = most[e];
+            high[e] = ref[e] + reach;
+            from[e] = (double)ref[e] * p.inv;
           }
+      }
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) a[e].sum += exp64(((double)f[e] - (double)a[e].ref) * p.inv);
-    }
+      for (int e = 0; e < VEC; ++e)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[e] += ex(__builtin_fma((double)f[k][e], p.inv, -from[e]));
+    };
+    int v = v0 + r;
+    for (; v + (UN - 1) * rl < v1; v += UN * rl) take(std::integral_constant<int, UN>(), v);
+    for (; v < v1; v += rl) take(std::integral_constant<int, 1>(), v);
   }
+  // one reference for the slice, and the sums by it: over the wavefront, then the four of them
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    __syncthreads();
-    sh[threadIdx.x] = a[e];
-    for (int o = rl >> 1; o > 0; o >>= 1) {
-      __syncthreads();
-      if (r < o) sh[threadIdx.x] = joined(sh[threadIdx.x], sh[threadIdx.x + o * p.ct], p.inv);
+    float all = ref[e], top = most[e];
+    for (int o = p.ct; o < 64; o <<= 1) {
+      all = fmaxf(all, __shfl_xor(all, o, 64));
+      top = __builtin_elementwise_maximum(top, __shfl_xor(top, o, 64));
     }
-    if (r == 0 && t0 + e < n) p.mass[(t0 + e + (of_draft ? p.columns : 0)) * p.slices + blockIdx.y] = sh[c];
+    if (sum[e] != 0.0 && all != ref[e]) sum[e] *= ex(((double)ref[e] - (double)all) * p.inv);
+    for (int o = p.ct; o < 64; o <<= 1) sum[e] += __shfl_xor(sum[e], o, 64);
+    if ((int)(threadIdx.x & 63) < p.ct) {
+      sSum[wave][c][e] = sum[e];
+      sRef[wave][c][e] = all;
+      sMost[wave][c][e] = top;
+    }
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < p.ct * VEC) {
+    const int cc = threadIdx.x / VEC, e = threadIdx.x % VEC;
+    const long long t = ((long long)((int)blockIdx.x - (of_draft ? p.groups_t : 0)) * p.ct + cc) * VEC + e;
+    float all = sRef[0][cc][e], top = sMost[0][cc][e];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      all = fmaxf(all, sRef[w][cc][e]);
+      top = __builtin_elementwise_maximum(top, sMost[w][cc][e]);
+    }
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const double x = sSum[w][cc][e];
+      if (x != 0.0) s += sRef[w][cc][e] == all ? x : x * ex(((double)sRef[w][cc][e] - (double)all) * p.inv);
+    }
+    if (t < n) p.mass[(t + (of_draft ? p.columns : 0)) * p.slices + blockIdx.y] = Mass{s, all, top};
   }
 }
 
 // All slices of a column, in every lane of the wavefront.
-__device__ __forceinline__ Mass whole_column(const VerifyP& p, long long column) {
+__device__ __forceinline__ Mass whole_column(const VerifyP& p, const Exp& ex, long long column) {
   const int lane = threadIdx.x & 63;
-  Mass a = Mass{0.0, -INFINITY, -INFINITY};
-  if (lane < p.slices) a = p.mass[column * p.slices + lane];
+  Mass a[SLICES / 64];
+  Mass all = Mass{0.0, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < SLICES / 64; ++i) {
+    a[i] = Mass{0.0, -INFINITY, -INFINITY};
+    if (lane + 64 * i < p.slices) a[i] = p.mass[column * p.slices + lane + 64 * i];
+  }
+#pragma unroll
+  for (int i = 0; i < SLICES / 64; ++i) {
+    all.ref = fmaxf(all.ref, a[i].ref);
+    all.most = __builtin_elementwise_maximum(all.most, a[i].most);
+  }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    Mass b;
-    b.sum = __shfl_xor(a.sum, o, 64);
-    b.ref = __shfl_xor(a.ref, o, 64);
-    b.most = __shfl_xor(a.most, o, 64);
-    a = lane & o ? joined(b, a, p.inv) : joined(a, b, p.inv);      // the same in both lanes, to the bit
+    all.ref = fmaxf(all.ref, __shfl_xor(all.ref, o, 64));
+    all.most = __builtin_elementwise_maximum(all.most, __shfl_xor(all.most, o, 64));
   }
-  return a;
+#pragma unroll
+  for (int i = 0; i < SLICES / 64; ++i)
+    if (a[i].sum != 0.0) all.sum += a[i].sum * ex(((double)a[i].ref - (double)all.ref) * p.inv);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) all.sum += __shfl_xor(all.sum, o, 64);
+  return all;
 }
 
-__device__ __forceinline__ double weight(const Chosen& c, float xt, float xd, bool rest, double inv) {
-  const double pt = exp64(((double)xt - c.ref_t) * inv) * c.inv_t;
-  if (!rest) return pt;
-  return fmax(pt - exp64(((double)xd - c.ref_d) * inv) * c.inv_d, 0.0);
-}
-
+// A workgroup for a sequence, a wavefront for a position.
 template <typename E>
-__global__ __launch_bounds__(256) void verify_weigh_kernel(const VerifyP p) {
-  __shared__ Chosen sc;
+__global__ __launch_bounds__(256) void verify_decide_kernel(const VerifyP p) {
+  __shared__ double table[32];
   __shared__ int stop[4];
   __shared__ Chosen found[4];
-  __shared__ double sr[4], sp[4];
-  const int seq = (int)blockIdx.x, part = (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  fill_table(table);
+  const Exp ex{table};
+  const int seq = (int)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const auto begin = [&](int s) { return p.draft_start ? min(max(p.draft_start[s], 0), p.T) : (s ? p.T : 0); };
   const int a = begin(seq), n = max(begin(seq + 1) - a, 0);
-  const E* target = (const E*)p.target;
-  const E* draft = (const E*)p.draft;
-  // the positions four at a time, a wavefront each: every part does so again, which costs less than a kernel of its own
-  int accepted = n;
   for (int i0 = 0; i0 <= n; i0 += 4) {
     const int i = i0 + wave;
     if (i <= n) {
-      const int ct = min(a + seq + i, p.columns - 1);
-      const Mass mt = whole_column(p, ct);
+      const int ct = min(a + seq + i, p.columns - 1), x = i < n ? p.draft_id[a + i] : 0, at = min(max(x, 0), p.V - 1);
+      const float xt = (float)((const E*)p.target)[(long long)at * p.ldt + ct];
+      const Mass mt = whole_column(p, ex, ct);
       Chosen c = Chosen{ct, -1, 0, 0, (double)mt.ref, 1.0 / mt.sum, 0.0, 0.0};
       c.bad = !(fabsf(mt.most) < INFINITY);
       bool keep = false;
       if (i < n) {
-        const Mass md = whole_column(p, (long long)p.columns + a + i);
+        const float xd = (float)((const E*)p.draft)[(long long)at * p.ldd + a + i];
+        const Mass md = whole_column(p, ex, (long long)p.columns + a + i);
         c.col_d = a + i;
         c.ref_d = md.ref;
         c.inv_d = 1.0 / md.sum;
         c.bad = c.bad || !(fabsf(md.most) < INFINITY);
-        const int x = p.draft_id[a + i];
-        if (x >= 0 && x < p.V && !c.bad) {
-          const double pt = exp64(((double)(float)target[(long long)x * p.ldt + ct] - c.ref_t) * p.inv) * c.inv_t;
-          const double qd = exp64(((double)(float)draft[(long long)x * p.ldd + a + i] - c.ref_d) * p.inv) * c.inv_d;
-          keep = (double)p.u[a + i] * qd < pt;
-        }
+        if (x == at && !c.bad) keep = (double)p.u[a + i] * (ex(((double)xd - c.ref_d) * p.inv) * c.inv_d) < ex(((double)xt - c.ref_t) * p.inv) * c.inv_t;
       }
       if (lane == 0) {
         stop[wave] = !keep;
@@ -182,41 +233,69 @@ __global__ __launch_bounds__(256) void verify_weigh_kernel(const VerifyP p) {
     for (int w = 3; w >= 0; --w)
       if (i0 + w <= n && stop[w]) at = w;
     if (at >= 0) {
-      accepted = i0 + at;
-      if (threadIdx.x == 0) sc = found[at];
-      __syncthreads();
+      if (threadIdx.x == 0) {
+        p.accepted[seq] = i0 + at;
+        p.chosen[seq] = found[at];
+      }
       break;
     }
     __syncthreads();
   }
-  const Chosen c = sc;
-  if (part == 0 && threadIdx.x == 0) {
-    p.accepted[seq] = accepted;
-    p.chosen[seq] = c;
-  }
+}
+
+__device__ __forceinline__ double weight(const Chosen& c, const Exp& ex, float xt, float xd, bool rest, double inv) {
+  const double pt = ex(((double)xt - c.ref_t) * inv) * c.inv_t;
+  if (!rest) return pt;
+  return fmax(pt - ex(((double)xd - c.ref_d) * inv) * c.inv_d, 0.0);
+}
+
+// A workgroup has a part of the vocabulary for S sequences: neighbouring lanes are neighbouring sequences, whose columns lie in the same lines of memory.
+template <typename E, int S>
+__global__ __launch_bounds__(256) void verify_weigh_kernel(const VerifyP p) {
+  constexpr int RL = 256 / S, UN = 4;
+  __shared__ double table[32];
+  __shared__ double sr[4][S], sp[4][S];
+  fill_table(table);
+  const Exp ex{table};
+  const int s = threadIdx.x % S, r0 = threadIdx.x / S, wave = threadIdx.x >> 6, seq = (int)blockIdx.x * S + s, part = (int)blockIdx.y;
+  const Chosen c = p.chosen[min(seq, p.n_seq - 1)];
   const int v0 = part * p.part_rows, v1 = min(v0 + p.part_rows, p.V);
-  double r = 0.0, s = 0.0;
-  if (!c.bad)
-    for (int v = v0 + (int)threadIdx.x; v < v1; v += 256) {
-      const float xt = (float)target[(long long)v * p.ldt + c.col_t];
-      const double pt = exp64(((double)xt - c.ref_t) * p.inv) * c.inv_t;
-      s += pt;
-      if (c.col_d >= 0) r += fmax(pt - exp64(((double)(float)draft[(long long)v * p.ldd + c.col_d] - c.ref_d) * p.inv) * c.inv_d, 0.0);
-    }
+  double r = 0.0, q = 0.0;
+  if (!c.bad) {
+    const E* target = (const E*)p.target + c.col_t;
+    const E* draft = (const E*)p.draft + max(c.col_d, 0);
+    const bool drafted = c.col_d >= 0;
+    for (int v = v0 + r0; v < v1; v += UN * RL) {
+      float xt[UN], xd[UN];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    r += __shfl_xor(r, o, 64);
-    s += __shfl_xor(s, o, 64);
+      for (int k = 0; k < UN; ++k) {
+        const long long at = min(v + k * RL, v1 - 1);
+        xt[k] = (float)target[at * p.ldt];
+        xd[k] = drafted ? (float)draft[at * p.ldd] : 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < UN; ++k) {
+        const bool in = v + k * RL < v1;
+        const double pt = ex(((double)xt[k] - c.ref_t) * p.inv) * c.inv_t;
+        q += in ? pt : 0.0;
+        if (drafted) r += in ? fmax(pt - ex(((double)xd[k] - c.ref_d) * p.inv) * c.inv_d, 0.0) : 0.0;
+      }
+    }
   }
-  if (lane == 0) {
-    sr[wave] = r;
-    sp[wave] = s;
+#pragma unroll
+  for (int o = S; o < 64; o <<= 1) {
+    r += __shfl_xor(r, o, 64);
+    q += __shfl_xor(q, o, 64);
+  }
+  if ((int)(threadIdx.x & 63) < S) {
+    sr[wave][s] = r;
+    sp[wave][s] = q;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if ((int)threadIdx.x < S && seq < p.n_seq) {
     double* to = p.sums + ((long long)seq * p.parts + part) * 2;
-    to[0] = ((sr[0] + sr[1]) + sr[2]) + sr[3];
-    to[1] = ((sp[0] + sp[1]) + sp[2]) + sp[3];
+    to[0] = ((sr[0][s] + sr[1][s]) + sr[2][s]) + sr[3][s];
+    to[1] = ((sp[0][s] + sp[1][s]) + sp[2][s]) + sp[3][s];
   }
 }
 
@@ -233,9 +312,12 @@ __device__ __forceinline__ double upto(double x) {
 
 template <typename E>
 __global__ __launch_bounds__(256) void verify_find_kernel(const VerifyP p) {
+  __shared__ double table[32];
   __shared__ double totals[4];
   __shared__ int firsts[4], lasts[4];
   const int seq = (int)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  fill_table(table);
+  const Exp ex{table};
   const Chosen c = p.chosen[seq];
   if (c.bad) {
     if (threadIdx.x == 0) p.next_id[seq] = -1;
@@ -258,7 +340,7 @@ __global__ __launch_bounds__(256) void verify_find_kernel(const VerifyP p) {
   for (int b = v0; b < v1; b += 256) {
     const int v = b + (int)threadIdx.x;
     double w = 0.0;
-    if (v < v1) w = weight(c, (float)((const E*)p.target)[(long long)v * p.ldt + c.col_t], rest ? (float)((const E*)p.draft)[(long long)v * p.ldd + c.col_d] : 0.0f, rest, p.inv);
+    if (v < v1) w = weight(c, ex, (float)((const E*)p.target)[(long long)v * p.ldt + c.col_t], rest ? (float)((const E*)p.draft)[(long long)v * p.ldd + c.col_d] : 0.0f, rest, p.inv);
     double run = upto(w);
     if (lane == 63) totals[wave] = run;
     __syncthreads();
@@ -312,9 +394,13 @@ static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 
 template <typename E>
 static void launch_verify(strp_ctx* ctx, const VerifyP& p, const VerifyPlan& q) {
-  hipLaunchKernelGGL((verify_sums_kernel<E>), dim3((unsigned)(q.groups_t + q.groups_d), (unsigned)q.slices), dim3(256), 0, ctx->stream, p);
-  hipLaunchKernelGGL((verify_weigh_kernel<E>), dim3((unsigned)p.n_seq, (unsigned)q.parts), dim3(256), 0, ctx->stream, p);
-  hipLaunchKernelGGL((verify_find_kernel<E>), dim3((unsigned)p.n_seq), dim3(256), 0, ctx->stream, p);
+  const dim3 block(256);
+  const unsigned n = (unsigned)p.n_seq;
+  hipLaunchKernelGGL((verify_sums_kernel<E>), dim3((unsigned)(q.groups_t + q.groups_d), (unsigned)q.slices), block, 0, ctx->stream, p);
+  hipLaunchKernelGGL((verify_decide_kernel<E>), dim3(n), block, 0, ctx->stream, p);
+  if (n >= 8) hipLaunchKernelGGL((verify_weigh_kernel<E, 8>), dim3((n + 7) / 8, (unsigned)q.parts), block, 0, ctx->stream, p);
+  else hipLaunchKernelGGL((verify_weigh_kernel<E, 1>), dim3(n, (unsigned)q.parts), block, 0, ctx->stream, p);
+  hipLaunchKernelGGL((verify_find_kernel<E>), dim3(n), block, 0, ctx->stream, p);
 }
 
 }  // namespace strp

@@ -120,8 +120,8 @@ def check_verify():
             lib.workspace(lib.lib.strp_verify_draft_workspace_bytes(V, T, n))
             for dt in (strp.BF16, strp.F32):
                 assert call(V=V, T=T, n_seq=n, ldt=8192, ldd=4096, dtype=dt)[0] == strp.OK, (V, T, n)
-    lib.workspace(1024)
-    st, launches = call()
+    lib.workspace(4096)
+    st, launches = call(V=50000)
     assert st == strp.ENOMEM and not launches
     bare = C.c_void_p()
     assert lib.lib.strp_create(C.byref(bare), 0, None) == strp.OK

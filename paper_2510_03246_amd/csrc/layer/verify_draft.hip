@@ -12,26 +12,29 @@
 
 namespace strp {
 
-constexpr int SLICES = 256, PARTS = 64;    // at most: a lane has four of the slices of a column, one of the parts
+constexpr int SLICES = 256, PARTS = 256;   // at most: a lane has four of either
 
-// e^y to a few units of 2^-52 for y <= 600, 0 where y is below -700 (NaN: 0 too).  y = (32 k + j) ln 2 / 32 + r with |r| <= ln 2 / 64, so that e^y = 2^k 2^(j/32) e^r: a table of 32 in LDS,
-// which 64 banks give to any lanes at once, and the series to r^5 (the next term is below 2^-48.6 of the whole).  14 instructions in 64 bits; without the table and to r^12 it is 24.
+// e^y for y from -705 to 600, to 2^-48 of itself (and where y is far below zero, and nothing hangs on it, to 2^-44).  y = (32 k + j) ln 2 / 32 + r with
+// |r| <= ln 2 / 64, so that e^y = 2^k 2^(j/32) e^r: a table of 32 in LDS, which 64 banks give to any lanes at once, and the series to r^5.  12 instructions in
+// 64 bits (without the table and to r^12: 22, and verify_256 took 445 us instead of 224).
 struct Exp {
   const double* table;
-  __device__ __forceinline__ double operator()(double y) const {
+  __device__ __forceinline__ double near(double y) const {
     constexpr double ROUND = 6755399441055744.0;                    // 1.5 2^52: what is added to it is rounded to whole numbers, which its lower bits then have
-    const double t = __builtin_fma(fmax(y, -701.0), 46.16624130844682904, ROUND), n = t - ROUND;
-    double r = __builtin_fma(n, -2.166084938653512e-02, y);     // ln 2 / 32 in two parts, the first of 32 bits: its product with n is exact
-    r = __builtin_fma(n, -5.9631716539705866e-12, r);
+    const double t = __builtin_fma(y, 46.16624130844682904, ROUND), n = t - ROUND;
+    const double r = __builtin_fma(n, -2.1660849392498290836e-02, y);
     double p = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
     p = __builtin_fma(p, r, 1.0 / 6.0);
     p = __builtin_fma(p, r, 0.5);
     p = __builtin_fma(p, r, 1.0) * r;
-    const int i = (int)__builtin_bit_cast(unsigned long long, t);
+    const unsigned i = (unsigned)__builtin_bit_cast(unsigned long long, t);
     const double b = table[i & 31];
-    const unsigned long long e = __builtin_bit_cast(unsigned long long, __builtin_fma(b, p, b)) + ((unsigned long long)(unsigned)(i >> 5) << 52);
-    return y >= -700.0 ? __builtin_bit_cast(double, e) : 0.0;
+    const unsigned long long e = __builtin_bit_cast(unsigned long long, __builtin_fma(b, p, b));
+    const unsigned high = (unsigned)(e >> 32) + ((i & ~31u) << 15);      // k into the exponent
+    return __builtin_bit_cast(double, (unsigned long long)high << 32 | (unsigned)e);
   }
+  // 0 where y is below -700 or NaN
+  __device__ __forceinline__ double operator()(double y) const { return y >= -700.0 ? near(y) : 0.0; }
 };
 constexpr double LN2 = 0.69314718055994530942;
 // 2^(j/32), j < 32, by the series of e^x on [0, ln 2)
@@ -124,12 +127,14 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum[e] += ex(__builtin_fma((double)f[k][e], p.inv, -from[e]));
+        for (int k = 0; k < N; ++k) sum[e] += ex.near(fmax(__builtin_fma((double)f[k][e], p.inv, -from[e]), -700.0));      // e^-700, for -inf and NaN too, is nothing beside ref's own share
     };
     int v = v0 + r;
     for (; v + (UN - 1) * rl < v1; v += UN * rl) take(std::integral_constant<int, UN>(), v);
     for (; v < v1; v += rl) take(std::integral_constant<int, 1>(), v);
   }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sum[e] = ref[e] == -INFINITY ? 0.0 : sum[e];
   // one reference for the slice, and the sums by it: over the wavefront, then the four of them
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
@@ -325,15 +330,39 @@ __global__ __launch_bounds__(256) void verify_find_kernel(const VerifyP p) {
   }
   // every wavefront finds the part for itself
   const double* from = p.sums + (long long)seq * p.parts * 2;
-  const double r = lane < p.parts && c.col_d >= 0 ? from[2 * lane] : 0.0, s = lane < p.parts ? from[2 * lane + 1] : 0.0;
-  const bool rest = __builtin_amdgcn_ballot_w64(r > 0.0) != 0;
-  const double mine = rest ? r : s, sum = upto(mine), total = __shfl(sum, 63, 64);
+  double r[PARTS / 64], s[PARTS / 64], rs = 0.0, ss = 0.0;      // lane l has the parts 4 l and on
+#pragma unroll
+  for (int i = 0; i < PARTS / 64; ++i) {
+    const int at = PARTS / 64 * lane + i;
+    const bool in = at < p.parts;
+    r[i] = in && c.col_d >= 0 ? from[2 * at] : 0.0;
+    s[i] = in ? from[2 * at + 1] : 0.0;
+    rs += r[i];
+    ss += s[i];
+  }
+  const bool rest = __builtin_amdgcn_ballot_w64(rs > 0.0) != 0;
+  const double mine = rest ? rs : ss, sum = upto(mine), total = __shfl(sum, 63, 64);
   const float u = p.u_next[seq];
   const double goal = u < 1.0f ? (double)u * total : (double)INFINITY;
   const unsigned long long over = __builtin_amdgcn_ballot_w64(sum > goal && mine > 0.0), some = __builtin_amdgcn_ballot_w64(mine > 0.0);
-  const int part = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : 0;
-  double before = __shfl(sum, part > 0 ? part - 1 : 0, 64);
-  if (part == 0) before = 0.0;
+  const int holder = over ? __builtin_ctzll(over) : some ? 63 - __builtin_clzll(some) : 0;
+  // of the holder's parts the first whose sum is over the goal, or the last that has any
+  double before = __shfl(sum - mine, holder, 64);
+  int part = PARTS / 64 * holder;
+  {
+    double run = before;
+    bool done = false;
+#pragma unroll
+    for (int i = 0; i < PARTS / 64; ++i) {
+      const double x = __shfl(rest ? r[i] : s[i], holder, 64);
+      if (!done && x > 0.0) {
+        before = run;
+        part = PARTS / 64 * holder + i;
+      }
+      run += x;
+      done = done || (x > 0.0 && run > goal);
+    }
+  }
   // its entries, 256 at a time
   const int v0 = part * p.part_rows, v1 = min(v0 + p.part_rows, p.V);
   int last = -1;                           // the last entry with r > 0, should rounding leave the sums of the part below the goal
@@ -378,7 +407,7 @@ static VerifyPlan plan_verify(int V, long long T, int n_seq, int dtype) {
   q.groups_t = (int)((chunks_t + q.ct - 1) / q.ct);
   q.groups_d = (int)((chunks_d + q.ct - 1) / q.ct);
   // as many slices as fill the chip twice over, none below one entry a thread
-  long long slices = 2048 / (q.groups_t + q.groups_d) + 1;
+  long long slices = 1024 / (q.groups_t + q.groups_d) + 1;
   const long long most = (V + 256 / q.ct - 1) / (256 / q.ct);
   if (slices > most) slices = most;
   if (slices > SLICES) slices = SLICES;
@@ -398,7 +427,9 @@ static void launch_verify(strp_ctx* ctx, const VerifyP& p, const VerifyPlan& q) 
   const unsigned n = (unsigned)p.n_seq;
   hipLaunchKernelGGL((verify_sums_kernel<E>), dim3((unsigned)(q.groups_t + q.groups_d), (unsigned)q.slices), block, 0, ctx->stream, p);
   hipLaunchKernelGGL((verify_decide_kernel<E>), dim3(n), block, 0, ctx->stream, p);
-  if (n >= 8) hipLaunchKernelGGL((verify_weigh_kernel<E, 8>), dim3((n + 7) / 8, (unsigned)q.parts), block, 0, ctx->stream, p);
+  // 32 sequences of four tokens and one lie in three lines of memory, 8 in one or two: from where 32 a workgroup fill the chip
+  if (n >= 128) hipLaunchKernelGGL((verify_weigh_kernel<E, 32>), dim3((n + 31) / 32, (unsigned)q.parts), block, 0, ctx->stream, p);
+  else if (n >= 8) hipLaunchKernelGGL((verify_weigh_kernel<E, 8>), dim3((n + 7) / 8, (unsigned)q.parts), block, 0, ctx->stream, p);
   else hipLaunchKernelGGL((verify_weigh_kernel<E, 1>), dim3(n, (unsigned)q.parts), block, 0, ctx->stream, p);
   hipLaunchKernelGGL((verify_find_kernel<E>), dim3(n), block, 0, ctx->stream, p);
 }

@@ -5,65 +5,12 @@
 // tile of rows by 128 (fp32: 64) keys, numbered sequence by sequence, and every workgroup gets as many of them as any other, one after the other: so a long sequence
 // beside short ones, or one alone, fills the chip as well as many alike.  The lengths are in device memory, so every workgroup works its share out
 // for itself.  What it does not finish it leaves as (maximum, sum, weighted sum) in the workspace, and a second kernel puts such parts together in their order.
-#include "paged_cache.h"
+#include "cache_attention.h"
+#include "cache_wide.h"
 
 #include <type_traits>
 
 namespace strp {
-
-constexpr int ROWS = 16;
-constexpr float LOG2E = 1.44269504088896341f;
-
-struct RowsP {
-  Pages c;
-  const void* Q;
-  void* C;
-  const void* K;
-  const void* V;
-  const floatx4* sK;       // (lowest, step) of two keys
-  const floatx4* sV;
-  const int32_t* kv_of_head;
-  int heads, group;
-  long long ldq, ldc;
-  float scale_log2e;
-  int workers, least;      // workgroups, and the fewest units that one gets
-  // what workgroups leave unfinished: [workers][2], of a tile of rows that began before (0) or goes on behind (1)
-  float* part;             // [slot][row][channels]
-  float2* ml;              // [slot][row]
-  long long* off;          // [slot][row] where the row's results go, -1: no such row
-  int* parts;              // [worker] how many workgroups share the tile that begins in slot 1; 0: none
-};
-
-__device__ __forceinline__ float both_16(float x, bool sum) {      // with the lane 16 further in its half
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-  const unsigned a = r[0], b = r[1];
-  return sum ? __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b) : __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
-}
-__device__ __forceinline__ float both_32(float x, bool sum) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
-  const unsigned a = r[0], b = r[1];
-  return sum ? __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b) : __builtin_elementwise_maximum(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
-}
-// over the four lanes that have the same row
-__device__ __forceinline__ float quads_max(float x) { return both_32(both_16(x, false), false); }
-__device__ __forceinline__ float quads_sum(float x) { return both_32(both_16(x, true), true); }
-
-// a value that all lanes have, in scalar registers
-__device__ __forceinline__ long long uniform(long long x) {
-  const unsigned lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-  return (long long)((unsigned long long)hi << 32 | lo);
-}
-
-// a base that stays in scalar registers beside its lanes' offsets (or the sums of both that do not change are kept in vector registers, two for an address)
-__device__ __forceinline__ const char* opaque(const char* p) {
-  asm("" : "+s"(p));
-  return p;
-}
-
-__device__ __forceinline__ unsigned pick(unsigned a, unsigned b, unsigned sel) { return __builtin_amdgcn_perm(b, a, sel); }
-constexpr unsigned LOWS = 0x05040100u, HIGHS = 0x07060302u;      // the lower, the upper halves of a and b
-// whole numbers 0..15 in bits 0-3 and 16-19 as bf16 of 128 + n, which is exact
-__device__ __forceinline__ unsigned with_128(unsigned x) { return (x & 0x000F000Fu) | 0x43004300u; }
 
 // One tile of the cache's keys or values as a lane has it.  Keys: lane (key l % 16, quarter l / 16 of a step of the contraction).  Values: channels W (l % 16) .. + W of
 // the keys 4 (l / 16) .. + 4, which is where the probabilities of the scores' registers are.
@@ -97,44 +44,32 @@ struct Tile<__bf16, true, W> : TileQ4<__bf16, W> {};
 template <int W>
 struct Tile<float, true, W> : TileQ4<float, W> {};
 
+template <int W>
+struct RowsLds {
+  static constexpr int PITCH = 16 * W + 4;
+  float o[4][ROWS][PITCH];
+};
+
 template <typename E, bool Q4, int W, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
+__device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, unsigned char* smem, unsigned block) {
   constexpr bool BF = sizeof(E) == 2;
   typedef Tile<E, Q4, W> TileT;
-  constexpr int NC = TileT::NC, DH = 16 * W, PITCH = DH + 4;
+  constexpr int NC = TileT::NC, DH = 16 * W;
   constexpr int NT = BF || Q4 ? 2 : 1, KW = 16 * NT, UNIT = 4 * KW;      // tiles and keys of a wavefront in a unit, keys of a unit
-  __shared__ __attribute__((aligned(16))) float sO[4][ROWS][PITCH];
+  auto& sO = ((RowsLds<W>*)smem)->o;
   __shared__ float sM[4][ROWS], sL[4][ROWS];
   __shared__ long long sOff[ROWS];
-  __shared__ unsigned short sOrder[MAX_CACHE_HEADS];      // the heads by the key-value head that they read
-  __shared__ int sFirst[MAX_CACHE_HEADS + 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quad = lane >> 4;
   const Pages& c = p.c;
   const int dh = c.dh;
   // neighbours in the work are neighbours on an XCD
-  const int worker = (int)(blockIdx.x & 7) * (p.workers >> 3) + (int)(blockIdx.x >> 3);
+  const int worker = (int)(block & 7) * (WORKERS >> 3) + (int)(block >> 3);
 
-  if (p.kv_of_head) {
-    __shared__ int sOf[MAX_CACHE_HEADS];
-    for (int h = tid; h < p.heads; h += 256) sOf[h] = clamped(p.kv_of_head[h], 0, c.kv_heads - 1);
-    __syncthreads();
-    for (int h = tid; h < p.heads; h += 256) {
-      int at = 0;
-      for (int o = 0; o < p.heads; ++o) at += sOf[o] < sOf[h] || (sOf[o] == sOf[h] && o < h);
-      sOrder[at] = (unsigned short)h;
-    }
-    for (int g = tid; g <= c.kv_heads; g += 256) {
-      int at = 0;
-      for (int o = 0; o < p.heads; ++o) at += sOf[o] < g;
-      sFirst[g] = at;
-    }
-    __syncthreads();
-  }
-  auto group_of = [&](int kv) { return p.kv_of_head ? sFirst[kv + 1] - sFirst[kv] : p.group; };
-  auto tiles_of = [&](int n) {             // tiles of rows of a sequence with n new tokens
-    if (!p.kv_of_head) return c.kv_heads * ((n * p.group + ROWS - 1) / ROWS);
+  auto tiles_of = [&](int n, int group) { return p.wide && n * group > WIDE_FROM ? 0 : (n * group + ROWS - 1) / ROWS; };      // of the rows that share a key-value head
+  auto all_tiles = [&](int n) {            // of a sequence with n new tokens
+    if (!heads.first) return c.kv_heads * tiles_of(n, heads.group);
     int sum = 0;
-    for (int g = 0; g < c.kv_heads; ++g) sum += (n * group_of(g) + ROWS - 1) / ROWS;
+    for (int g = 0; g < c.kv_heads; ++g) sum += tiles_of(n, heads.of(g));
     return sum;
   };
   struct Seq { int begin, n, past, units, tiles; };
@@ -144,7 +79,7 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
     q.n = max(seq_begin(c, s + 1) - q.begin, 0);
     q.past = seq_past(c, s);
     q.units = q.n ? (min(q.past + q.n, c.cap) + UNIT - 1) / UNIT : 0;
-    q.tiles = q.n ? tiles_of(q.n) : 0;
+    q.tiles = q.n ? all_tiles(q.n) : 0;
     return q;
   };
   // this workgroup's units, and the sequence that they begin in
@@ -162,7 +97,7 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
     upto += lane >= o ? x : 0;
   }
   const long long total = uniform(__shfl(upto, 63, 64));
-  long long per = (total + p.workers - 1) / p.workers;
+  long long per = (total + WORKERS - 1) / WORKERS;
   per = per < p.least ? p.least : per;
   long long u = worker * per;
   const long long u1 = u + per < total ? u + per : total;
@@ -192,23 +127,23 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
     const int row_tile = (int)(rel / q.units), b0 = (int)(rel - (long long)row_tile * q.units);
     const int b1 = (long long)q.units - b0 < u1 - u ? q.units : b0 + (int)(u1 - u);
     int kv, rt, group;
-    if (!p.kv_of_head) {
-      const int per_kv = (q.n * p.group + ROWS - 1) / ROWS;
+    if (!heads.first) {
+      const int per_kv = tiles_of(q.n, heads.group);
       kv = row_tile / per_kv;
       rt = row_tile - kv * per_kv;
-      group = p.group;
+      group = heads.group;
     } else {
       rt = row_tile;
       for (kv = 0; kv < c.kv_heads - 1; ++kv) {
-        const int t = (q.n * same(group_of(kv)) + ROWS - 1) / ROWS;
+        const int t = tiles_of(q.n, same(heads.of(kv)));
         if (rt < t) break;
         rt -= t;
       }
-      group = same(group_of(kv));
+      group = same(heads.of(kv));
     }
     const int rows = min(ROWS, q.n * group - rt * ROWS), r = min(n16, rows - 1);
     const int at = rt * ROWS + r, token = at / group, in_group = at - token * group;
-    const int head = p.kv_of_head ? sOrder[sFirst[kv] + in_group] : kv * group + in_group;
+    const int head = heads.head(kv, in_group);
     const int keys = min(q.past + q.n, c.cap);
     const int see = min(q.past + token, keys - 1);                                             // the row's last key
     const int see_all = min(q.past + rt * ROWS / group, keys - 1), see_any = min(q.past + (rt * ROWS + rows - 1) / group, keys - 1);
@@ -613,12 +548,57 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
   }
 }
 
+// The map of heads by workgroup, in LDS.
+struct MapLds {
+  unsigned short order[MAX_CACHE_HEADS];
+  int first[MAX_CACHE_HEADS + 1];
+};
+__device__ __forceinline__ Heads heads_of(const RowsP& p, MapLds& lds, int* of) {      // of: room for MAX_CACHE_HEADS
+  if (!p.kv_of_head) return Heads{nullptr, nullptr, p.group};
+  const int tid = threadIdx.x;
+  for (int h = tid; h < p.heads; h += 256) of[h] = clamped(p.kv_of_head[h], 0, p.c.kv_heads - 1);
+  __syncthreads();
+  for (int h = tid; h < p.heads; h += 256) {
+    int at = 0;
+    for (int o = 0; o < p.heads; ++o) at += of[o] < of[h] || (of[o] == of[h] && o < h);
+    lds.order[at] = (unsigned short)h;
+  }
+  for (int g = tid; g <= p.c.kv_heads; g += 256) {
+    int at = 0;
+    for (int o = 0; o < p.heads; ++o) at += of[o] < g;
+    lds.first[g] = at;
+  }
+  __syncthreads();
+  return Heads{lds.order, lds.first, p.group};
+}
+
+template <typename E, bool Q4, int W, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
+  __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(RowsLds<W>)];
+  __shared__ MapLds map;
+  static_assert(sizeof(RowsLds<W>) >= 4 * MAX_CACHE_HEADS, "room for the map");
+  const Heads heads = heads_of(p, map, (int*)smem);
+  rows_share<E, Q4, W, SPLIT>(p, heads, smem, blockIdx.x);
+}
+template <int W, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void cache_wide_kernel(const RowsP p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[Wide<W>::BYTES];
+  __shared__ MapLds map;
+  static_assert(Wide<W>::BYTES >= 4 * MAX_CACHE_HEADS, "room for the map");
+  const Heads heads = heads_of(p, map, (int*)smem);
+  wide_share<W, SPLIT>(p, heads, smem, blockIdx.x);
+}
+
 // The parts of tiles that several workgroups had, in the order of the keys.  A workgroup for a row of the tile that begins in a workgroup of the first kernel: a wavefront has a fourth of
 // the parts, a lane two channels.
 template <typename E>
 __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
   __shared__ float sO[4][128];
   __shared__ float sM[4], sL[4];
+  if (sizeof(E) == 2 && blockIdx.x >= (unsigned)WORKERS) {
+    if constexpr (sizeof(E) == 2) wide_join(p, (int)blockIdx.x - WORKERS, (int)blockIdx.y);
+    return;
+  }
   const int worker = (int)blockIdx.x, row = (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int parts = p.parts[worker];
   if (parts == 0) return;
@@ -675,22 +655,26 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
   ((E*)p.C)[to + (long long)threadIdx.x * p.ldc] = (E)(sum / L);
 }
 
-constexpr int WORKERS = 512;               // two workgroups a CU
-
-struct RowsBytes { size_t part, ml, off, parts; };
+struct RowsBytes { size_t part, ml, off, wide_part, wide_ml, wide_off, parts; };
 static RowsBytes rows_bytes(int dh) {
-  const size_t rows = (size_t)WORKERS * 2 * ROWS;
-  return RowsBytes{rows * dh * 4, rows * sizeof(float2), rows * 8, (size_t)WORKERS * 4};
+  const size_t rows = (size_t)WORKERS * 2 * ROWS, wide = (size_t)WORKERS * 2 * WIDE;
+  return RowsBytes{rows * dh * 4, rows * sizeof(float2), rows * 8, wide * dh * 4, wide * sizeof(float2), wide * 8, (size_t)WORKERS * 4};
 }
 static size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 
 template <typename E, bool Q4, bool SPLIT>
 static void launch_rows(strp_ctx* ctx, const RowsP& p, int join_rows) {
-  const dim3 grid((unsigned)p.workers), block(256);
-  if (p.c.dh <= 32) hipLaunchKernelGGL((cache_rows_kernel<E, Q4, 2, SPLIT>), grid, block, 0, ctx->stream, p);
-  else if (p.c.dh <= 64) hipLaunchKernelGGL((cache_rows_kernel<E, Q4, 4, SPLIT>), grid, block, 0, ctx->stream, p);
-  else hipLaunchKernelGGL((cache_rows_kernel<E, Q4, 8, SPLIT>), grid, block, 0, ctx->stream, p);
-  hipLaunchKernelGGL((cache_join_kernel<E>), dim3((unsigned)p.workers, (unsigned)join_rows), block, 0, ctx->stream, p);
+  const dim3 grid((unsigned)WORKERS), block(256);
+  const auto go = [&](auto width) {
+    constexpr int W = decltype(width)::value;
+    if constexpr (sizeof(E) == 2 && !Q4)
+      if (p.wide) hipLaunchKernelGGL((cache_wide_kernel<W, SPLIT>), grid, block, 0, ctx->stream, p);
+    hipLaunchKernelGGL((cache_rows_kernel<E, Q4, W, SPLIT>), grid, block, 0, ctx->stream, p);
+  };
+  if (p.c.dh <= 32) go(std::integral_constant<int, 2>());
+  else if (p.c.dh <= 64) go(std::integral_constant<int, 4>());
+  else go(std::integral_constant<int, 8>());
+  hipLaunchKernelGGL((cache_join_kernel<E>), dim3((unsigned)(p.wide ? 2 * WORKERS : WORKERS), (unsigned)join_rows), block, 0, ctx->stream, p);
 }
 
 }  // namespace strp
@@ -702,7 +686,7 @@ extern "C" {
 size_t strp_cache_attention_workspace_bytes(int32_t d_head) {
   if (d_head <= 0 || d_head > 128) return 0;
   const RowsBytes b = rows_bytes(d_head);
-  return 256 + up256(b.part) + up256(b.ml) + up256(b.off) + up256(b.parts);
+  return 256 + up256(b.part) + up256(b.ml) + up256(b.off) + up256(b.wide_part) + up256(b.wide_ml) + up256(b.wide_off) + 2 * up256(b.parts);
 }
 
 strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* in) {
@@ -722,13 +706,19 @@ strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* i
   STRP_TAKE(ctx, arena, ml, float2, b.ml / sizeof(float2));
   STRP_TAKE(ctx, arena, off, long long, b.off / 8);
   STRP_TAKE(ctx, arena, parts, int, b.parts / 4);
+  STRP_TAKE(ctx, arena, wide_part, float, b.wide_part / 4);
+  STRP_TAKE(ctx, arena, wide_ml, float2, b.wide_ml / sizeof(float2));
+  STRP_TAKE(ctx, arena, wide_off, long long, b.wide_off / 8);
+  STRP_TAKE(ctx, arena, wide_parts, int, b.parts / 4);
   OnDevice on(ctx);
   if (!on.ok()) return fail(ctx, STRP_EHIP, "cache_attention: device %d cannot be made current", ctx->device);
   RowsP p{pages_of(c, in->T), in->Q, in->C, c.K, c.V, (const floatx4*)c.K_scale, (const floatx4*)c.V_scale, in->kv_of_head, in->heads, in->heads / c.kv_heads,
-          in->ldq, in->ldc, in->scale * LOG2E, WORKERS, 1, part, ml, off, parts};
+          in->ldq, in->ldc, in->scale * LOG2E, 1, 4, 0, part, ml, off, parts, wide_part, wide_ml, wide_off, wide_parts};
   if (p.group == 0) p.group = 1;
   // a tile has no more rows than the heads that one key-value head can have times the tokens
   const long long rows = (in->kv_of_head ? in->heads : p.group) * in->T;
+  // Single tokens alone, of no more heads than that, are left to the workgroups of 16 rows: with as many sequences as tokens that is what a call most likely is.
+  p.wide = in->dtype == STRP_BF16 && c.format == STRP_CACHE_BF16 && rows > WIDE_FROM && (in->T > c.n_seq || rows / in->T > WIDE_FROM);
   const int join_rows = rows < ROWS ? (int)rows : ROWS;
   // the lengths are on the device: the operations and bytes of a cache that is full
   const double keys = (double)p.c.cap, T = (double)in->T, row = c.format == STRP_CACHE_Q4 ? 0.5 * c.d_head + 8.0 : bytes_of(in->dtype) * (double)c.d_head;

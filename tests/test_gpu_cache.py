@@ -371,16 +371,33 @@ def test_attention_of_chunks(ctx, dts):
     attention_case(ctx, [(150, 0), (1, 400), (129, 77), (2, 2), (64, 64)], 4, 1, 128, 64, dts, first=5, seed=1)
 
 
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("seqs,heads,kv,dh,page,kv_of", [
+    ([(33, 0)], 1, 1, 128, 16, None),                                                # rows just past those taken 16 at a time, one tile
+    ([(128, 0)], 1, 1, 64, 64, None), ([(129, 5)], 1, 1, 64, 16, None),              # a whole tile, a row more
+    ([(257, 70)], 2, 1, 32, 32, None), ([(384, 63)], 2, 2, 128, 128, None),          # pairs of tiles, and one alone
+    ([(700, 0)], 7, 1, 72, 16, None), ([(90, 1000)], 21, 3, 104, 64, None),          # groups that do not divide a tile
+    ([(40, 20000)], 2, 1, 128, 64, None), ([(70, 9000)], 4, 2, 64, 1024, None),      # a tile's keys over many workgroups
+    ([(50, 300), (1, 5), (0, 9), (31, 60), (32, 0), (200, 0), (1, 4000)], 2, 2, 64, 16, None),      # both ways beside each other
+    ([(60, 90), (1, 800), (9, 30)], 12, 3, 40, 16, [0, 0, 2, 0, 0, 0, 0, 0, 0, 0, 0, 0]),           # by a map: one head many, one one, one none
+    ([(1, 500), (1, 20)], 66, 1, 64, 16, None),                                      # single tokens of many heads
+], ids=str)
+def test_attention_of_many_rows(ctx, seqs, heads, kv, dh, page, kv_of, dts):
+    attention_case(ctx, seqs, heads, kv, dh, page, dts, kv_of=kv_of, seed=1)
+    attention_case(ctx, seqs, heads, kv, dh, page, dts, kv_of=kv_of, first=7, behind=2, seed=4)
+
+
 def test_attention_scales_and_peaked_scores(ctx):
     for dts in CASES:
         attention_case(ctx, [(1, 300), (3, 90)], 4, 2, 64, 16, dts, scale=1e-6)
+        attention_case(ctx, [(100, 200)], 4, 2, 64, 16, dts, scale=1.0, spread=1.0, seed=3)
         attention_case(ctx, [(1, 300), (3, 90)], 4, 2, 64, 16, dts, scale=2.0, spread=0.5, seed=2)
 
 
 @pytest.mark.parametrize("dh", [32, 64, 128])
 def test_attention_with_rounded_probabilities(fast, dh):
     for cdt in (BF16, Q4):
-        attention_case(fast, [(1, 300), (3, 90), (1, 3000), (200, 20)], 4, 2, dh, 16, (BF16, cdt), split=False)
+        attention_case(fast, [(1, 300), (3, 90), (1, 3000), (200, 20), (70, 2000)], 4, 2, dh, 16, (BF16, cdt), split=False)
 
 
 @pytest.mark.parametrize("dts", CASES[:2], ids=IDS[:2])

@@ -65,10 +65,14 @@ __device__ __forceinline__ long long uniform(long long x) {
   return (long long)((unsigned long long)hi << 32 | lo);
 }
 
+// Memory of the device as such: a pointer of which the compiler does not know that is read by loads that count as those of LDS too, and everything is waited for at once.
+template <typename T>
+using Global = const __attribute__((address_space(1))) T*;
 // a base that stays in scalar registers beside its lanes' offsets (or the sums of both that do not change are kept in vector registers, two for an address)
-__device__ __forceinline__ const char* opaque(const char* p) {
-  asm("" : "+s"(p));
-  return p;
+__device__ __forceinline__ Global<char> opaque(const void* p) {
+  Global<char> g = (Global<char>)p;
+  asm("" : "+s"(g));
+  return g;
 }
 
 __device__ __forceinline__ unsigned pick(unsigned a, unsigned b, unsigned sel) { return __builtin_amdgcn_perm(b, a, sel); }

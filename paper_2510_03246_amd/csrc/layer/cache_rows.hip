@@ -119,105 +119,94 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     ++s;
     q = uniform_sequence();
   };
-  while (u >= base + (long long)q.units * q.tiles) next_sequence();
 
-  while (true) {
-    // ---- a segment: blocks b0 .. b1 of one tile of rows ----
+  // A segment: units b0 .. b1 of one tile of rows.  The one behind it is known while it is worked on: its first keys and values are on their way before the last ones here are done
+  // with, or nothing would be read while the wavefronts join their results (64 sequences of 0 to 4000 tokens, two segments a workgroup: 137 us instead of AAA).
+  struct Segment { int s, begin, past, keys, units, kv, rt, group, rows, b0, b1; };
+  auto segment_at = [&](long long u) {
+    while (u >= base + (long long)q.units * q.tiles) next_sequence();
+    Segment g{s, q.begin, q.past, min(q.past + q.n, c.cap), q.units, 0, 0, 0, 0, 0, 0};
     const long long rel = u - base;
-    const int row_tile = (int)(rel / q.units), b0 = (int)(rel - (long long)row_tile * q.units);
-    const int b1 = (long long)q.units - b0 < u1 - u ? q.units : b0 + (int)(u1 - u);
-    int kv, rt, group;
+    const int row_tile = (int)(rel / q.units);
+    g.b0 = (int)(rel - (long long)row_tile * q.units);
+    g.b1 = (long long)q.units - g.b0 < u1 - u ? q.units : g.b0 + (int)(u1 - u);
+    g.rt = row_tile;
     if (!heads.first) {
       const int per_kv = tiles_of(q.n, heads.group);
-      kv = row_tile / per_kv;
-      rt = row_tile - kv * per_kv;
-      group = heads.group;
+      g.kv = row_tile / per_kv;
+      g.rt = row_tile - g.kv * per_kv;
+      g.group = heads.group;
     } else {
-      rt = row_tile;
-      for (kv = 0; kv < c.kv_heads - 1; ++kv) {
-        const int t = tiles_of(q.n, same(heads.of(kv)));
-        if (rt < t) break;
-        rt -= t;
+      for (; g.kv < c.kv_heads - 1; ++g.kv) {
+        const int t = tiles_of(q.n, same(heads.of(g.kv)));
+        if (g.rt < t) break;
+        g.rt -= t;
       }
-      group = same(heads.of(kv));
+      g.group = same(heads.of(g.kv));
     }
-    const int rows = min(ROWS, q.n * group - rt * ROWS), r = min(n16, rows - 1);
-    const int at = rt * ROWS + r, token = at / group, in_group = at - token * group;
+    g.rows = min(ROWS, q.n * g.group - g.rt * ROWS);
+    return g;
+  };
+  // pages of the wavefront's keys: lane l has that of tile l % NT of its keys in unit b + l / NT
+  auto pages_from = [&](const Segment& g, int b) {
+    const int key = (b + lane / NT) * UNIT + wave * KW + (lane % NT) * 16;
+    return clamped((c.table + (long long)g.s * c.ld_table)[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
+  };
+  const int in_page = (1 << c.page_log2) - 1;
+
+  TileT T[NT];
+  Segment g{}, next{};
+  int next_ids = 0;
+  bool begun = false, loaded = false;      // loaded: the segment's first keys and values are here or on their way
+  while (true) {
+    if (begun && u >= u1) break;
+    g = next;
+    int ids = next_ids, bt = g.b0;
+    if (begun) u += g.b1 - g.b0;           // where the next one begins
+    const bool follows = u < u1;
+    if (follows) {
+      next = segment_at(u);
+      next_ids = pages_from(next, next.b0);
+    }
+    if (!begun) {
+      begun = true;
+      continue;
+    }
+    const int b0 = g.b0, b1 = g.b1, kv = g.kv, group = g.group, rows = g.rows;
+    const int r = min(n16, rows - 1), at = g.rt * ROWS + r, token = at / group, in_group = at - token * group;
     const int head = heads.head(kv, in_group);
-    const int keys = min(q.past + q.n, c.cap);
-    const int see = min(q.past + token, keys - 1);                                             // the row's last key
-    const int see_all = min(q.past + rt * ROWS / group, keys - 1), see_any = min(q.past + (rt * ROWS + rows - 1) / group, keys - 1);
-    const long long out = (long long)head * dh * p.ldc + q.begin + token;
+    const int see = min(g.past + token, g.keys - 1);                                           // the row's last key
+    const int see_all = min(g.past + g.rt * ROWS / group, g.keys - 1), see_any = min(g.past + (g.rt * ROWS + rows - 1) / group, g.keys - 1);
+    const long long out = (long long)head * dh * p.ldc + g.begin + token;
 
-    // the row's query as the second operand
-    int width = dh, quarter = quad;
-    asm volatile("" : "+s"(width), "+v"(quarter));        // what this works out is not worth registers for the rest of the kernel
-    const E* Qp = (const E*)p.Q + (long long)head * dh * p.ldq + q.begin + token;
-    uintx4 qb[BF ? NC : 1];
-    float qf[BF ? 1 : (Q4 ? NC * 8 : NC * 4)];
-    float qsum = 0.0f;
-    if constexpr (BF) {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        unsigned short e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          // of 4 bits a lane has channels 8 NC apart where its heads are whole, with channel j beside j + 4
-          const int ch = Q4 ? (width == DH ? 8 * NC * quarter + 8 * i : 32 * i + 8 * quarter) + (j >> 1) + 4 * (j & 1) : 32 * i + 8 * quarter + j;
-          e[j] = ((const unsigned short*)Qp)[(long long)(ch < width ? ch : 0) * p.ldq];
-          e[j] = ch < width ? e[j] : (unsigned short)0;
-          if constexpr (Q4) qsum += __builtin_bit_cast(float, (unsigned)e[j] << 16);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) qb[i][j] = (unsigned)e[2 * j] | (unsigned)e[2 * j + 1] << 16;
-        __builtin_amdgcn_sched_barrier(0);       // not every address at once, for the registers
-      }
-    } else {
-      constexpr int PER = Q4 ? 8 : 4;
-#pragma unroll
-      for (int i = 0; i < NC; ++i)
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-          const int ch = Q4 ? (width == DH ? 8 * NC * quarter + 8 * i : 32 * i + 8 * quarter) + j : 16 * i + 4 * quarter + j;
-          const float x = ((const float*)Qp)[(long long)(ch < width ? ch : 0) * p.ldq];
-          qf[i * PER + j] = ch < width ? x : 0.0f;
-          if constexpr (Q4) qsum += qf[i * PER + j];
-          if (j == PER - 1) __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    if constexpr (Q4) qsum = quads_sum(qsum);
-
-    // pages of the wavefront's keys: lane l has that of tile l % NT of its keys in block bt + l / NT
-    const int32_t* table = c.table + (long long)s * c.ld_table;
-    int ids = 0, bt = b0;
-    auto look_up = [&](int b) {
-      const int key = (b + lane / NT) * UNIT + wave * KW + (lane % NT) * 16;
-      ids = clamped(table[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
-    };
-    const int in_page = (1 << c.page_log2) - 1;
-    auto tile_row = [&](int b, int t) {    // the row of the cache that the wavefront's tile t of block b begins at
-      const int page = __builtin_amdgcn_readlane(ids, NT * (b - bt) + t);
-      return (((long long)page * c.kv_heads + kv) << c.page_log2) + ((b * UNIT + wave * KW + t * 16) & in_page);
-    };
-
-    TileT T[NT];
-    auto load_k = [&](int b) {
+    // the rows of the cache that the wavefront's tiles of unit b begin at
+    struct Places { long long row[NT]; };
+    auto places = [&](int of, int kv_head, int b, int from) {
+      Places x;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const long long row = tile_row(b, t);
+        const int page = __builtin_amdgcn_readlane(of, NT * (b - from) + t);
+        x.row[t] = (((long long)page * c.kv_heads + kv_head) << c.page_log2) + ((b * UNIT + wave * KW + t * 16) & in_page);
+      }
+      return x;
+    };
+    auto load_k = [&](const Places& at) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const long long row = at.row[t];
         if constexpr (!Q4) {
-          const char* g = opaque((const char*)p.K + row * (dh * (int)sizeof(E)));
+          const auto g = opaque((const char*)p.K + row * (dh * (int)sizeof(E)));
           constexpr int CH = BF ? 32 : 16, LN = CH / 4;
 #pragma unroll
           for (int i = 0; i < NC; ++i) {
             const int ch = CH * i + LN * quad;
-            T[t].k[i] = *(const typename TileT::Key*)(g + (unsigned)(n16 * dh + (ch < dh ? ch : 0)) * (unsigned)sizeof(E));
+            T[t].k[i] = *(Global<typename TileT::Key>)(g + (unsigned)(n16 * dh + (ch < dh ? ch : 0)) * (unsigned)sizeof(E));
           }
         } else {
-          const char* g = opaque((const char*)p.K + row * (dh / 2));
+          const auto g = opaque((const char*)p.K + row * (dh / 2));
           if (dh == DH) {
             typedef unsigned vec __attribute__((ext_vector_type(NC)));
-            const vec x = *(const vec*)(g + (unsigned)(n16 * (DH / 2) + 4 * NC * quad));
+            const vec x = *(Global<vec>)(g + (unsigned)(n16 * (DH / 2) + 4 * NC * quad));
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
               if constexpr (NC == 1) T[t].k[i] = x[0];
@@ -227,70 +216,114 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
               const int ch = 32 * i + 8 * quad;
-              T[t].k[i] = *(const unsigned*)(g + (unsigned)(n16 * (dh / 2) + (ch < dh ? ch : 0) / 2));
+              T[t].k[i] = *(Global<unsigned>)(g + (unsigned)(n16 * (dh / 2) + (ch < dh ? ch : 0) / 2));
             }
           }
-          const floatx4* sc = (const floatx4*)(opaque((const char*)(p.sK + (row >> 1))) + 32u * (unsigned)quad);
+          const auto sc = (Global<floatx4>)(opaque(p.sK + (row >> 1)) + 32u * (unsigned)quad);
           T[t].ks[0] = sc[0];
           T[t].ks[1] = sc[1];
         }
       }
     };
-    auto load_v = [&](int b) {
+    auto load_v = [&](const Places& at) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const long long row = tile_row(b, t);
+        const long long row = at.row[t];
         const int ch = W * n16 < dh ? W * n16 : 0;
-        const char* rows_at = opaque((const char*)p.V + (Q4 ? row * (dh / 2) : row * (dh * (int)sizeof(E))));
+        const auto rows_at = opaque((const char*)p.V + (Q4 ? row * (dh / 2) : row * (dh * (int)sizeof(E))));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if constexpr (!Q4) {
-            const E* g = (const E*)(rows_at + (unsigned)((4 * quad + e) * dh + ch) * (unsigned)sizeof(E));
+            const auto g = rows_at + (unsigned)((4 * quad + e) * dh + ch) * (unsigned)sizeof(E);
             if constexpr (BF) {
               typedef unsigned vec __attribute__((ext_vector_type(W / 2)));
-              const vec x = *(const vec*)g;
+              const vec x = *(Global<vec>)g;
 #pragma unroll
               for (int j = 0; j < W / 2; ++j) {
                 if constexpr (W == 2) T[t].v[e][j] = x[0];
                 else T[t].v[e][j] = x[j];
               }
             } else {
-              load_floats<(W < 4 ? W : 4)>(g, *(float(*)[W < 4 ? W : 4]) & T[t].v[e][0]);
-              if constexpr (W == 8) load_floats<4>(g + 4, *(float(*)[4]) & T[t].v[e][4]);
+              constexpr int PART = W < 4 ? W : 4;
+              typedef float vec __attribute__((ext_vector_type(PART)));
+#pragma unroll
+              for (int i = 0; i < W; i += PART) {
+                const vec x = *(Global<vec>)(g + 4 * i);
+#pragma unroll
+                for (int j = 0; j < PART; ++j) T[t].v[e][i + j] = x[j];
+              }
             }
           } else {
-            const char* g = rows_at + (unsigned)((4 * quad + e) * (dh / 2) + ch / 2);
-            if constexpr (W == 8) T[t].v[e] = *(const unsigned*)g;
-            else if constexpr (W == 4) T[t].v[e] = *(const unsigned short*)g;
-            else T[t].v[e] = *(const unsigned char*)g;
+            const auto g = rows_at + (unsigned)((4 * quad + e) * (dh / 2) + ch / 2);
+            if constexpr (W == 8) T[t].v[e] = *(Global<unsigned>)g;
+            else if constexpr (W == 4) T[t].v[e] = *(Global<unsigned short>)g;
+            else T[t].v[e] = *(Global<unsigned char>)g;
           }
         }
         if constexpr (Q4) {
-          const floatx4* sc = (const floatx4*)(opaque((const char*)(p.sV + (row >> 1))) + 32u * (unsigned)quad);
+          const auto sc = (Global<floatx4>)(opaque(p.sV + (row >> 1)) + 32u * (unsigned)quad);
           T[t].vs[0] = sc[0];
           T[t].vs[1] = sc[1];
         }
       }
     };
 
+    if (!loaded) {
+      const Places first = places(ids, kv, b0, b0);
+      load_k(first);
+      load_v(first);
+    }
+    // the row's query as the second operand
+    int width = dh, quarter = quad;
+    asm volatile("" : "+s"(width), "+v"(quarter));        // what this works out is not worth registers for the rest of the kernel
+    const E* Qp = (const E*)p.Q + (long long)head * dh * p.ldq + g.begin + token;
+    uintx4 qb[BF ? NC : 1];
+    float qf[BF ? 1 : (Q4 ? NC * 8 : NC * 4)];
+    float qsum = 0.0f;
+    {
+      constexpr int PER = BF || Q4 ? 8 : 4;
+      // of 4 bits a lane has channels 8 NC apart where its heads are whole; products of bf16 have channel j beside j + 4
+      auto channel = [&](int i, int j) {
+        if constexpr (!Q4) return (BF ? 32 : 16) * i + PER * quarter + j;
+        else return (width == DH ? 8 * NC * quarter + 8 * i : 32 * i + 8 * quarter) + (BF ? (j >> 1) + 4 * (j & 1) : j);
+      };
+      E x[NC][PER];
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const int ch = channel(i, j);
+          x[i][j] = Qp[(long long)(ch < width ? ch : 0) * p.ldq];
+        }
+      __builtin_amdgcn_sched_barrier(0);         // all of them asked for before any is waited for
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          x[i][j] = channel(i, j) < width ? x[i][j] : (E)0.0f;
+          if constexpr (!BF) qf[i * PER + j] = x[i][j];
+          if constexpr (Q4) qsum += (float)x[i][j];
+        }
+        if constexpr (BF) {
+          typedef __bf16 pairs __attribute__((ext_vector_type(8)));
+          qb[i] = __builtin_bit_cast(uintx4, pairs{x[i][0], x[i][1], x[i][2], x[i][3], x[i][4], x[i][5], x[i][6], x[i][7]});
+        }
+      }
+    }
+    if constexpr (Q4) qsum = quads_sum(qsum);
+
     floatx4 O[W];
     float m, l, weight, lowest;            // weight: sum of what the values were multiplied by (of 4 bits: to take 128 off again); lowest: of p lowest
     bool careful = false, odd;
+    // the wavefront's units that some row sees
+    const int keys_of_wave = see_any - wave * KW;
+    const int be = keys_of_wave < 0 ? b0 : min(b1, keys_of_wave / UNIT + 1);
     while (true) {
       odd = false;
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
       m = -INFINITY;
       l = weight = lowest = 0.0f;
-      // the wavefront's blocks that some row sees
-      const int keys_of_wave = see_any - wave * KW;
-      const int be = keys_of_wave < 0 ? b0 : min(b1, keys_of_wave / UNIT + 1);
-      if (b0 < be) {
-        bt = b0;
-        look_up(bt);
-        load_k(b0);
-        load_v(b0);
-      }
 #pragma unroll 1
       for (int b = b0; b < be; ++b) {
         const int k0 = b * UNIT + wave * KW;
@@ -336,14 +369,22 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[t][e] = __builtin_fmaf(S[t][e], T[t].ks[e >> 1][2 * (e & 1) + 1], qsum * T[t].ks[e >> 1][2 * (e & 1)]);
         }
+        // the next unit, or the next segment's first
         const bool more = b + 1 < be;
+        Places to;
         if (more) {
           if (b + 1 - bt == 64 / NT) {
             bt = b + 1;
-            look_up(bt);
+            ids = pages_from(g, bt);
           }
-          load_k(b + 1);
+          to = places(ids, kv, b + 1, bt);
+        } else if (follows) {
+          to = places(next_ids, next.kv, next.b0, next.b0);
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) to.row[t] = 0;      // what all read at their ends: were these loads left out, those before them would have to be waited for together
         }
+        load_k(to);
         // the softmax: lane (row, quad) has the keys 4 quad .. + 4 of both tiles
         const bool whole = k0 + KW - 1 <= see_all;
         if (!whole)
@@ -455,7 +496,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
                 O[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, P[t][e], O[j], 0, 0, 0);
               }
         }
-        if (more) load_v(b + 1);
+        load_v(to);
       }
       if constexpr (!Q4) {
         if (__builtin_amdgcn_ballot_w64(odd)) {
@@ -468,14 +509,14 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
             for (int key = k0; key < k0 + KW && key <= see_any; ++key) {
               int width = dh, from = 4 * W * quad;
               asm volatile("" : "+s"(width), "+v"(from));
-              const int page = clamped(table[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
-              const E* g = (const E*)p.V + ((((long long)page * c.kv_heads + kv) << c.page_log2) + (key & in_page)) * dh;
+              const int page = clamped((c.table + (long long)g.s * c.ld_table)[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
+              const E* values = (const E*)p.V + ((((long long)page * c.kv_heads + kv) << c.page_log2) + (key & in_page)) * dh;
 #pragma unroll
               for (int j = 0; j < W; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const int ch = from + W * e + j;
-                  const float v = (float)g[ch < width ? ch : 0];
+                  const float v = (float)values[ch < width ? ch : 0];
                   O[j][e] += key <= see && !(fabsf(v) < INFINITY) ? v : 0.0f;
                   __builtin_amdgcn_sched_barrier(0);
                 }
@@ -492,7 +533,15 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
         for (int e = 0; e < 4; ++e) most = __builtin_elementwise_maximum(most, fabsf(O[j][e]));
       if (!__builtin_amdgcn_ballot_w64(!(most < INFINITY))) break;
       careful = true;
+      if (b0 < be) {
+        bt = b0;
+        ids = pages_from(g, b0);
+        const Places first = places(ids, kv, b0, b0);
+        load_k(first);
+        load_v(first);
+      }
     }
+    loaded = follows && b0 < be;
 
     // ---- the four wavefronts together ----
     l = quads_sum(l);
@@ -524,7 +573,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
         f[w] = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mw - M) * p.scale_log2e);      // a wavefront that saw no key has zeros
         L += f[w] * sL[w][row];
       }
-      const bool whole_row = b0 == 0 && b1 == q.units;
+      const bool whole_row = b0 == 0 && b1 == g.units;
       const long long to = sOff[row];
       const int slot = worker * 2 + (b0 == 0 ? 1 : 0);
       if (to >= 0) {
@@ -540,11 +589,8 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
         }
       }
       // the workgroups from this one to that with the tile's last unit
-      if (!whole_row && b0 == 0 && tid == 0) p.parts[worker] = (int)((u - b0 + q.units - 1) / per) - worker + 1;
+      if (!whole_row && b0 == 0 && tid == 0) p.parts[worker] = (int)((u - b1 + g.units - 1) / per) - worker + 1;      // (u: where this one ends)
     }
-    u += b1 - b0;
-    if (u >= u1) break;
-    while (u >= base + (long long)q.units * q.tiles) next_sequence();
   }
 }
 

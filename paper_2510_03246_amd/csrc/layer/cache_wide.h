@@ -160,9 +160,13 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int ch = 16 * d + 8 * half + e;
-          const __bf16 v = Q[(long long)(ch < width ? ch : 0) * p.ldq];
-          qf[d][e] = ch < width ? v : (__bf16)0.0f;
+          qf[d][e] = Q[(long long)(ch < width ? ch : 0) * p.ldq];
         }
+      __builtin_amdgcn_sched_barrier(0);                                   // all of them asked for before any is waited for
+#pragma unroll
+      for (int d = 0; d < NS; ++d)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qf[d][e] = 16 * d + 8 * half + e < width ? qf[d][e] : (__bf16)0.0f;
     }
 
     // pages of the wavefront's 16 keys of a unit: lane l has that of unit bt + l
@@ -178,12 +182,18 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       to += (unsigned)wave * (16 * PITCH);
       int mine = lane, width = dh;
       asm volatile("" : "+v"(mine), "+s"(width));        // worked out each time, for the registers
+      auto piece = [&](int i) { return mine / CHUNKS + EACH * i; };      // its row
+      auto chunk_of = [&](int row) { return (mine % CHUNKS) ^ (of_k ? order_k(row) : order_v(row)); };
+      if (full) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int rr = mine / CHUNKS + EACH * i, chunk = (mine % CHUNKS) ^ (of_k ? order_k(rr) : order_v(rr));
-        if (full) copy_to_lds_from(from, (unsigned)(rr * PITCH + chunk * 16), to + 1024 * i);
-        else copy_to_lds(8 * chunk < width ? (const void*)(from + (unsigned)(rr * width + chunk * 8) * 2u) : (const void*)cache_zero_chunk, to + 1024 * i);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < LOADS; ++i) copy_to_lds_from(from, (unsigned)(piece(i) * PITCH + chunk_of(piece(i)) * 16), to + 1024 * i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int row = piece(i), chunk = chunk_of(row);
+          copy_to_lds(8 * chunk < width ? (const void*)(from + (unsigned)(row * width + chunk * 8) * 2u) : (const void*)cache_zero_chunk, to + 1024 * i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     };
     unsigned toK, toV, atK, atV;           // where the next tile goes, and is read

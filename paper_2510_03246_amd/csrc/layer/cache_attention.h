@@ -70,7 +70,7 @@ template <typename T>
 using Global = const __attribute__((address_space(1))) T*;
 // a base that stays in scalar registers beside its lanes' offsets (or the sums of both that do not change are kept in vector registers, two for an address)
 __device__ __forceinline__ Global<char> opaque(const void* p) {
-  Global<char> g = (Global<char>)p;
+  Global<char> g = (Global<char>)uniform((long long)p);
   asm("" : "+s"(g));
   return g;
 }

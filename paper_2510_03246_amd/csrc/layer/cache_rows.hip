@@ -56,9 +56,13 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
   typedef Tile<E, Q4, W> TileT;
   constexpr int NC = TileT::NC, DH = 16 * W;
   constexpr int NT = BF || Q4 ? 2 : 1, KW = 16 * NT, UNIT = 4 * KW;      // tiles and keys of a wavefront in a unit, keys of a unit
+  constexpr int EXTRA = 2;                 // units that a tile counts beyond its keys'
   auto& sO = ((RowsLds<W>*)smem)->o;
   __shared__ float sM[4][ROWS], sL[4][ROWS];
   __shared__ long long sOff[ROWS];
+  constexpr int HELD = 512;
+  __shared__ int sBegin[HELD + 1], sPast[HELD];
+  __shared__ __attribute__((aligned(16))) E sQ[ROWS][DH + 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quad = lane >> 4;
   const Pages& c = p.c;
   const int dh = c.dh;
@@ -72,13 +76,21 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     for (int g = 0; g < c.kv_heads; ++g) sum += tiles_of(n, heads.of(g));
     return sum;
   };
+  const bool held = c.n_seq <= HELD;
+  if (held) {
+    for (int i = tid; i <= c.n_seq; i += 256) {
+      sBegin[i] = seq_begin(c, i);
+      if (i < c.n_seq) sPast[i] = seq_past(c, i);
+    }
+    __syncthreads();
+  }
   struct Seq { int begin, n, past, units, tiles; };
   auto sequence = [&](int s) {
     Seq q;
-    q.begin = seq_begin(c, s);
-    q.n = max(seq_begin(c, s + 1) - q.begin, 0);
-    q.past = seq_past(c, s);
-    q.units = q.n ? (min(q.past + q.n, c.cap) + UNIT - 1) / UNIT : 0;
+    q.begin = held ? sBegin[s] : seq_begin(c, s);
+    q.n = max((held ? sBegin[s + 1] : seq_begin(c, s + 1)) - q.begin, 0);
+    q.past = held ? sPast[s] : seq_past(c, s);
+    q.units = q.n ? (min(q.past + q.n, c.cap) + UNIT - 1) / UNIT + EXTRA : 0;
     q.tiles = q.n ? all_tiles(q.n) : 0;
     return q;
   };
@@ -122,14 +134,16 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 
   // A segment: units b0 .. b1 of one tile of rows.  The one behind it is known while it is worked on: its first keys and values are on their way before the last ones here are done
   // with, or nothing would be read while the wavefronts join their results (64 sequences of 0 to 4000 tokens, two segments a workgroup: 137 us instead of AAA).
-  struct Segment { int s, begin, past, keys, units, kv, rt, group, rows, b0, b1; };
+  struct Segment { int s, begin, past, keys, units, kv, rt, group, rows, b0, b1, all; long long last; };      // all: units of the share; last: the tile's last one
   auto segment_at = [&](long long u) {
     while (u >= base + (long long)q.units * q.tiles) next_sequence();
-    Segment g{s, q.begin, q.past, min(q.past + q.n, c.cap), q.units, 0, 0, 0, 0, 0, 0};
+    Segment g{s, q.begin, q.past, min(q.past + q.n, c.cap), q.units - EXTRA, 0, 0, 0, 0, 0, 0, 0, 0};
     const long long rel = u - base;
-    const int row_tile = (int)(rel / q.units);
-    g.b0 = (int)(rel - (long long)row_tile * q.units);
-    g.b1 = (long long)q.units - g.b0 < u1 - u ? q.units : g.b0 + (int)(u1 - u);
+    const int row_tile = (int)(rel / q.units), from = (int)(rel - (long long)row_tile * q.units), to = (long long)q.units - from < u1 - u ? q.units : from + (int)(u1 - u);
+    g.b0 = max(from - EXTRA, 0);
+    g.b1 = max(to - EXTRA, 0);
+    g.all = to - from;
+    g.last = u - from + q.units - 1;
     g.rt = row_tile;
     if (!heads.first) {
       const int per_kv = tiles_of(q.n, heads.group);
@@ -150,31 +164,65 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
   // pages of the wavefront's keys: lane l has that of tile l % NT of its keys in unit b + l / NT
   auto pages_from = [&](const Segment& g, int b) {
     const int key = (b + lane / NT) * UNIT + wave * KW + (lane % NT) * 16;
-    return clamped((c.table + (long long)g.s * c.ld_table)[min(key >> c.page_log2, c.ld_table - 1)], 0, c.pages - 1);
+    return (c.table + (long long)g.s * c.ld_table)[min(key >> c.page_log2, c.ld_table - 1)];      // brought into its range where it is used, not to wait for it here
+  };
+  // A segment's queries: asked for while the one before is worked on, then turned round through LDS; a wavefront has a fourth of the channels.
+  // Of 4 bits, products of bf16 have channel j beside j + 4.
+  struct Queries { E x[W]; };
+  struct Row { int token, head; };
+  auto row_of = [&](const Segment& g, int r) {
+    const int at = g.rt * ROWS + min(r, g.rows - 1), token = at / g.group;
+    return Row{token, heads.head(g.kv, at - token * g.group)};
+  };
+  auto ask_queries = [&](const Segment& g) {
+    Queries q;
+    const Row r = row_of(g, n16);
+    int width = dh, first = (4 * wave + quad) * W;
+    asm volatile("" : "+s"(width), "+v"(first));          // what this works out is not worth registers for the rest of the kernel
+    const E* from = (const E*)p.Q + (long long)r.head * dh * p.ldq + g.begin + r.token;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      const int at = first + j, ch = BF && Q4 ? (at & ~7) + ((at & 7) >> 1) + 4 * (at & 1) : at;
+      q.x[j] = from[(long long)(ch < width ? ch : 0) * p.ldq];
+    }
+    return q;
+  };
+  auto put_queries = [&](const Queries& q) {
+    typedef E vec __attribute__((ext_vector_type(W)));
+    vec v;
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = ((4 * wave + quad) * W + j & ~7) < dh ? q.x[j] : (E)0.0f;      // (heads are whole eights)
+    *(vec*)&sQ[n16][(4 * wave + quad) * W] = v;
   };
   const int in_page = (1 << c.page_log2) - 1;
 
   TileT T[NT];
   Segment g{}, next{};
+  Queries queries{};
   int next_ids = 0;
-  bool begun = false, loaded = false;      // loaded: the segment's first keys and values are here or on their way
+  bool begun = false, first = false, loaded = false;      // loaded: the segment's first keys and values are here or on their way
   while (true) {
     if (begun && u >= u1) break;
     g = next;
     int ids = next_ids, bt = g.b0;
-    if (begun) u += g.b1 - g.b0;           // where the next one begins
-    const bool follows = u < u1;
-    if (follows) {
-      next = segment_at(u);
-      next_ids = pages_from(next, next.b0);
+    if (begun) u += g.all;                 // where the next one begins
+    if (u < u1) next = segment_at(u);
+    // a share may begin or end among the units that a tile counts beyond its keys
+    while (u < u1 && next.b1 == 0) {
+      u += next.all;
+      if (u < u1) next = segment_at(u);
     }
+    const bool follows = u < u1;
     if (!begun) {
-      begun = true;
+      if (!follows) break;
+      next_ids = pages_from(next, next.b0);
+      queries = ask_queries(next);
+      begun = first = true;
       continue;
     }
     const int b0 = g.b0, b1 = g.b1, kv = g.kv, group = g.group, rows = g.rows;
-    const int r = min(n16, rows - 1), at = g.rt * ROWS + r, token = at / group, in_group = at - token * group;
-    const int head = heads.head(kv, in_group);
+    const Row row = row_of(g, n16);
+    const int token = row.token, head = row.head;
     const int see = min(g.past + token, g.keys - 1);                                           // the row's last key
     const int see_all = min(g.past + g.rt * ROWS / group, g.keys - 1), see_any = min(g.past + (g.rt * ROWS + rows - 1) / group, g.keys - 1);
     const long long out = (long long)head * dh * p.ldc + g.begin + token;
@@ -185,7 +233,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
       Places x;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const int page = __builtin_amdgcn_readlane(of, NT * (b - from) + t);
+        const int page = clamped(__builtin_amdgcn_readlane(of, NT * (b - from) + t), 0, c.pages - 1);
         x.row[t] = (((long long)page * c.kv_heads + kv_head) << c.page_log2) + ((b * UNIT + wave * KW + t * 16) & in_page);
       }
       return x;
@@ -273,40 +321,37 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
       load_k(first);
       load_v(first);
     }
-    // the row's query as the second operand
-    int width = dh, quarter = quad;
-    asm volatile("" : "+s"(width), "+v"(quarter));        // what this works out is not worth registers for the rest of the kernel
-    const E* Qp = (const E*)p.Q + (long long)head * dh * p.ldq + g.begin + token;
+    if (first) {
+      put_queries(queries);
+      __syncthreads();
+      first = false;
+    }
+    if (follows) {
+      next_ids = pages_from(next, next.b0);
+      queries = ask_queries(next);
+    }
+    // the row's query as the second operand; of 4 bits a lane has channels 8 NC apart where its heads are whole
     uintx4 qb[BF ? NC : 1];
     float qf[BF ? 1 : (Q4 ? NC * 8 : NC * 4)];
     float qsum = 0.0f;
-    {
-      constexpr int PER = BF || Q4 ? 8 : 4;
-      // of 4 bits a lane has channels 8 NC apart where its heads are whole; products of bf16 have channel j beside j + 4
-      auto channel = [&](int i, int j) {
-        if constexpr (!Q4) return (BF ? 32 : 16) * i + PER * quarter + j;
-        else return (width == DH ? 8 * NC * quarter + 8 * i : 32 * i + 8 * quarter) + (BF ? (j >> 1) + 4 * (j & 1) : j);
-      };
-      E x[NC][PER];
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
+    for (int i = 0; i < NC; ++i) {
+      const int eight = Q4 && dh == DH ? NC * quad + i : 4 * i + quad;
+      if constexpr (BF) {
+        qb[i] = *(const uintx4*)&sQ[n16][8 * eight];
+        if constexpr (Q4)
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-          const int ch = channel(i, j);
-          x[i][j] = Qp[(long long)(ch < width ? ch : 0) * p.ldq];
-        }
-      __builtin_amdgcn_sched_barrier(0);         // all of them asked for before any is waited for
+          for (int d = 0; d < 4; ++d) qsum += __builtin_bit_cast(float, qb[i][d] << 16) + __builtin_bit_cast(float, qb[i][d] & 0xffff0000u);
+      } else {
+        constexpr int PER = Q4 ? 8 : 4;
 #pragma unroll
-      for (int i = 0; i < NC; ++i) {
+        for (int j = 0; j < PER; j += 4) {
+          const floatx4 x = *(const floatx4*)&sQ[n16][PER * eight + j];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-          x[i][j] = channel(i, j) < width ? x[i][j] : (E)0.0f;
-          if constexpr (!BF) qf[i * PER + j] = x[i][j];
-          if constexpr (Q4) qsum += (float)x[i][j];
-        }
-        if constexpr (BF) {
-          typedef __bf16 pairs __attribute__((ext_vector_type(8)));
-          qb[i] = __builtin_bit_cast(uintx4, pairs{x[i][0], x[i][1], x[i][2], x[i][3], x[i][4], x[i][5], x[i][6], x[i][7]});
+          for (int e = 0; e < 4; ++e) {
+            qf[i * PER + j + e] = x[e];
+            if constexpr (Q4) qsum += x[e];
+          }
         }
       }
     }
@@ -551,7 +596,8 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j] += lowest;
     }
-    __syncthreads();                       // the segment before has been read
+    __syncthreads();                       // the segment before has been read, and this one's queries
+    if (follows) put_queries(queries);
     if (quad == 0) {
       sM[wave][n16] = m;
       sL[wave][n16] = l;
@@ -589,7 +635,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
         }
       }
       // the workgroups from this one to that with the tile's last unit
-      if (!whole_row && b0 == 0 && tid == 0) p.parts[worker] = (int)((u - b1 + g.units - 1) / per) - worker + 1;      // (u: where this one ends)
+      if (!whole_row && b0 == 0 && tid == 0) p.parts[worker] = (int)(g.last / per) - worker + 1;
     }
   }
 }

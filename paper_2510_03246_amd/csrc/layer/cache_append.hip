@@ -362,7 +362,8 @@ static void launch_append(strp_ctx* ctx, AppendP p) {
   p.items = 2 * p.c.kv_heads + (p.Q ? p.heads : 0);
   // sine and cosine are worked out once for the heads of a workgroup: as many heads as leave the chip four workgroups a CU
   const long long wgs = (long long)tiles * p.items;
-  p.per = (int)(wgs / 1024 < 1 ? 1 : wgs / 1024 < 16 ? wgs / 1024 : 16);
+  const long long resident = few ? 1024 : p.c.dh > 64 ? 768 : 1024, per = (wgs + resident - 1) / resident;
+  p.per = (int)(per < 8 ? per : 8);
   const dim3 grid((unsigned)tiles, (unsigned)((p.items + p.per - 1) / p.per));
   const auto go = [&](auto width) {
     constexpr int DHP = decltype(width)::value;

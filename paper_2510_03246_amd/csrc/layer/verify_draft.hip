@@ -14,40 +14,48 @@ namespace strp {
 
 constexpr int SLICES = 256, PARTS = 256;   // at most: a lane has four of either
 
-// e^y for y from -705 to 600, to 2^-48 of itself (and where y is far below zero, and nothing hangs on it, to 2^-44).  y = (32 k + j) ln 2 / 32 + r with
-// |r| <= ln 2 / 64, so that e^y = 2^k 2^(j/32) e^r: a table of 32 in LDS, which 64 banks give to any lanes at once, and the series to r^5.  12 instructions in
-// 64 bits (without the table and to r^12: 22, and verify_256 took 445 us instead of 224).
-struct Exp {
-  const double* table;
-  __device__ __forceinline__ double near(double y) const {
-    constexpr double ROUND = 6755399441055744.0;                    // 1.5 2^52: what is added to it is rounded to whole numbers, which its lower bits then have
-    const double t = __builtin_fma(y, 46.16624130844682904, ROUND), n = t - ROUND;
-    const double r = __builtin_fma(n, -2.1660849392498290836e-02, y);
-    double p = __builtin_fma(r, 1.0 / 120.0, 1.0 / 24.0);
-    p = __builtin_fma(p, r, 1.0 / 6.0);
-    p = __builtin_fma(p, r, 0.5);
-    p = __builtin_fma(p, r, 1.0) * r;
-    const unsigned i = (unsigned)__builtin_bit_cast(unsigned long long, t);
-    const double b = table[i & 31];
-    const unsigned long long e = __builtin_bit_cast(unsigned long long, __builtin_fma(b, p, b));
-    const unsigned high = (unsigned)(e >> 32) + ((i & ~31u) << 15);      // k into the exponent
-    return __builtin_bit_cast(double, (unsigned long long)high << 32 | (unsigned)e);
-  }
-  // 0 where y is below -700 or NaN
-  __device__ __forceinline__ double operator()(double y) const { return y >= -700.0 ? near(y) : 0.0; }
-};
-constexpr double LN2 = 0.69314718055994530942;
-// 2^(j/32), j < 32, by the series of e^x on [0, ln 2)
-__device__ __forceinline__ void fill_table(double* table) {
-  if (threadIdx.x < 32) {
-    const double x = threadIdx.x * (LN2 / 32.0);
+// e^y to 2^-43 of itself, for y from -705 to 600, in units of ln 2 / 32: y = 32 k + j + r with |r| <= 1/2, so that e^y = 2^k 2^(j/32) 2^(r/32): a table of 32 in LDS, which 64 banks
+// give to any lanes at once, and a polynomial of the fourth degree (the series to r^5 with that power taken for the nearest lower ones on the interval, a Chebyshev polynomial less).
+// 10 instructions in 64 bits (without the table and to r^12: 22, and verify_256 took 445 us instead of 224).
+constexpr double LN2 = 0.69314718055994530942, UNITS = 32.0 / LN2;      // of ln 2 / 32 in one
+constexpr double LOWEST = -700.0 * UNITS;
+struct ExpTable { double of[32]; };
+constexpr ExpTable exp_table() {           // 2^(j/32), j < 32, by the series of e^x on [0, ln 2)
+  ExpTable t{};
+  for (int j = 0; j < 32; ++j) {
     double s = 1.0;
-#pragma unroll
-    for (int k = 18; k > 0; --k) s = __builtin_fma(s, x / (double)k, 1.0);
-    table[threadIdx.x] = s;
+    for (int k = 22; k > 0; --k) s = 1.0 + s * (j / UNITS) / k;
+    t.of[j] = s;
   }
+  return t;
+}
+__device__ const ExpTable exp_values = exp_table();
+__device__ __forceinline__ void fill_table(double* table) {
+  if (threadIdx.x < 32) table[threadIdx.x] = __builtin_bit_cast(double, __builtin_bit_cast(unsigned long long, exp_values.of[threadIdx.x]) - ((unsigned long long)threadIdx.x << 47));
   __syncthreads();
 }
+struct Exp {
+  const double* table;
+  __device__ __forceinline__ double near(double y) const {          // y in units
+    constexpr double ROUND = 6755399441055744.0;                    // 1.5 2^52: what is added to it is rounded to whole numbers, which its lower bits then have
+    constexpr double L = 1.0 / UNITS, A = 0.5 * L, C1 = L * (1.0 - 5.0 * A * A * A * A / 1920.0), C2 = L * L / 2.0, C3 = L * L * L * (1.0 / 6.0 + 20.0 * A * A / 1920.0), C4 = L * L * L * L / 24.0;
+    const double t = y + ROUND, r = y - (t - ROUND);
+    double p = __builtin_fma(r, C4, C3);
+    p = __builtin_fma(p, r, C2);
+    p = __builtin_fma(p, r, C1) * r;
+    const unsigned i = (unsigned)__builtin_bit_cast(unsigned long long, t);
+    // k and j, whole, into the exponent and behind it: the table has j taken off there
+    const unsigned long long of = __builtin_bit_cast(unsigned long long, table[i & 31]);
+    const unsigned high = (unsigned)(of >> 32) + (i << 15);
+    const double b = __builtin_bit_cast(double, (unsigned long long)high << 32 | (unsigned)of);
+    return __builtin_fma(b, p, b);
+  }
+  // 0 where y is below -700 or NaN
+  __device__ __forceinline__ double operator()(double y) const {
+    const double x = y * UNITS;
+    return x >= LOWEST ? near(x) : 0.0;
+  }
+};
 
 // Sum of e^((x - ref) / temperature) over some entries.  ref is one of them and no more than 500 temperatures below any: with 64 bits it need not be the largest.
 // most: the largest, NaN where there is one.
@@ -80,7 +88,7 @@ struct VerifyP {
 
 template <typename E>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
-  constexpr int VEC = 16 / sizeof(E), UN = 4;
+  constexpr int VEC = 16 / sizeof(E), UN = 2;
   __shared__ double table[32];
   __shared__ double sSum[4][8][VEC];
   __shared__ float sRef[4][8][VEC], sMost[4][8][VEC];
@@ -90,7 +98,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
   const int c = threadIdx.x % p.ct, r = threadIdx.x / p.ct, rl = 256 / p.ct, wave = threadIdx.x >> 6;
   const long long t0 = ((long long)((int)blockIdx.x - (of_draft ? p.groups_t : 0)) * p.ct + c) * VEC, ld = of_draft ? p.ldd : p.ldt;
   const int n = of_draft ? p.T : p.columns, v0 = (int)blockIdx.y * p.rows, v1 = min(v0 + p.rows, p.V);
-  double sum[VEC], from[VEC];              // from: ref / temperature
+  double sum[VEC], from[VEC];              // from: ref / temperature, in the units of Exp
   float ref[VEC], most[VEC], high[VEC];    // high: what ref may not stay behind
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
@@ -98,13 +106,25 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
     ref[e] = most[e] = high[e] = -INFINITY;
   }
   const float reach = (float)(500.0 / p.inv);
+  const double scale = p.inv * UNITS;
   if (t0 < n) {
     const E* x = (const E*)(of_draft ? p.draft : p.target) + t0;
-    auto take = [&](auto count, int v) {
+    typedef E vec __attribute__((ext_vector_type(VEC)));
+    struct Rows { vec x[UN]; };
+    // rows v, v + rl, ..: asked for while those before them are worked on
+    auto ask = [&](int v) {
+      Rows rows;
+#pragma unroll
+      for (int k = 0; k < UN; ++k) rows.x[k] = *(const vec*)(x + (long long)min(v + k * rl, v1 - 1) * ld);
+      return rows;
+    };
+    auto take = [&](auto count, const Rows& rows) {
       constexpr int N = decltype(count)::value;
       float f[N][VEC];
 #pragma unroll
-      for (int k = 0; k < N; ++k) load_floats<VEC>(x + (long long)(v + k * rl) * ld, f[k]);
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[k][e] = (float)rows.x[k][e];
       bool far = false;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -121,17 +141,30 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
             sum[e] *= ref[e] == -INFINITY ? 0.0 : ex(((double)ref[e] - (double)most[e]) * p.inv);
             ref[e] = most[e];
             high[e] = ref[e] + reach;
-            from[e] = (double)ref[e] * p.inv;
+            from[e] = (double)ref[e] * scale;
           }
       }
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum[e] += ex.near(fmax(__builtin_fma((double)f[k][e], p.inv, -from[e]), -700.0));      // e^-700, for -inf and NaN too, is nothing beside ref's own share
+        for (int k = 0; k < N; ++k) sum[e] += ex.near(fmax(__builtin_fma((double)f[k][e], scale, -from[e]), LOWEST));      // e^-700, for -inf and NaN too, is nothing beside ref's own share
     };
     int v = v0 + r;
-    for (; v + (UN - 1) * rl < v1; v += UN * rl) take(std::integral_constant<int, UN>(), v);
-    for (; v < v1; v += rl) take(std::integral_constant<int, 1>(), v);
+    if (v < v1) {
+      Rows rows = ask(v);
+#pragma unroll 1
+      for (; v + (UN - 1) * rl < v1; v += UN * rl) {
+        const Rows next = ask(v + UN * rl);
+        take(std::integral_constant<int, UN>(), rows);
+        rows = next;
+      }
+#pragma unroll 1
+      for (; v < v1; v += rl) {
+        take(std::integral_constant<int, 1>(), rows);
+#pragma unroll
+        for (int k = 0; k + 1 < UN; ++k) rows.x[k] = rows.x[k + 1];
+      }
+    }
   }
 #pragma unroll
   for (int e = 0; e < VEC; ++e) sum[e] = ref[e] == -INFINITY ? 0.0 : sum[e];
@@ -200,17 +233,18 @@ __device__ __forceinline__ Mass whole_column(const VerifyP& p, const Exp& ex, lo
 }
 
 // A workgroup for a sequence, a wavefront for a position.
+constexpr int DECIDERS = 8;
 template <typename E>
-__global__ __launch_bounds__(256) void verify_decide_kernel(const VerifyP p) {
+__global__ __launch_bounds__(64 * DECIDERS) void verify_decide_kernel(const VerifyP p) {
   __shared__ double table[32];
-  __shared__ int stop[4];
-  __shared__ Chosen found[4];
+  __shared__ int stop[DECIDERS];
+  __shared__ Chosen found[DECIDERS];
   fill_table(table);
   const Exp ex{table};
   const int seq = (int)blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const auto begin = [&](int s) { return p.draft_start ? min(max(p.draft_start[s], 0), p.T) : (s ? p.T : 0); };
   const int a = begin(seq), n = max(begin(seq + 1) - a, 0);
-  for (int i0 = 0; i0 <= n; i0 += 4) {
+  for (int i0 = 0; i0 <= n; i0 += DECIDERS) {
     const int i = i0 + wave;
     if (i <= n) {
       const int ct = min(a + seq + i, p.columns - 1), x = i < n ? p.draft_id[a + i] : 0, at = min(max(x, 0), p.V - 1);
@@ -235,7 +269,7 @@ __global__ __launch_bounds__(256) void verify_decide_kernel(const VerifyP p) {
     }
     __syncthreads();
     int at = -1;
-    for (int w = 3; w >= 0; --w)
+    for (int w = DECIDERS - 1; w >= 0; --w)
       if (i0 + w <= n && stop[w]) at = w;
     if (at >= 0) {
       if (threadIdx.x == 0) {
@@ -406,8 +440,8 @@ static VerifyPlan plan_verify(int V, long long T, int n_seq, int dtype) {
   while (q.ct < widest && q.ct < chunks_t) q.ct *= 2;
   q.groups_t = (int)((chunks_t + q.ct - 1) / q.ct);
   q.groups_d = (int)((chunks_d + q.ct - 1) / q.ct);
-  // as many workgroups as the chip holds at once, three a CU in bf16 and six in fp32 (verify_256 152 us; 1044 workgroups 165, 2052 161), none below one entry a thread
-  long long slices = (dtype == STRP_BF16 ? 768 : 1536) / (q.groups_t + q.groups_d);
+  // as many workgroups as the chip holds at once, four a CU in bf16 and six in fp32 (verify_64 60 us; 768 workgroups 66), none below one entry a thread
+  long long slices = (dtype == STRP_BF16 ? 1024 : 1536) / (q.groups_t + q.groups_d);
   if (slices < 1) slices = 1;
   const long long most = (V + 256 / q.ct - 1) / (256 / q.ct);
   if (slices > most) slices = most;
@@ -427,10 +461,10 @@ static void launch_verify(strp_ctx* ctx, const VerifyP& p, const VerifyPlan& q) 
   const dim3 block(256);
   const unsigned n = (unsigned)p.n_seq;
   hipLaunchKernelGGL((verify_sums_kernel<E>), dim3((unsigned)(q.groups_t + q.groups_d), (unsigned)q.slices), block, 0, ctx->stream, p);
-  hipLaunchKernelGGL((verify_decide_kernel<E>), dim3(n), block, 0, ctx->stream, p);
+  hipLaunchKernelGGL((verify_decide_kernel<E>), dim3(n), dim3(64 * DECIDERS), 0, ctx->stream, p);
   // 32 sequences of four tokens and one lie in three lines of memory, 8 in one or two: from where 32 a workgroup fill the chip
   if (n >= 128) hipLaunchKernelGGL((verify_weigh_kernel<E, 32>), dim3((n + 31) / 32, (unsigned)q.parts), block, 0, ctx->stream, p);
-  else if (n >= 8) hipLaunchKernelGGL((verify_weigh_kernel<E, 8>), dim3((n + 7) / 8, (unsigned)q.parts), block, 0, ctx->stream, p);
+  else if (n >= 8) hipLaunchKernelGGL((verify_weigh_kernel<E, 16>), dim3((n + 15) / 16, (unsigned)q.parts), block, 0, ctx->stream, p);
   else hipLaunchKernelGGL((verify_weigh_kernel<E, 1>), dim3(n, (unsigned)q.parts), block, 0, ctx->stream, p);
   hipLaunchKernelGGL((verify_find_kernel<E>), dim3(n), block, 0, ctx->stream, p);
 }

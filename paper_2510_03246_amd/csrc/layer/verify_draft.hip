@@ -45,9 +45,10 @@ struct Exp {
     p = __builtin_fma(p, r, C1) * r;
     const unsigned i = (unsigned)__builtin_bit_cast(unsigned long long, t);
     // k and j, whole, into the exponent and behind it: the table has j taken off there
-    const unsigned long long of = __builtin_bit_cast(unsigned long long, table[i & 31]);
-    const unsigned high = (unsigned)(of >> 32) + (i << 15);
-    const double b = __builtin_bit_cast(double, (unsigned long long)high << 32 | (unsigned)of);
+    const uint2 of = ((const uint2*)table)[i & 31];
+    unsigned high;
+    asm("v_lshl_add_u32 %0, %1, 15, %2" : "=v"(high) : "v"(i), "v"(of.y));      // (as an addition of 64 bits it would be three instructions)
+    const double b = __builtin_bit_cast(double, (unsigned long long)high << 32 | of.x);
     return __builtin_fma(b, p, b);
   }
   // 0 where y is below -700 or NaN
@@ -109,13 +110,16 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
   const double scale = p.inv * UNITS;
   if (t0 < n) {
     const E* x = (const E*)(of_draft ? p.draft : p.target) + t0;
-    typedef E vec __attribute__((ext_vector_type(VEC)));
-    struct Rows { vec x[UN]; };
-    // rows v, v + rl, ..: asked for while those before them are worked on
-    auto ask = [&](int v) {
+    struct Rows { uintx4 x[UN]; };
+    // rows from `at` on, rl apart, no further than the slice's last: asked for while those before them are worked on
+    const E* final_row = x + (long long)(v1 - 1) * ld;
+    auto ask = [&](const E* at) {
       Rows rows;
 #pragma unroll
-      for (int k = 0; k < UN; ++k) rows.x[k] = *(const vec*)(x + (long long)min(v + k * rl, v1 - 1) * ld);
+      for (int k = 0; k < UN; ++k) {
+        const E* from = at + (long long)(k * rl) * ld;
+        rows.x[k] = *(const uintx4*)(from < final_row ? from : final_row);
+      }
       return rows;
     };
     auto take = [&](auto count, const Rows& rows) {
@@ -124,7 +128,10 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
 #pragma unroll
       for (int k = 0; k < N; ++k)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) f[k][e] = (float)rows.x[k][e];
+        for (int e = 0; e < VEC; ++e) {
+          const unsigned w = rows.x[k][e * sizeof(E) / 4];
+          f[k][e] = __builtin_bit_cast(float, sizeof(E) == 4 ? w : e % 2 ? w & 0xffff0000u : w << 16);
+        }
       bool far = false;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -151,10 +158,13 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
     };
     int v = v0 + r;
     if (v < v1) {
-      Rows rows = ask(v);
+      const E* at = x + (long long)v * ld;
+      const long long step = (long long)(UN * rl) * ld;
+      Rows rows = ask(at);
 #pragma unroll 1
       for (; v + (UN - 1) * rl < v1; v += UN * rl) {
-        const Rows next = ask(v + UN * rl);
+        at += step;
+        const Rows next = ask(at);
         take(std::integral_constant<int, UN>(), rows);
         rows = next;
       }
@@ -440,8 +450,8 @@ static VerifyPlan plan_verify(int V, long long T, int n_seq, int dtype) {
   while (q.ct < widest && q.ct < chunks_t) q.ct *= 2;
   q.groups_t = (int)((chunks_t + q.ct - 1) / q.ct);
   q.groups_d = (int)((chunks_d + q.ct - 1) / q.ct);
-  // as many workgroups as the chip holds at once, four a CU in bf16 and six in fp32 (verify_64 60 us; 768 workgroups 66), none below one entry a thread
-  long long slices = (dtype == STRP_BF16 ? 1024 : 1536) / (q.groups_t + q.groups_d);
+  // as many workgroups as the chip holds at once, three a CU in bf16 and six in fp32 (verify_256 131 us; 1024 workgroups 134, 2048 138), none below one entry a thread
+  long long slices = (dtype == STRP_BF16 ? 768 : 1536) / (q.groups_t + q.groups_d);
   if (slices < 1) slices = 1;
   const long long most = (V + 256 / q.ct - 1) / (256 / q.ct);
   if (slices > most) slices = most;

@@ -380,7 +380,7 @@ size_t strp_token_logprobs_workspace_bytes(int32_t V, int64_t T, int32_t n_top);
  *   K, V [pages x kv_heads x page x d_head], a token's channels contiguous (that is how the attention of single tokens reads them), in
  *     STRP_CACHE_BF16, STRP_CACHE_F32: values of that type;
  *     STRP_CACHE_Q4: two channels a byte, the even one in the lower half, as whole numbers n of 0 to 15 that stand for lowest + n step;
- *       K_scale, V_scale [pages x kv_heads x page x 2] fp32: lowest and step of a token's channels in one head.
+ *       K_scale, V_scale [pages x kv_heads x page x 2] fp32: lowest and step of a token's channels in one head, finite or NaN.
  *   table [n_seq x ld_table]: the pages of a sequence in the order of its tokens: token j is row j % page of page table[j / page].
  *   past [n_seq]: tokens that the cache holds of each sequence before the call's own;  seq_start: n_seq + 1 ascending offsets into the
  *     call's T tokens, as in strp_attention, or NULL for one sequence of all of them (n_seq = 1).  Token t of sequence i has
@@ -407,8 +407,8 @@ typedef struct {
  *     (x, y) -> (x cos a - y sin a, y cos a + x sin a)  for channels (j, j + rot / 2) of each head, or (2j, 2j + 1) where pairs != 0,
  *   in 64 bits, rounded to fp32 and then to the output's type; channels from rot on are as they were.
  *   STRP_CACHE_Q4, for a token and head, all of it in fp32 on the turned keys of fp32: lowest = min x, step = (max x - lowest) / 15,
- *   n = (x - lowest) / step to the nearest whole number (0 where step is 0).  What is not finite, or a range that fp32 does not hold,
- *   stands for values that are not finite.
+ *   n = (x - lowest) / step to the nearest whole number (0 where step is 0).  Where a channel is not finite, or the range too large for fp32, lowest
+ *   and step are NaN.
  * Tokens outside every sequence are not stored, and their Qr keeps what it holds.  No two tokens may have one place.
  * Errors: STRP_EINVAL (null K, V or cache pointers, sizes not positive, d_head no multiple of 8 or above 128, page no power of two from 16 to
  * 65536, ld_table * page above 2^30, heads or kv_heads above 1024, n_seq above 65536, T above 2^27, rot odd, negative or above d_head, inv_freq

@@ -127,7 +127,10 @@ __device__ __forceinline__ void store_rows(const AppendP& p, bool isK, int h, co
         lo = __builtin_elementwise_minimum(lo, __shfl_xor(lo, o, 64));
         hi = __builtin_elementwise_maximum(hi, __shfl_xor(hi, o, 64));
       }
-      const float step = (hi - lo) / 15.0f;
+      // what is not finite, or too far apart: NaN, since a score of minus infinity would hide a key of infinity
+      const bool fine = fabsf(hi - lo) < INFINITY && fabsf(lo) < INFINITY;
+      const float step = fine ? (hi - lo) / 15.0f : __builtin_nanf("");
+      lo = fine ? lo : __builtin_nanf("");
       unsigned w = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {

@@ -672,13 +672,12 @@ __global__ __launch_bounds__(256, 2) void cache_rows_kernel(const RowsP p) {
   const Heads heads = heads_of(p, map, (int*)smem);
   rows_share<E, Q4, W, SPLIT>(p, heads, smem, blockIdx.x);
 }
-template <int W, bool SPLIT>
+template <bool Q4, int W, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void cache_wide_kernel(const RowsP p) {
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[Wide<W>::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[Wide<W, Q4>::BYTES];
   __shared__ MapLds map;
-  static_assert(Wide<W>::BYTES >= 4 * MAX_CACHE_HEADS, "room for the map");
   const Heads heads = heads_of(p, map, (int*)smem);
-  wide_share<W, SPLIT>(p, heads, smem, blockIdx.x);
+  wide_share<W, SPLIT, Q4>(p, heads, smem, blockIdx.x);
 }
 
 // The parts of tiles that several workgroups had, in the order of the keys.  A workgroup for a row of the tile that begins in a workgroup of the first kernel: a wavefront has a fourth of
@@ -759,8 +758,8 @@ static void launch_rows(strp_ctx* ctx, const RowsP& p, int join_rows) {
   const dim3 grid((unsigned)WORKERS), block(256);
   const auto go = [&](auto width) {
     constexpr int W = decltype(width)::value;
-    if constexpr (sizeof(E) == 2 && !Q4)
-      if (p.wide) hipLaunchKernelGGL((cache_wide_kernel<W, SPLIT>), grid, block, 0, ctx->stream, p);
+    if constexpr (sizeof(E) == 2)
+      if (p.wide) hipLaunchKernelGGL((cache_wide_kernel<Q4, W, SPLIT>), grid, block, 0, ctx->stream, p);
     hipLaunchKernelGGL((cache_rows_kernel<E, Q4, W, SPLIT>), grid, block, 0, ctx->stream, p);
   };
   if (p.c.dh <= 32) go(std::integral_constant<int, 2>());
@@ -810,7 +809,7 @@ strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* i
   // a tile has no more rows than the heads that one key-value head can have times the tokens
   const long long rows = (in->kv_of_head ? in->heads : p.group) * in->T;
   // Single tokens alone, of no more heads than that, are left to the workgroups of 16 rows: with as many sequences as tokens that is what a call most likely is.
-  p.wide = in->dtype == STRP_BF16 && c.format == STRP_CACHE_BF16 && rows > WIDE_FROM && (in->T > c.n_seq || rows / in->T > WIDE_FROM);
+  p.wide = in->dtype == STRP_BF16 && rows > WIDE_FROM && (in->T > c.n_seq || rows / in->T > WIDE_FROM);
   const int join_rows = rows < ROWS ? (int)rows : ROWS;
   // the lengths are on the device: the operations and bytes of a cache that is full
   const double keys = (double)p.c.cap, T = (double)in->T, row = c.format == STRP_CACHE_Q4 ? 0.5 * c.d_head + 8.0 : bytes_of(in->dtype) * (double)c.d_head;

@@ -15,15 +15,27 @@ namespace strp {
 
 __device__ const unsigned cache_zero_chunk[4] = {0u, 0u, 0u, 0u};
 
-template <int W>
+// KT: keys of a unit, fewer of 4 bits for the registers
+template <int W, bool Q4>
 struct Wide {
-  static constexpr int DHP = 16 * W, PITCH = 2 * DHP, KT = 64, TILE = KT * PITCH, RING = 2, BYTES = 2 * RING * TILE;
+  static constexpr int DHP = 16 * W, PITCH = 2 * DHP, KT = Q4 ? 32 : 64, TILE = KT * PITCH, RING = 2, BYTES = 2 * RING * TILE > 4 * MAX_CACHE_HEADS ? 2 * RING * TILE : 4 * MAX_CACHE_HEADS;
 };
 
-template <int W, bool SPLIT>
+// Whole numbers of 4 bits, two channels a byte, as bf16 in the channels' order.
+__device__ __forceinline__ uintx4 numbers_of(unsigned x) {
+  const unsigned even = x & 0x0f0f0f0fu, odd = (x >> 4) & 0x0f0f0f0fu;
+  uintx4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = pick(__builtin_bit_cast(unsigned, (float)((even >> (8 * i)) & 255u)), __builtin_bit_cast(unsigned, (float)((odd >> (8 * i)) & 255u)), HIGHS);
+  return r;
+}
+
+// Q4: keys and values come by way of registers, as whole numbers in bf16; lowest and step of K enter the scores, those of V the probabilities, in fp32.
+template <int W, bool SPLIT, bool Q4>
 __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, unsigned char* smem, unsigned block) {
-  typedef Wide<W> Z;
-  constexpr int NC = Z::DHP / 32, NS = Z::DHP / 16, KT = Z::KT, PITCH = Z::PITCH, TILE = Z::TILE, LOADS = TILE / 4096;      // LOADS: KBs of a tile that a wavefront moves
+  typedef Wide<W, Q4> Z;
+  constexpr int NC = Z::DHP / 32, NS = Z::DHP / 16, KT = Z::KT, U = KT / 32, KEYS = KT / 4, PITCH = Z::PITCH, TILE = Z::TILE, LOADS = TILE / 4096;      // LOADS: KBs of a tile that a wavefront moves
   constexpr int CHUNKS = PITCH / 16, EACH = 64 / CHUNKS;                   // chunks of a row, rows of a KB
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, l32 = lane & 31;
   const Pages& c = p.c;
@@ -94,10 +106,12 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
   Seq q = uniform_sequence();
 
   const unsigned ldsK = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem, ldsV = ldsK + Z::RING * TILE;
-  // a wavefront moves 16 rows of a tile, EACH of them at a time: lane l has chunk l % CHUNKS of row l / CHUNKS of them
+  // a wavefront moves KEYS rows of a tile, EACH of them at a time: lane l has chunk l % CHUNKS of row l / CHUNKS of them
   auto order_k = [](int row) { return (row / (256 / PITCH)) & (CHUNKS - 1); };
   auto order_v = [](int row) { return PITCH == 256 ? (row & 3) << 2 : PITCH == 128 ? ((row >> 1) & 1) << 2 : 0; };
   const bool full = 2 * dh == PITCH;
+  __shared__ __attribute__((aligned(16))) float2 scales[Q4 ? 2 : 1][Q4 ? 3 : 1][Q4 ? KT : 1];      // of K and V, three units: some wavefronts are a unit ahead of others
+  __shared__ int not_finite[Q4 ? 3 : 1][4];                                // of V's, a bit for a key
   // fragments of K: key l32 (+ 32 u), chunk 2 d + h; of V: keys 16 k + 4 h + (lane % 16) / 4 (+ 8), the 16 channels of the lane's group
   const int kr = (lane & 15) >> 2;
   const unsigned offK = (unsigned)(l32 * PITCH + ((h ^ order_k(l32)) * 16));
@@ -168,18 +182,26 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
         for (int e = 0; e < 8; ++e) qf[d][e] = 16 * d + 8 * half + e < width ? qf[d][e] : (__bf16)0.0f;
     }
+    float qsum = 0.0f;
+    if constexpr (Q4) {
+#pragma unroll
+      for (int d = 0; d < NS; ++d)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qsum += (float)qf[d][e];
+      qsum = both_32(qsum, true);
+    }
 
-    // pages of the wavefront's 16 keys of a unit: lane l has that of unit bt + l
+    // pages of the wavefront's keys of a unit: lane l has that of unit bt + l
     const int32_t* table = c.table + (long long)s * c.ld_table;
     const int in_page = (1 << c.page_log2) - 1;
     int ids = 0, bt = 0;
     auto look_up = [&](int b) {
       bt = b;
-      ids = clamped(table[min((int)(((long long)(b + lane) * KT + wave * 16) >> c.page_log2), c.ld_table - 1)], 0, c.pages - 1);
+      ids = clamped(table[min((int)(((long long)(b + lane) * KT + wave * KEYS) >> c.page_log2), c.ld_table - 1)], 0, c.pages - 1);
     };
     auto issue = [&](const void* pool, long long row, unsigned to, bool of_k) {
       const char* from = (const char*)pool + row * (2 * dh);
-      to += (unsigned)wave * (16 * PITCH);
+      to += (unsigned)wave * (KEYS * PITCH);
       int mine = lane, width = dh;
       asm volatile("" : "+v"(mine), "+s"(width));        // worked out each time, for the registers
       auto piece = [&](int i) { return mine / CHUNKS + EACH * i; };      // its row
@@ -198,11 +220,58 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
     };
     unsigned toK, toV, atK, atV;           // where the next tile goes, and is read
     long long next_row = 0;
-    auto ahead = [&](unsigned& x, unsigned from) { x = x == from + (Z::RING - 1) * TILE ? from : x + TILE; };
-    auto issue_k = [&](int b) {            // units in their order
+    // 4 bits: a lane has an eighth of the channels of a key of K and of one of V (heads of 32: a fourth, or nothing), and K's scales of that key or V's or nothing
+    constexpr int PARTS = 64 / KEYS, DW = W >= 4 ? W / 4 : 1;
+    struct Packed { unsigned k[DW], v[DW]; float2 scale; };
+    auto page_of = [&](int b) {            // units in their order
       if (b - bt == 64) look_up(b);
       const int page = __builtin_amdgcn_readlane(ids, b - bt);
-      next_row = (((long long)page * c.kv_heads + kv) << c.page_log2) + ((b * KT + wave * 16) & in_page);
+      return (((long long)page * c.kv_heads + kv) << c.page_log2) + ((b * KT + wave * KEYS) & in_page);
+    };
+    auto ask_packed = [&](long long k_row, long long v_row) {
+      Packed x;
+      int mine = lane, width = dh;
+      asm volatile("" : "+v"(mine), "+s"(width));        // worked out each time, for the registers
+      const int key = mine / PARTS, part = mine % PARTS;
+      const auto gk = opaque((const char*)p.K + k_row * (dh / 2)), gv = opaque((const char*)p.V + v_row * (dh / 2));
+#pragma unroll
+      for (int j = 0; j < DW; ++j) {
+        const int chunk = part * DW + j;
+        const unsigned off = (unsigned)(key * (width / 2) + (8 * chunk < width ? 4 * chunk : 0));      // (channels that are not there meet queries of zero, or nobody)
+        x.k[j] = *(Global<unsigned>)(gk + off);
+        x.v[j] = *(Global<unsigned>)(gv + off);
+      }
+      const auto gs = (part & 1 ? opaque((const float2*)p.sV + v_row) : opaque((const float2*)p.sK + k_row)) + 8u * (unsigned)key;
+      x.scale = float2{((Global<float>)gs)[0], ((Global<float>)gs)[1]};
+      return x;
+    };
+    // K of the unit that goes to slot ks of three, V of that before it
+    auto put_packed = [&](const Packed& x, unsigned to_k, unsigned to_v, int k_unit) {
+      int mine = lane;
+      asm volatile("" : "+v"(mine));
+      const int key = mine / PARTS, part = mine % PARTS, row = wave * KEYS + key;
+#pragma unroll
+      for (int j = 0; j < DW; ++j) {
+        const int chunk = part * DW + j;
+        if (PARTS * DW > CHUNKS && chunk >= CHUNKS) continue;
+        *(__attribute__((address_space(3))) uintx4*)(size_t)(to_k + row * PITCH + ((chunk ^ order_k(row)) * 16)) = numbers_of(x.k[j]);
+        *(__attribute__((address_space(3))) uintx4*)(size_t)(to_v + row * PITCH + ((chunk ^ order_v(row)) * 16)) = numbers_of(x.v[j]);
+      }
+      // scales of V that are not finite would reach rows that do not see their key, by a probability of zero: they are looked at by themselves
+      const bool bad = part == 1 && !(fabsf(x.scale.x) < INFINITY && fabsf(x.scale.y) < INFINITY);
+      const unsigned long long which = __builtin_amdgcn_ballot_w64(bad);
+      const int k_slot = k_unit % 3, v_slot = (k_unit + 2) % 3;
+      if (part < 2) scales[part][part ? v_slot : k_slot][row] = bad ? float2{0.0f, 0.0f} : x.scale;
+      if (lane == 0) {
+        int bits = 0;
+        if (which)
+          for (int i = 0; i < KEYS; ++i) bits |= (int)(which >> (PARTS * i + 1) & 1) << i;
+        not_finite[v_slot][wave] = bits;
+      }
+    };
+    auto ahead = [&](unsigned& x, unsigned from) { x = x == from + (Z::RING - 1) * TILE ? from : x + TILE; };
+    auto issue_k = [&](int b) {
+      next_row = page_of(b);
       issue(p.K, next_row, toK, true);
       ahead(toK, ldsK);
     };
@@ -212,12 +281,12 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
     };
 
     floatx16 O[NC];
-    float m, l[2];
+    float m, l[2], lowest;                 // lowest: the sum of p lowest, of 4 bits
     bool again = false;
-    struct Scores { floatx16 u[2]; };
+    struct Scores { floatx16 u[U]; };
     auto clear = [&](Scores& S) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < U; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) S.u[t][e] = 0.0f;
     };
@@ -225,13 +294,13 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
       for (int d = d0; d < d1; ++d)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) S.u[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_k(from, d, t), qf[d], S.u[t], 0, 0, 0);
+        for (int t = 0; t < U; ++t) S.u[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_k(from, d, t), qf[d], S.u[t], 0, 0, 0);
     };
     // the running maximum with a tile's scores, what is held rescaled to it; returns what is to be taken from a score in powers of two
     auto raise = [&](const Scores& S) {
       float mt = m;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < U; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) mt = __builtin_elementwise_maximum(mt, S.u[t][e]);
       mt = both_32(mt, false);
@@ -240,7 +309,8 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       if (__builtin_amdgcn_ballot_w64(grown)) {
         const float fac = grown ? __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e) : 1.0f;
         l[0] *= fac;
-        if constexpr (!SPLIT) l[1] *= fac;
+        if constexpr (!SPLIT || Q4) l[1] *= fac;
+        if constexpr (Q4) lowest *= fac;
 #pragma unroll
         for (int ch = 0; ch < NC; ++ch)
 #pragma unroll
@@ -252,33 +322,51 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
     // Probabilities of the quarter k of a tile's keys and, in fp32, their sum.  SPLIT: hi has their upper 16 bits and lo what that leaves, together within 2^-16 of them;
     // else hi is rounded to bf16 and the sum is of what was rounded.
     struct Probs { bf16x8 hi, lo; };
-    auto quarter = [&](const Scores& S, int k, float ref) {
+    auto quarter = [&](const Scores& S, int k, float ref, int b) {
       uintx4 hi, lo;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float x[2];
 #pragma unroll
         for (int f = 0; f < 2; ++f) x[f] = __builtin_amdgcn_exp2f(__builtin_fmaf(S.u[k >> 1][8 * (k & 1) + 2 * e + f], p.scale_log2e, -ref));
+        if constexpr (Q4) {
+          l[0] += x[0] + x[1];
+          const int key = 16 * k + 8 * (e >> 1) + 2 * (e & 1);             // and 4 h: the first of the two
+          const floatx4 s = *(const floatx4*)&scales[1][b % 3][key + 4 * h];
+#pragma unroll
+          for (int f = 0; f < 2; ++f) {
+            lowest = __builtin_fmaf(x[f], s[2 * f], lowest);
+            x[f] *= s[2 * f + 1];
+          }
+        }
         if constexpr (SPLIT) {
           const unsigned x0 = __builtin_bit_cast(unsigned, x[0]), x1 = __builtin_bit_cast(unsigned, x[1]);
-          l[0] += x[0] + x[1];
+          if constexpr (!Q4) l[0] += x[0] + x[1];
           hi[e] = pick(x0, x1, HIGHS);
           const bf16x2 left = {(__bf16)(x[0] - __builtin_bit_cast(float, x0 & 0xffff0000u)), (__bf16)(x[1] - __builtin_bit_cast(float, x1 & 0xffff0000u))};
           lo[e] = __builtin_bit_cast(unsigned, left);
         } else {
           const bf16x2 one = {(__bf16)x[0], (__bf16)x[1]};
           hi[e] = __builtin_bit_cast(unsigned, one);
-          l[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(one, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[e & 1], false);
+          if constexpr (!Q4) l[e & 1] = __builtin_amdgcn_fdot2_f32_bf16(one, bf16x2{(__bf16)1.0f, (__bf16)1.0f}, l[e & 1], false);
         }
       }
       return Probs{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
     };
     // Unit b, whose scores are in S; those of the next one go to N.
     auto unit = [&](int b, Scores& S, Scores& N) {
-      wait_loads<0>();
-      __builtin_amdgcn_s_barrier();        // K of the next unit and V of this one are there, and nobody reads those before them any more
-      if (b + 1 < b1) {
-        const long long row = next_row;    // of unit b + 1
+      if constexpr (Q4) {
+        __syncthreads();
+      } else {
+        wait_loads<0>();
+        __builtin_amdgcn_s_barrier();      // K of the next unit and V of this one are there, and nobody reads those before them any more
+      }
+      [[maybe_unused]] Packed packed;
+      const long long row = next_row;      // of unit b + 1
+      if constexpr (Q4) {
+        next_row = page_of(b + 2);         // (what lies behind the last unit is asked for too, and nobody looks at it: a condition here would cost registers)
+        packed = ask_packed(next_row, row);
+      } else if (b + 1 < b1) {
         if (b + 2 < b1) issue_k(b + 2);
         else ahead(toK, ldsK);
         issue_v(row);
@@ -289,9 +377,19 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
         clear(N);
         const bool whole = k0 + KT - 1 <= see_all;
         const int to = see - k0 - 4 * h;
+        if constexpr (Q4)
+#pragma unroll
+          for (int t = 0; t < U; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+              const floatx4 s = *(const floatx4*)&scales[0][b % 3][32 * t + 8 * (e >> 2) + 4 * h + (e & 3)];
+#pragma unroll
+              for (int f = 0; f < 2; ++f) S.u[t][e + f] = __builtin_fmaf(S.u[t][e + f], s[2 * f + 1], qsum * s[2 * f]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
         if (!whole)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
+          for (int t = 0; t < U; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               S.u[t][e] = 32 * t + 8 * (e >> 2) + (e & 3) > to ? -INFINITY : S.u[t][e];
@@ -301,11 +399,11 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
         // Where some key is not seen by every row, a value that is not finite would reach those too, by a probability of zero: such values are left out
         // of the products and added to the results of the rows that see them.
         bool odd = false;
-        if (!whole || again) {
+        if (!Q4 && (!whole || again)) {
           typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
           ushort2v most = {0, 0};
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
+          for (int k = 0; k < 2 * U; ++k)
 #pragma unroll
             for (int ch = 0; ch < NC; ++ch) {
               const uintx4 bits = __builtin_bit_cast(uintx4, frag_v(atV, ch, k)) & 0x7fff7fffu;
@@ -318,14 +416,14 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
             }
           odd = most[0] >= 0x7f80 || most[1] >= 0x7f80;
         }
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+        odd = !Q4 && __builtin_amdgcn_ballot_w64(odd) != 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2 * U; ++k) {
           bf16x8 v[NC];
 #pragma unroll
           for (int ch = 0; ch < NC; ++ch) v[ch] = frag_v(atV, ch, k);
-          scores(N, atK, k * NS / 4, (k + 1) * NS / 4);
-          const Probs P = quarter(S, k, ref);
+          scores(N, atK, k * NS / (2 * U), (k + 1) * NS / (2 * U));
+          const Probs P = quarter(S, k, ref, b);
           if (odd)
 #pragma unroll
             for (int ch = 0; ch < NC; ++ch)
@@ -340,6 +438,14 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
             for (int ch = 0; ch < NC; ++ch) O[ch] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[ch], P.lo, O[ch], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (Q4) {
+          const int slot = b % 3;
+          const int any = __builtin_amdgcn_readfirstlane(not_finite[slot][0] | not_finite[slot][1] | not_finite[slot][2] | not_finite[slot][3]);
+          if (any)
+#pragma unroll 1
+            for (int i = 0; i < KT; ++i)
+              if (not_finite[slot][i / KEYS] >> (i % KEYS) & 1) lowest = k0 + i <= see ? __builtin_nanf("") : lowest;
         }
         if (odd)
 #pragma unroll 1
@@ -358,6 +464,12 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
               }
           }
       }
+      if constexpr (Q4)
+        if (b + 1 < b1) {
+          put_packed(packed, toK, toV, b + 2);
+          ahead(toK, ldsK);
+          ahead(toV, ldsV);
+        }
       ahead(atV, ldsV);
     };
     int* lost_of = (int*)smem;             // between the passes, of the four wavefronts
@@ -365,21 +477,35 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       toK = atK = ldsK;
       toV = atV = ldsV;
       m = -INFINITY;
-      l[0] = l[1] = 0.0f;
+      l[0] = l[1] = lowest = 0.0f;
 #pragma unroll
       for (int ch = 0; ch < NC; ++ch)
 #pragma unroll
         for (int e = 0; e < 16; ++e) O[ch][e] = 0.0f;
       __syncthreads();                     // nobody reads the segment before any more
       look_up(b0);
-      issue_k(b0);
-      const long long row = next_row;
-      issue_k(b0 + 1);                     // (behind the last unit: pages that lie in the cache, for nobody)
-      issue_v(row);
+      // (behind the last unit: pages that lie in the cache, for nobody)
       Scores a, b;
       clear(a);
-      wait_loads<2 * LOADS>();
-      __builtin_amdgcn_s_barrier();
+      if constexpr (Q4) {
+        const long long row = page_of(b0);
+        next_row = page_of(b0 + 1);
+        const Packed x = ask_packed(row, row), y = ask_packed(next_row, row);
+        put_packed(x, toK, toV, b0 + 3);                 // (its V comes again with the next; the slots of three units further are its own)
+        ahead(toK, ldsK);
+        __syncthreads();
+        put_packed(y, toK, toV, b0 + 1);
+        ahead(toK, ldsK);
+        ahead(toV, ldsV);
+        __syncthreads();
+      } else {
+        issue_k(b0);
+        const long long row = next_row;
+        issue_k(b0 + 1);
+        issue_v(row);
+        wait_loads<2 * LOADS>();
+        __builtin_amdgcn_s_barrier();
+      }
 #pragma unroll
       for (int d = 0; d < NS; d += 2) {
         scores(a, atK, d, d + 2);
@@ -390,6 +516,7 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
         unit(i, a, b);
         if (i + 1 < b1) unit(i + 1, b, a);
       }
+      if constexpr (Q4) break;
       wait_loads<0>();                     // LDS is not to be written behind this
       if (again) break;
       // A value of V that is not finite and is seen by every row of a tile has been multiplied by a probability or by a part of one, which may be zero: the workgroup then
@@ -407,6 +534,13 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       again = true;
     }
     const float sum = both_32(l[0] + l[1], true);
+    if constexpr (Q4) {
+      lowest = both_32(lowest, true);
+#pragma unroll
+      for (int ch = 0; ch < NC; ++ch)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) O[ch][e] += lowest;
+    }
     int width = dh, half = h;
     asm volatile("" : "+s"(width), "+v"(half));                            // what follows from these is worked out here, not kept from segment to segment
     const long long out = r < rows ? (long long)head * dh * p.ldc + q.begin + token : -1;

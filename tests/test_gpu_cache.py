@@ -237,6 +237,9 @@ def test_append_of_what_is_not_finite(ctx):
         finite = torch.isfinite(v[0, :, :4])
         assert torch.equal(finite.all(-1).cpu(), torch.tensor([[False, True, False, True], [True, False, False, True]]))
         assert not finite[0, 0].any() and not finite[1, 2].any()
+    # keys of infinity could give scores of minus infinity, which would hide them: lowest and step are NaN
+    for sc in (cache.K_scale, cache.V_scale):
+        assert sc[0][~torch.isfinite(sc[0]).all(-1)][:3].isnan().all()
 
 
 def test_append_of_constant_and_tiny_heads(ctx):
@@ -422,6 +425,25 @@ def test_values_that_are_not_finite_show_where_they_are_seen(ctx, dts, n):
             rest = torch.arange(dh, device="cuda") != 5
             assert torch.equal(got[h * dh:(h + 1) * dh][rest], want[h * dh:(h + 1) * dh][rest]), at
         assert torch.equal(got[:, ~sees], want[:, ~sees])
+
+
+@pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 4, 33, 100, 200])
+@pytest.mark.parametrize("scale", ["K_scale", "V_scale"])
+def test_scales_of_4_bits_that_are_not_finite_show_where_they_are_seen(ctx, dt, n, scale):
+    """The tokens that see such a key have nothing that is finite in that head, the others what they had."""
+    past, heads, dh = 200, 2, 64
+    for at, bad in ((past + n - 1, float("inf")), (past + n // 2, float("nan")), (3, -float("inf"))):
+        cache = random_cache(60, 2, 16, dh, Q4, 1)
+        table = table_for([(n, past)], 16, 60, 1)
+        Q = rand((heads * dh, ld8(n)), 3, dt)
+        want = ctx.strp_cache_attention(Q, n, heads, cache, table, ints([past]))[:, :n].clone()
+        getattr(cache, scale)[int(table[0, at // 16]), 0, at % 16, 1] = bad if scale == "V_scale" else float("nan")
+        got = ctx.strp_cache_attention(Q, n, heads, cache, table, ints([past]))[:, :n]
+        sees = torch.arange(past, past + n, device="cuda") >= at
+        assert torch.isfinite(want).all()
+        assert not torch.isfinite(got[:dh, sees]).any(), at
+        assert torch.equal(got[:dh, ~sees], want[:dh, ~sees]) and torch.equal(got[dh:], want[dh:]), at
 
 
 def test_attention_lowest_values(ctx):

@@ -133,7 +133,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
   };
 
   // A segment: units b0 .. b1 of one tile of rows.  The one behind it is known while it is worked on: its first keys and values are on their way before the last ones here are done
-  // with, or nothing would be read while the wavefronts join their results (64 sequences of 0 to 4000 tokens, two segments a workgroup: 137 us instead of AAA).
+  // with, or nothing would be read while the wavefronts join their results (512 sequences of 127 keys, eight segments a workgroup: 87 us, 108 with the queries asked for between segments).
   struct Segment { int s, begin, past, keys, units, kv, rt, group, rows, b0, b1, all; long long last; };      // all: units of the share; last: the tile's last one
   auto segment_at = [&](long long u) {
     while (u >= base + (long long)q.units * q.tiles) next_sequence();
@@ -196,7 +196,13 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
   };
   const int in_page = (1 << c.page_log2) - 1;
 
-  TileT T[NT];
+  // Units asked for ahead: of 4 bits one is too little to hide the way from memory (eight sequences of 33000 keys, 32 heads of 128 on 8: 84 us instead of 92).
+  constexpr int AHEAD = BF && Q4 && W > 2 ? 2 : 1;
+  struct Tiles {
+    TileT t[NT];
+    __device__ __forceinline__ TileT& operator[](int i) { return t[i]; }
+  };
+  Tiles T[AHEAD];
   Segment g{}, next{};
   Queries queries{};
   int next_ids = 0;
@@ -227,6 +233,10 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     const int see_all = min(g.past + g.rt * ROWS / group, g.keys - 1), see_any = min(g.past + (g.rt * ROWS + rows - 1) / group, g.keys - 1);
     const long long out = (long long)head * dh * p.ldc + g.begin + token;
 
+    // the wavefront's units that some row sees
+    const int keys_of_wave = see_any - wave * KW;
+    const int be = keys_of_wave < 0 ? b0 : min(b1, keys_of_wave / UNIT + 1);
+
     // the rows of the cache that the wavefront's tiles of unit b begin at
     struct Places { long long row[NT]; };
     auto places = [&](int of, int kv_head, int b, int from) {
@@ -238,7 +248,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
       }
       return x;
     };
-    auto load_k = [&](const Places& at) {
+    auto load_k = [&](const Places& at, Tiles& T) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const long long row = at.row[t];
@@ -273,7 +283,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
         }
       }
     };
-    auto load_v = [&](const Places& at) {
+    auto load_v = [&](const Places& at, Tiles& T) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const long long row = at.row[t];
@@ -316,11 +326,11 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
       }
     };
 
-    if (!loaded) {
-      const Places first = places(ids, kv, b0, b0);
-      load_k(first);
-      load_v(first);
-    }
+    auto load = [&](const Places& at, Tiles& T) {
+      load_k(at, T);
+      load_v(at, T);
+    };
+    if (!loaded) load(places(ids, kv, b0, b0), T[0]);
     if (first) {
       put_queries(queries);
       __syncthreads();
@@ -329,6 +339,13 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     if (follows) {
       next_ids = pages_from(next, next.b0);
       queries = ask_queries(next);
+    }
+    if constexpr (AHEAD == 2) {
+      if (b0 + 1 < be) {
+        if (!loaded) load(places(ids, kv, b0 + 1, b0), T[1]);
+      } else if (b0 < be && follows) {
+        load(places(next_ids, next.kv, next.b0, next.b0), T[1]);           // (a segment of one unit: what was asked for before it was none of the next one's)
+      }
     }
     // the row's query as the second operand; of 4 bits a lane has channels 8 NC apart where its heads are whole
     uintx4 qb[BF ? NC : 1];
@@ -360,17 +377,13 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     floatx4 O[W];
     float m, l, weight, lowest;            // weight: sum of what the values were multiplied by (of 4 bits: to take 128 off again); lowest: of p lowest
     bool careful = false, odd;
-    // the wavefront's units that some row sees
-    const int keys_of_wave = see_any - wave * KW;
-    const int be = keys_of_wave < 0 ? b0 : min(b1, keys_of_wave / UNIT + 1);
     while (true) {
       odd = false;
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
       m = -INFINITY;
       l = weight = lowest = 0.0f;
-#pragma unroll 1
-      for (int b = b0; b < be; ++b) {
+      auto unit = [&](int b, Tiles& T) {
         const int k0 = b * UNIT + wave * KW;
         floatx4 S[NT];
 #pragma unroll
@@ -414,22 +427,22 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
             for (int e = 0; e < 4; ++e) S[t][e] = __builtin_fmaf(S[t][e], T[t].ks[e >> 1][2 * (e & 1) + 1], qsum * T[t].ks[e >> 1][2 * (e & 1)]);
         }
-        // the next unit, or the next segment's first
-        const bool more = b + 1 < be;
+        // the unit that these registers are for next, or one of the next segment's
+        const bool more = b + AHEAD < be;
         Places to;
         if (more) {
-          if (b + 1 - bt == 64 / NT) {
-            bt = b + 1;
+          if (b + AHEAD - bt == 64 / NT) {
+            bt = b + AHEAD;
             ids = pages_from(g, bt);
           }
-          to = places(ids, kv, b + 1, bt);
+          to = places(ids, kv, b + AHEAD, bt);
         } else if (follows) {
-          to = places(next_ids, next.kv, next.b0, next.b0);
+          to = places(next_ids, next.kv, next.b0 + (b + AHEAD - be), next.b0);
         } else {
 #pragma unroll
           for (int t = 0; t < NT; ++t) to.row[t] = 0;      // what all read at their ends: were these loads left out, those before them would have to be waited for together
         }
-        load_k(to);
+        load_k(to, T);
         // the softmax: lane (row, quad) has the keys 4 quad .. + 4 of both tiles
         const bool whole = k0 + KW - 1 <= see_all;
         if (!whole)
@@ -541,8 +554,20 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
                 O[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, P[t][e], O[j], 0, 0, 0);
               }
         }
-        load_v(to);
+        load_v(to, T);
+      };
+#pragma unroll 1
+      for (int b = b0; b < be; b += AHEAD) {
+        unit(b, T[0]);
+        if constexpr (AHEAD == 2)
+          if (b + 1 < be) unit(b + 1, T[1]);
       }
+      if constexpr (AHEAD == 2)
+        if (b0 < be && (be - b0) % 2) {
+          const Tiles x = T[0];
+          T[0] = T[1];
+          T[1] = x;
+        }
       if constexpr (!Q4) {
         if (__builtin_amdgcn_ballot_w64(odd)) {
           // rare: the values of the blocks that were looked at once more, key by key, those that are not finite to the rows that see them
@@ -581,9 +606,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
       if (b0 < be) {
         bt = b0;
         ids = pages_from(g, b0);
-        const Places first = places(ids, kv, b0, b0);
-        load_k(first);
-        load_v(first);
+        load(places(ids, kv, b0, b0), T[0]);
       }
     }
     loaded = follows && b0 < be;

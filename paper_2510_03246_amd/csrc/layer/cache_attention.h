@@ -77,7 +77,11 @@ __device__ __forceinline__ Global<char> opaque(const void* p) {
 
 __device__ __forceinline__ unsigned pick(unsigned a, unsigned b, unsigned sel) { return __builtin_amdgcn_perm(b, a, sel); }
 constexpr unsigned LOWS = 0x05040100u, HIGHS = 0x07060302u;      // the lower, the upper halves of a and b
-// whole numbers 0..15 in bits 0-3 and 16-19 as bf16 of 128 + n, which is exact
-__device__ __forceinline__ unsigned with_128(unsigned x) { return (x & 0x000F000Fu) | 0x43004300u; }
+// Whole numbers 0..15 in bits 0-3 and 16-19 as bf16 of 128 + n, which is exact: one instruction where one of the constants is in a vector register, two where both are known.
+struct Numbers128 {
+  unsigned of_128 = 0x43004300u;
+  __device__ __forceinline__ Numbers128() { asm("" : "+v"(of_128)); }
+  __device__ __forceinline__ unsigned operator()(unsigned x) const { return (x & 0x000F000Fu) | of_128; }
+};
 
 }  // namespace strp

@@ -196,8 +196,9 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
   };
   const int in_page = (1 << c.page_log2) - 1;
 
-  // Units asked for ahead: of 4 bits one is too little to hide the way from memory (eight sequences of 33000 keys, 32 heads of 128 on 8: 84 us instead of 92).
+  // Units asked for ahead: of 4 bits one is too little to hide the way from memory (eight sequences of 33000 keys, 32 heads of 128 on 8: 84 us instead of 92, before shorter code made it 78).
   constexpr int AHEAD = BF && Q4 && W > 2 ? 2 : 1;
+  const Numbers128 with_128;
   struct Tiles {
     TileT t[NT];
     __device__ __forceinline__ TileT& operator[](int i) { return t[i]; }
@@ -375,14 +376,16 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     if constexpr (Q4) qsum = quads_sum(qsum);
 
     floatx4 O[W];
-    float m, l, weight, lowest;            // weight: sum of what the values were multiplied by (of 4 bits: to take 128 off again); lowest: of p lowest
+    float m, l, lowest;
+    floatx4 weight;                        // of 4 bits: lowest: the sum of p lowest; weight, in each entry: of what the whole numbers were multiplied by, to take 128 off again
     bool careful = false, odd;
     while (true) {
       odd = false;
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
       m = -INFINITY;
-      l = weight = lowest = 0.0f;
+      l = lowest = 0.0f;
+      weight = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
       auto unit = [&](int b, Tiles& T) {
         const int k0 = b * UNIT + wave * KW;
         floatx4 S[NT];
@@ -449,7 +452,14 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[t][e] = k0 + 16 * t + 4 * quad + e <= see ? S[t][e] : -INFINITY;
+            for (int e = 0; e < 4; ++e) {
+              const bool seen = k0 + 16 * t + 4 * quad + e <= see;
+              S[t][e] = seen ? S[t][e] : -INFINITY;
+              if constexpr (Q4) {          // lowest and step of a key that is not seen may be anything, and would meet a probability of zero
+                T[t].vs[e >> 1][2 * (e & 1)] = seen ? T[t].vs[e >> 1][2 * (e & 1)] : 0.0f;
+                T[t].vs[e >> 1][2 * (e & 1) + 1] = seen ? T[t].vs[e >> 1][2 * (e & 1) + 1] : 0.0f;
+              }
+            }
         float mt = m;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -466,18 +476,18 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
           for (int j = 0; j < W; ++j) O[j] *= fac;
           m = grown ? mt : m;
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
+        const float ref = m == -INFINITY ? 0.0f : m, ref_log2 = ref * p.scale_log2e;
         float P[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            P[t][e] = __builtin_amdgcn_exp2f((S[t][e] - ref) * p.scale_log2e);      // the difference first: it is exact, or small against what it is taken from
+            if constexpr (BF) P[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[t][e], p.scale_log2e, -ref_log2));
+            else P[t][e] = __builtin_amdgcn_exp2f((S[t][e] - ref) * p.scale_log2e);      // the difference first: it is exact, or small against what it is taken from
             if constexpr (!BF || SPLIT || Q4) l += P[t][e];
             if constexpr (Q4) {
-              const bool seen = whole || k0 + 16 * t + 4 * quad + e <= see;
-              lowest += seen ? P[t][e] * T[t].vs[e >> 1][2 * (e & 1)] : 0.0f;
-              P[t][e] = seen ? P[t][e] * T[t].vs[e >> 1][2 * (e & 1) + 1] : 0.0f;
+              lowest = __builtin_fmaf(P[t][e], T[t].vs[e >> 1][2 * (e & 1)], lowest);
+              P[t][e] *= T[t].vs[e >> 1][2 * (e & 1) + 1];
             }
           }
         // Values.  Where some key is not seen by every row, a value that is not finite would reach those too, by a probability of zero:
@@ -495,13 +505,16 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
               const float h0 = __builtin_bit_cast(float, b0_ & 0xffff0000u), h1 = __builtin_bit_cast(float, b1_ & 0xffff0000u);
               const bf16x2 rest = bf16x2{(__bf16)(x0 - h0), (__bf16)(x1 - h1)};
               lo[d] = __builtin_bit_cast(unsigned, rest);
-              if constexpr (Q4) weight += (h0 + (float)rest[0]) + (h1 + (float)rest[1]);
             } else {
               const bf16x2 one = bf16x2{(__bf16)x0, (__bf16)x1};
               hi[d] = __builtin_bit_cast(unsigned, one);
-              if constexpr (Q4) weight += (float)one[0] + (float)one[1];
-              else l += (float)one[0] + (float)one[1];
+              if constexpr (!Q4) l += (float)one[0] + (float)one[1];
             }
+          }
+          if constexpr (Q4) {
+            const uintx4 ones = uintx4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+            weight = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, hi), weight, 0, 0, 0);
+            if constexpr (SPLIT) weight = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, lo), weight, 0, 0, 0);
           }
           if constexpr (!Q4) {
             if (check)
@@ -615,7 +628,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     l = quads_sum(l);
     if constexpr (Q4) {
       lowest = quads_sum(lowest);
-      if constexpr (BF) lowest -= 128.0f * quads_sum(weight);
+      if constexpr (BF) lowest -= 128.0f * weight[0];
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j] += lowest;
     }

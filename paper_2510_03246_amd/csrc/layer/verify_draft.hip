@@ -46,8 +46,8 @@ struct Exp {
     const unsigned i = (unsigned)__builtin_bit_cast(unsigned long long, t);
     // k and j, whole, into the exponent and behind it: the table has j taken off there
     const uint2 of = ((const uint2*)table)[i & 31];
-    unsigned high;
-    asm("v_lshl_add_u32 %0, %1, 15, %2" : "=v"(high) : "v"(i), "v"(of.y));      // (as an addition of 64 bits it would be three instructions)
+    unsigned high = of.y + (i << 15);
+    asm("" : "+v"(high));                  // (or it becomes an addition of 64 bits, three instructions)
     const double b = __builtin_bit_cast(double, (unsigned long long)high << 32 | of.x);
     return __builtin_fma(b, p, b);
   }

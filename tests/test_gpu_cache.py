@@ -307,14 +307,14 @@ def attention_reference(Q, cache, table, seqs, starts, heads, kv_of, scale, spli
     return out, tol
 
 
-def attention_case(ctx, seqs, heads, kv, dh, page, dts, first=0, behind=0, kv_of=None, scale=None, seed=0, spread=1.5, split=True, extra=2, fix=None):
+def attention_case(ctx, seqs, heads, kv, dh, page, dts, first=0, behind=0, kv_of=None, scale=None, seed=0, spread=1.5, split=True, extra=2, spare=2):
     dt, cdt = dts
     starts = starts_of(seqs, first)
     T = starts[-1] + behind
     pages = sum(-(-(n + p) // page) for n, p in seqs) + extra
     cache = random_cache(pages, kv, page, dh, cdt, seed + 10, bad=True)
     good = random_cache(pages, kv, page, dh, cdt, seed + 10)
-    table = table_for(seqs, page, pages, seed)
+    table = table_for(seqs, page, pages, seed, spare)
     # only what a sequence holds is finite: rows behind it, other pages and the columns of no token are not
     for i, (n, past) in enumerate(seqs):
         for j in range(-(-(n + past) // page) if n else 0):
@@ -323,8 +323,6 @@ def attention_case(ctx, seqs, heads, kv, dh, page, dts, first=0, behind=0, kv_of
             for a, b in zip((cache.K, cache.V, cache.K_scale, cache.V_scale), (good.K, good.V, good.K_scale, good.V_scale)):
                 if a is not None:
                     a[g, :, :rows] = b[g, :, :rows]
-    if fix:
-        fix(cache, table)
     Q = padded(heads * dh, T, seed, dt, spread)
     Q[:, :first] = float("nan")
     Q[:, starts[-1]:] = float("inf")
@@ -370,8 +368,9 @@ def test_attention_long(ctx, dts):
 
 @pytest.mark.parametrize("dts", CASES, ids=IDS)
 def test_attention_of_chunks(ctx, dts):
-    attention_case(ctx, [(300, 500)], 4, 2, 64, 16, dts)
-    attention_case(ctx, [(150, 0), (1, 400), (129, 77), (2, 2), (64, 64)], 4, 1, 128, 64, dts, first=5, seed=1)
+    for spare in (2, 1 << 15):
+        attention_case(ctx, [(300, 500)], 4, 2, 64, 16, dts, spare=spare)
+        attention_case(ctx, [(150, 0), (1, 400), (129, 77), (2, 2), (64, 64)], 4, 1, 128, 64, dts, first=5, seed=1, spare=spare)
 
 
 @pytest.mark.parametrize("dts", CASES, ids=IDS)
@@ -386,14 +385,16 @@ def test_attention_of_chunks(ctx, dts):
     ([(1, 500), (1, 20)], 66, 1, 64, 16, None),                                      # single tokens of many heads
 ], ids=str)
 def test_attention_of_many_rows(ctx, seqs, heads, kv, dh, page, kv_of, dts):
-    attention_case(ctx, seqs, heads, kv, dh, page, dts, kv_of=kv_of, seed=1)
-    attention_case(ctx, seqs, heads, kv, dh, page, dts, kv_of=kv_of, first=7, behind=2, seed=4)
+    """Tables with room for many keys, for which rows are taken 128 at a time however few keys there are; and tables with little, by 16."""
+    for spare in (1 << 20) // page, 2:
+        attention_case(ctx, seqs, heads, kv, dh, page, dts, kv_of=kv_of, seed=1, spare=spare)
+        attention_case(ctx, seqs, heads, kv, dh, page, dts, kv_of=kv_of, first=7, behind=2, seed=4, spare=spare)
 
 
 def test_attention_scales_and_peaked_scores(ctx):
     for dts in CASES:
         attention_case(ctx, [(1, 300), (3, 90)], 4, 2, 64, 16, dts, scale=1e-6)
-        attention_case(ctx, [(100, 200)], 4, 2, 64, 16, dts, scale=1.0, spread=1.0, seed=3)
+        attention_case(ctx, [(100, 200)], 4, 2, 64, 16, dts, scale=1.0, spread=1.0, seed=3, spare=1 << 16)
         attention_case(ctx, [(1, 300), (3, 90)], 4, 2, 64, 16, dts, scale=2.0, spread=0.5, seed=2)
 
 
@@ -401,18 +402,20 @@ def test_attention_scales_and_peaked_scores(ctx):
 def test_attention_with_rounded_probabilities(fast, dh):
     for cdt in (BF16, Q4):
         attention_case(fast, [(1, 300), (3, 90), (1, 3000), (200, 20), (70, 2000)], 4, 2, dh, 16, (BF16, cdt), split=False)
+        attention_case(fast, [(1, 300), (200, 20), (70, 2000)], 4, 2, dh, 16, (BF16, cdt), split=False, spare=1 << 15)
 
 
 @pytest.mark.parametrize("dts", CASES[:2], ids=IDS[:2])
+@pytest.mark.parametrize("spare", [2, 1 << 15])
 @pytest.mark.parametrize("n", [1, 4, 100, 200])
-def test_values_that_are_not_finite_show_where_they_are_seen(ctx, dts, n):
+def test_values_that_are_not_finite_show_where_they_are_seen(ctx, dts, n, spare):
     """A value of infinity that later tokens of a tile see and earlier ones do not: theirs alone; one that all see: in all."""
     past, heads, dh = 200, 2, 64
     for at in (past + n - 1, past + n // 2, 3):
         def plant(cache, table):
             cache.V[int(table[0, at // 16]), 0, at % 16, 5] = float("inf")
         cache = random_cache(60, 1, 16, dh, dts[1], 1)
-        table = table_for([(n, past)], 16, 60, 1)
+        table = table_for([(n, past)], 16, 60, 1, spare)
         plain = copy_of(cache)
         Q = rand((heads * dh, ld8(n)), 3, dts[0])
         want = ctx.strp_cache_attention(Q, n, heads, plain, table, ints([past]))[:, :n]
@@ -430,12 +433,13 @@ def test_values_that_are_not_finite_show_where_they_are_seen(ctx, dts, n):
 @pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("n", [1, 4, 33, 100, 200])
 @pytest.mark.parametrize("scale", ["K_scale", "V_scale"])
-def test_scales_of_4_bits_that_are_not_finite_show_where_they_are_seen(ctx, dt, n, scale):
+@pytest.mark.parametrize("spare", [2, 1 << 15])
+def test_scales_of_4_bits_that_are_not_finite_show_where_they_are_seen(ctx, dt, n, scale, spare):
     """The tokens that see such a key have nothing that is finite in that head, the others what they had."""
     past, heads, dh = 200, 2, 64
     for at, bad in ((past + n - 1, float("inf")), (past + n // 2, float("nan")), (3, -float("inf"))):
         cache = random_cache(60, 2, 16, dh, Q4, 1)
-        table = table_for([(n, past)], 16, 60, 1)
+        table = table_for([(n, past)], 16, 60, 1, spare)
         Q = rand((heads * dh, ld8(n)), 3, dt)
         want = ctx.strp_cache_attention(Q, n, heads, cache, table, ints([past]))[:, :n].clone()
         getattr(cache, scale)[int(table[0, at // 16]), 0, at % 16, 1] = bad if scale == "V_scale" else float("nan")
@@ -479,17 +483,21 @@ def test_attention_beyond_32_bit_offsets(ctx):
 
 
 @pytest.mark.parametrize("dts", CASES, ids=IDS)
-def test_attention_wrong_tables_stay_in_bounds(ctx, dts):
+@pytest.mark.parametrize("columns", [0, 1 << 16])
+def test_attention_wrong_tables_stay_in_bounds(ctx, dts, columns):
     cache = random_cache(4, 2, 16, 64, dts[1], 1)
     Q = rand((256, 40), 2, dts[0])
     for table, past, starts in (([[-1, 99]], [20], [0, 40]), ([[0, 1], [2, 3]], [1 << 30, -7], [0, 3, 5]), ([[0, 1], [2, 3]], [5, 5], [0, 50, 20]),
                                 ([[0, 1], [2, 3]], [5, 5], [-9, 4, 1 << 30]), ([[0]], [15], [7, 7]), ([[0], [1]], [0, 0], [30, 10, 35])):
         C = torch.full((256, 40), 7.0, dtype=dts[0], device="cuda")
-        ctx.strp_cache_attention(Q, 40, 4, cache, ints(table), ints(past), ints(starts), out=C)
+        wide = torch.cat([ints(table), torch.full((len(table), columns), 77, dtype=torch.int32, device="cuda")], 1).contiguous()
+        ctx.strp_cache_attention(Q, 40, 4, cache, wide, ints(past), ints(starts), out=C)
         if starts == [7, 7]:
             assert (C == 7.0).all()
-    C = ctx.strp_cache_attention(Q, 40, 4, cache, ints([[0, 1, 2, 3]]), ints([24]), kv_of_head=ints([5, -1, 0, 1]))
-    want = ctx.strp_cache_attention(Q, 40, 4, cache, ints([[0, 1, 2, 3]]), ints([24]), kv_of_head=ints([1, 0, 0, 1]))
+    whole = torch.full((1, 4 + columns), -1, dtype=torch.int32, device="cuda")
+    whole[0, :4] = ints([0, 1, 2, 3])
+    C = ctx.strp_cache_attention(Q, 40, 4, cache, whole, ints([24]), kv_of_head=ints([5, -1, 0, 1]))
+    want = ctx.strp_cache_attention(Q, 40, 4, cache, whole, ints([24]), kv_of_head=ints([1, 0, 0, 1]))
     assert torch.equal(C, want) and torch.isfinite(C).all()
 
 

@@ -56,7 +56,8 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
   typedef Tile<E, Q4, W> TileT;
   constexpr int NC = TileT::NC, DH = 16 * W;
   constexpr int NT = BF || Q4 ? 2 : 1, KW = 16 * NT, UNIT = 4 * KW;      // tiles and keys of a wavefront in a unit, keys of a unit
-  constexpr int EXTRA = 2;                 // units that a tile counts beyond its keys'
+  // units that a tile counts beyond its keys' (64 sequences of 0 to 4000 keys, bf16: none 143 us, 1 134, 2 120, 4 121; the fp32 case 2 48 us, 1 46)
+  constexpr int EXTRA = BF ? 2 : 1;
   auto& sO = ((RowsLds<W>*)smem)->o;
   __shared__ float sM[4][ROWS], sL[4][ROWS];
   __shared__ long long sOff[ROWS];
@@ -413,12 +414,13 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
           } else if constexpr (!Q4) {
 #pragma unroll
             for (int i = 0; i < NC; ++i)
+              if (16 * i < dh)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float k = T[t].k[i][e];
-                if (16 * i + 16 > dh) k = 16 * i + 4 * quad < dh ? k : 0.0f;
-                S[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, qf[4 * i + e], S[t], 0, 0, 0);
-              }
+                for (int e = 0; e < 4; ++e) {
+                  float k = T[t].k[i][e];
+                  if (16 * i + 16 > dh) k = 16 * i + 4 * quad < dh ? k : 0.0f;
+                  S[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k, qf[4 * i + e], S[t], 0, 0, 0);
+                }
           } else {
 #pragma unroll
             for (int i = 0; i < NC; ++i)

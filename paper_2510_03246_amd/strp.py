@@ -236,6 +236,7 @@ class Context:
     def __init__(self, device=0, workspace_bytes: int | None = None):
         self.lib = load_library()
         self.device = torch.device("cuda", device)
+        self.index = self.device.index            # for the comparison in every call, where an attribute of an attribute costs twice
         torch.cuda.set_device(self.device)
         self.stream = torch.cuda.current_stream(self.device)
         h = C.c_void_p()
@@ -399,7 +400,7 @@ class Context:
     def _matrix(self, name, t, rows, cols, dtypes):
         """Leading dimension of t as an operand of `rows` rows and at least `cols` columns, of one of the dtypes, on this context's device."""
         shape = t.shape
-        if t.get_device() != self.device.index:
+        if t.get_device() != self.index:
             raise ValueError(f"{name} is on {t.device}, the context on {self.device}")
         if t.dtype not in dtypes:
             raise TypeError(f"{name}: unsupported dtype {t.dtype}")
@@ -415,11 +416,12 @@ class Context:
         """Address of a contiguous vector of at least n entries; 0 for None."""
         if t is None:
             return 0
-        if t.get_device() != self.device.index:
+        if t.get_device() != self.index:
             raise ValueError(f"{name} is on {t.device}, the context on {self.device}")
         if t.dtype is not dtype:
             raise TypeError(f"{name}: {t.dtype}, needs {dtype}")
-        if t.dim() != 1 or t.shape[0] < n or (n > 1 and t.stride(0) != 1):
+        shape = t.shape
+        if len(shape) != 1 or shape[0] < n or (n > 1 and not t.is_contiguous()):
             raise ValueError(f"{name}: needs {n} contiguous entries")
         return t.data_ptr()
 
@@ -508,7 +510,7 @@ class Context:
     # ---- what a model needs to generate ---------------------------------------------------
     def _pages(self, cache, table, past, seq_start, T):
         """Fields of strp_cache for a call on T tokens."""
-        if cache.device != self.device.index or table.get_device() != self.device.index:
+        if cache.device != self.index or table.get_device() != self.index:
             raise ValueError(f"the cache or its table is not on {self.device}")
         if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous():
             raise ValueError("table: needs contiguous int32 rows, one a sequence")
@@ -519,21 +521,24 @@ class Context:
         """Keys and values [kv_heads*d_head x ld] of T new tokens into the cache's pages: those of sequence i (tokens seq_start[i] to seq_start[i + 1]; None:
         one sequence of all) behind the past[i] that it has, in the pages table[i].  inv_freq [rot / 2] fp32: the first rot channels of every head of K and Q are
         turned by position * inv_freq, channels (j, j + rot / 2) together, or (2j, 2j + 1) with pairs.  Returns Q turned (q_out may be Q), None without Q."""
-        rows, dts = cache.kv_heads * cache.d_head, _CODES
-        ldk, ldv = self._matrix("K", K, rows, T, dts), self._matrix("V", V, rows, T, (K.dtype,))
+        dt, dh = K.dtype, cache.d_head
+        rows = cache.kv_heads * dh
+        ldk, ldv = self._matrix("K", K, rows, T, _CODES), self._matrix("V", V, rows, T, (dt,))
         heads = q = r = ldq = ldr = 0
         if Q is not None:
-            if Q.dim() != 2 or Q.shape[0] % cache.d_head:
-                raise ValueError(f"Q: {tuple(Q.shape)} is not heads of {cache.d_head}")
-            heads = Q.shape[0] // cache.d_head
+            if Q.dim() != 2 or Q.shape[0] % dh:
+                raise ValueError(f"Q: {tuple(Q.shape)} is not heads of {dh}")
+            rows = Q.shape[0]
+            heads = rows // dh
+            ldq = self._matrix("Q", Q, rows, T, (dt,))
             if q_out is None:
-                q_out = self._new(Q.shape[0], T, Q.dtype)
-            ldq, ldr = self._matrix("Q", Q, Q.shape[0], T, (K.dtype,)), self._matrix("q_out", q_out, Q.shape[0], T, (K.dtype,))
+                q_out = self._new(rows, T, dt)
+            ldr = ldq if q_out is Q else self._matrix("q_out", q_out, rows, T, (dt,))
             q, r = Q.data_ptr(), q_out.data_ptr()
         rot = 0 if inv_freq is None else 2 * inv_freq.shape[0]
         self.check(self.lib.strp_cache_append(self.h, _CACHE_APPEND.pack(
             *self._pages(cache, table, past, seq_start, T), K.data_ptr(), V.data_ptr(), q, r, self._vector("inv_freq", inv_freq, rot // 2, torch.float32),
-            _CODES[K.dtype], heads, rot, bool(pairs), T, ldk, ldv, ldq, ldr)))
+            _CODES[dt], heads, rot, bool(pairs), T, ldk, ldv, ldq, ldr)))
         return q_out if q else None
 
     def strp_cache_attention(self, Q, T, heads, cache, table, past, seq_start=None, kv_of_head=None, scale=None, out=None):

@@ -729,13 +729,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
     return;
   }
   const int worker = (int)blockIdx.x, row = (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int parts = p.parts[worker];
-  if (parts == 0) return;
   const long long first = (long long)worker * 2 + 1, to = p.off[first * ROWS + row];
-  if (to < 0) return;
+  const int parts = p.parts[worker];
+  if (parts == 0 || to < 0) return;
   const int dh = p.c.dh, ch = 2 * lane;
   float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
-  constexpr int UN = 8;
+  constexpr int UN = 4;
   for (int i0 = wave; i0 < parts; i0 += 4 * UN) {
     float2 ml[UN], x[UN];
 #pragma unroll

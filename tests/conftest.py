@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -10,6 +11,16 @@ if ROOT not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
+
+
+def pytest_collection_finish(session):
+    gc.collect()
+    gc.freeze()                                   # what is loaded by now is not looked through again
+
+
+def pytest_runtest_logfinish(nodeid, location):
+    """What a test leaves in cycles goes with it: in another test that counts the device's memory it would go at any time."""
+    gc.collect()
 
 
 @pytest.fixture(scope="session")

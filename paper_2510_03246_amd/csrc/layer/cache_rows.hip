@@ -724,11 +724,13 @@ template <typename E>
 __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
   __shared__ float sO[4][128];
   __shared__ float sM[4], sL[4];
+  // a tile's workgroups are on different XCDs: what one reads for itself comes an eighth as fast (105 tokens, 6 heads, on 31000 keys of 4 bits: join 34 us on one, 26 on all)
+  const int worker = (int)(blockIdx.x + blockIdx.y) & (WORKERS - 1);
   if (sizeof(E) == 2 && blockIdx.x >= (unsigned)WORKERS) {
-    if constexpr (sizeof(E) == 2) wide_join(p, (int)blockIdx.x - WORKERS, (int)blockIdx.y);
+    if constexpr (sizeof(E) == 2) wide_join(p, worker, (int)blockIdx.y);
     return;
   }
-  const int worker = (int)blockIdx.x, row = (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = (int)blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const long long first = (long long)worker * 2 + 1, to = p.off[first * ROWS + row];
   const int parts = p.parts[worker];
   if (parts == 0 || to < 0) return;

@@ -355,6 +355,7 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       }
       return Probs{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
     };
+    [[maybe_unused]] Packed pending;       // of 4 bits: K two units ahead and V one, on their way for a unit already
     // Unit b, whose scores are in S; those of the next one go to N.
     auto unit = [&](int b, Scores& S, Scores& N) {
       if constexpr (Q4) {
@@ -364,9 +365,9 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
         __builtin_amdgcn_s_barrier();      // K of the next unit and V of this one are there, and nobody reads those before them any more
       }
       [[maybe_unused]] Packed packed;
-      const long long row = next_row;      // of unit b + 1
+      const long long row = next_row;      // of unit b + 1, of 4 bits b + 2
       if constexpr (Q4) {
-        next_row = page_of(b + 2);         // (what lies behind the last unit is asked for too, and nobody looks at it: a condition here would cost registers)
+        next_row = page_of(b + 3);         // (what lies behind the last unit is asked for too, and nobody looks at it: a condition here would cost registers)
         packed = ask_packed(next_row, row);
       } else if (b + 1 < b1) {
         if (b + 2 < b1) issue_k(b + 2);
@@ -397,7 +398,7 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
               S.u[t][e] = 32 * t + 8 * (e >> 2) + (e & 3) > to ? -INFINITY : S.u[t][e];
               __builtin_amdgcn_sched_barrier(0);       // one comparison at a time, or their results take the scalar registers
             }
-        // products first: while they go on, another wavefront has the vector unit (4 bits: 317 us without, 299 for 1024 tokens on 6000 keys; bf16 the same)
+        // products first: while they go on, another wavefront has the vector unit (4 bits: 317 us without, 299 for 1024 tokens on 6000 keys; bf16 the same; with a unit more on its way 292)
         __builtin_amdgcn_s_setprio(0);
         const float ref = raise(S);
         __builtin_amdgcn_s_setprio(1);
@@ -473,10 +474,11 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       }
       if constexpr (Q4)
         if (b + 1 < b1) {
-          put_packed(packed, toK, toV, b + 2);
+          put_packed(pending, toK, toV, b + 2);
           ahead(toK, ldsK);
           ahead(toV, ldsV);
         }
+      if constexpr (Q4) pending = packed;
       ahead(atV, ldsV);
     };
     int* lost_of = (int*)smem;             // between the passes, of the four wavefronts
@@ -495,9 +497,10 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       Scores a, b;
       clear(a);
       if constexpr (Q4) {
-        const long long row = page_of(b0);
-        next_row = page_of(b0 + 1);
-        const Packed x = ask_packed(row, row), y = ask_packed(next_row, row);
+        const long long row = page_of(b0), second = page_of(b0 + 1);
+        next_row = page_of(b0 + 2);
+        const Packed x = ask_packed(row, row), y = ask_packed(second, row);
+        pending = ask_packed(next_row, second);
         put_packed(x, toK, toV, b0 + 3);                 // (its V comes again with the next; the slots of three units further are its own)
         ahead(toK, ldsK);
         __syncthreads();

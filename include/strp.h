@@ -465,7 +465,7 @@ size_t strp_cache_attention_workspace_bytes(int32_t d_head);
  *   everywhere), p behind the last one where all are;  u [T], u_next [n_seq] fp32 in [0, 1) are the caller's random numbers.
  *   From u_next = 1 on: the last v with r(v) > 0.  A position where a distribution that is needed has a NaN, +inf or nothing but -inf ends
  *   the sequence there, with next_id -1.
- * All of it is worked out in 64 bits, where 32 would put a token beside its place now and then.  Wrong entries of draft_start give wrong results,
+ * All of it is worked out in 64 bits (exponentials to 2^-43), where 32 would put a token beside its place now and then.  Wrong entries of draft_start give wrong results,
  * no access out of bounds.
  * Errors: STRP_EINVAL (null target, u_next, accepted or next_id, T > 0 without draft, draft_id and u, or without
  * draft_start where n_seq > 1, V or n_seq not positive, V above 2^30, T above

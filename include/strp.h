@@ -449,7 +449,7 @@ typedef struct {
   int64_t T, ldq, ldc;
 } strp_cache_attention_in;
 strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* in);
-/* Workspace (bytes, device) that strp_cache_attention needs for any call with this d_head; pure function. */
+/* Workspace (bytes, device) that strp_cache_attention needs for any call with this d_head (78 MB at 128); pure function. */
 size_t strp_cache_attention_workspace_bytes(int32_t d_head);
 
 /*

@@ -53,10 +53,8 @@ struct Exp {
     return __builtin_fma(b, p, b);
   }
   // 0 where y is below -700 or NaN
-  __device__ __forceinline__ double operator()(double y) const {
-    const double x = y * UNITS;
-    return x >= LOWEST ? near(x) : 0.0;
-  }
+  __device__ __forceinline__ double of_units(double y) const { return y >= LOWEST ? near(y) : 0.0; }
+  __device__ __forceinline__ double operator()(double y) const { return of_units(y * UNITS); }
 };
 
 // Sum of e^((x - ref) / temperature) over some entries.  ref is one of them and no more than 500 temperatures below any: with 64 bits it need not be the largest.
@@ -88,6 +86,12 @@ struct VerifyP {
   double* sums;                            // [n_seq][parts][2] of r and of p
 };
 
+// An exponent is x scale - from with from = ref scale, rounded: one instruction, but what that rounding took stays in every exponent, ref's own among them, and grows with ref / temperature.
+// It is one number a reference, so the sum by it is put right at its end (otherwise 10^-9 of it at logits of 20 and a temperature of 10^-6, 10^-3 at 10^-12, and anything at 10^-16).
+// From references of FAR units on differences come first: what is left would outgrow the exponents, and neighbouring logits are 2^21 units apart.
+constexpr double FAR = 35184372088832.0;   // 2^45
+__device__ __forceinline__ double left_over(float ref, double from, double scale) { return fabs(from) < FAR ? __builtin_fma((double)ref, scale, -from) : 0.0; }
+
 template <typename E>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
   constexpr int VEC = 16 / sizeof(E), UN = 2;
@@ -102,6 +106,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
   const int n = of_draft ? p.T : p.columns, v0 = (int)blockIdx.y * p.rows, v1 = min(v0 + p.rows, p.V);
   double sum[VEC], from[VEC];              // from: ref / temperature, in the units of Exp
   float ref[VEC], most[VEC], high[VEC];    // high: what ref may not stay behind
+  bool apart = false;                      // some reference is FAR
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
     sum[e] = from[e] = 0.0;
@@ -146,16 +151,29 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (most[e] > high[e]) {
-            sum[e] *= ref[e] == -INFINITY ? 0.0 : ex(((double)ref[e] - (double)most[e]) * p.inv);
+            const double to = (double)most[e] * scale;
+            sum[e] *= ref[e] == -INFINITY ? 0.0 : ex.of_units(((double)ref[e] - (double)most[e]) * scale - left_over(ref[e], from[e], scale) + left_over(most[e], to, scale));
             ref[e] = most[e];
             high[e] = ref[e] + reach;
-            from[e] = (double)ref[e] * scale;
+            from[e] = to;
+            apart = apart || !(fabs(to) < FAR);
           }
       }
+      // (the lower bound, for -inf and NaN too: e^-700 is nothing beside ref's own share)
+      if (__builtin_amdgcn_ballot_w64(apart)) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e)
+        for (int e = 0; e < VEC; ++e)
+#pragma unroll 1
+          for (int k = 0; k < N; ++k) {
+            const double y = fabs(from[e]) < FAR ? __builtin_fma((double)f[k][e], scale, -from[e]) : ((double)f[k][e] - (double)ref[e]) * scale;
+            sum[e] += ex.near(fmax(y, LOWEST));
+          }
+      } else {
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum[e] += ex.near(fmax(__builtin_fma((double)f[k][e], scale, -from[e]), LOWEST));      // e^-700, for -inf and NaN too, is nothing beside ref's own share
+        for (int e = 0; e < VEC; ++e)
+#pragma unroll
+          for (int k = 0; k < N; ++k) sum[e] += ex.near(fmax(__builtin_fma((double)f[k][e], scale, -from[e]), LOWEST));
+      }
     };
     int v = v0 + r;
     if (v < v1) {
@@ -178,7 +196,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyP p) {
     }
   }
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) sum[e] = ref[e] == -INFINITY ? 0.0 : sum[e];
+  for (int e = 0; e < VEC; ++e) sum[e] = ref[e] == -INFINITY ? 0.0 : sum[e] * ex.near(-left_over(ref[e], from[e], scale));
   // one reference for the slice, and the sums by it: over the wavefront, then the four of them
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {

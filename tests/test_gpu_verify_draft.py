@@ -257,3 +257,70 @@ def test_binding_refusals(ctx):
                       (strp.StrpError, lambda: ctx.strp_verify_draft(t, None, None, None, un[:0]))):
         with pytest.raises(err):
             call()
+
+
+# ---- temperatures at which a logit is 10^10 of them and more ----
+def softmax_apart(x, tau):
+    """Differences first: exact, or within 2^-53, where x / tau would lose them."""
+    x = x.double()
+    e = torch.exp((x - x.amax(0)) / tau)
+    return e / e.sum(0)
+
+
+def ties(V, cols, seed, dt, level, rows):
+    """Random logits below `level` and, in every column, `rows` of them at it: what is left of the distribution at a temperature of next to nothing."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.full((V, ld8(max(cols, 1))), float("nan"), dtype=dt, device="cuda")
+    top = torch.full((), level, device="cuda").to(dt).float()
+    x[:, :cols] = (top - top.abs() * (2.0 ** -6 + torch.rand((V, cols), generator=g, device="cuda"))).to(dt)
+    x[rows, :cols] = top.to(dt)
+    return x
+
+
+COLD = [1.0, 1e-3, 1e-6, 1e-10, 1e-12, 1e-14, 1e-16, 1e-18, 1e-21, 1e-24, 1e-30]
+
+
+@pytest.mark.parametrize("dt", [BF16, F32])
+@pytest.mark.parametrize("level", [20.3, -20.3, 3.0e4, -3.1e4, 1.0e30])
+def test_verify_the_normaliser_at_low_temperatures(ctx, dt, level):
+    """Five equal best tokens in the target and four in the draft, three of them the same; another level in the draft, so that nothing cancels.  Where the others
+    have no weight, p = 1/5 and q = 1/4, and a draft is kept below u = 0.8: fp32's neighbours of that are 1.5e-8 and 4.5e-8 away, while exponentials to 2^-43, a
+    factor 1 / temperature and a difference rounded once each (40 * 2^-52 where a weight counts) and sums of V terms make less than 2^-40."""
+    V, tol = 700, 2.0 ** -40
+    best_t, best_d = [3, 77, 300, 512, 699], [77, 300, 512, 613]
+    counts = [1, 1, 0, 3, 2, 0, 1]
+    starts = [0]
+    for n in counts:
+        starts.append(starts[-1] + n)
+    T, n_seq = starts[-1], len(counts)
+    above = float(torch.tensor(0.8, dtype=F32))                   # the nearest, above 0.8
+    below = above - 2.0 ** -24
+    assert below < 0.8 < above
+    target, draft = ties(V, T + n_seq, 1, dt, level, best_t), ties(V, T, 2, dt, level * 0.83, best_d)
+    ids = [300, 300, 77, 512, 300, 512, 77, 613]
+    us = [below, above, below, below, above, 0.1, 0.7, 0.3]
+    un = [0.1, 0.3, 0.5, 0.7, 0.9, 0.99, 0.19]
+    for tau in COLD:
+        got = ctx.strp_verify_draft(target, draft, ints(ids), floats(us), floats(un), ints(starts), tau)
+        none = ctx.strp_verify_draft(target[:, :ld8(n_seq)].contiguous(), None, None, None, floats(un), None, tau)
+        p, q = softmax_apart(target[:, :T + n_seq], tau), softmax_apart(draft[:, :T], tau)
+        if tau < 1e-2 * abs(level) / 700:
+            assert abs(float(p[3, 0]) - 0.2) < 1e-15 and abs(float(q[77, 0]) - 0.25) < 1e-15
+        for s, a in enumerate(starts[:-1]):
+            n, at = counts[s], 0
+            u32, goal = floats(us).double().tolist(), float(floats(un)[s])
+            while at < n:
+                left, right = u32[a + at] * float(q[ids[a + at], a + at]), float(p[ids[a + at], a + s + at])
+                assert abs(left - right) > tol * right            # the case is no matter of rounding
+                if not left < right:
+                    break
+                at += 1
+            assert int(got["accepted"][s]) == at, (tau, s, int(got["accepted"][s]), at)
+            r = p[:, a + s + at]
+            if at < n:
+                r = (r - q[:, a + at]).clamp_min(0)
+            for r, answer in ((r, int(got["next_ids"][s])), (p[:, s], int(none["next_ids"][s]))):
+                c = torch.cumsum(r, 0)
+                over = int((c > goal * float(c[-1])).nonzero()[0])
+                assert answer == over or float((c - goal * float(c[-1])).abs().min()) < tol, (tau, s, answer, over)
+        assert none["accepted"].tolist() == [0] * n_seq

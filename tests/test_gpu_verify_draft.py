@@ -324,3 +324,35 @@ def test_verify_the_normaliser_at_low_temperatures(ctx, dt, level):
                 over = int((c > goal * float(c[-1])).nonzero()[0])
                 assert answer == over or float((c - goal * float(c[-1])).abs().min()) < tol, (tau, s, answer, over)
         assert none["accepted"].tolist() == [0] * n_seq
+
+
+def test_verify_neighbouring_logits_at_a_temperature_between(ctx):
+    """fp32 neighbours that are some hundred temperatures apart: 64 and what follows it, 763 at 1e-8.  Only the larger ones, one entry in a hundred, have a weight: p = 1 / N, and a
+    draft of q = 1 / M, M of the same entries, is kept below u = M / N."""
+    V, n_seq = 50000, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    more = torch.rand((V, 2 * n_seq), generator=g, device="cuda") < 0.01
+    more[0] = False
+    more[7] = True
+    more[:, 1::2] = more[:, ::2]                                  # a sequence's position and the one behind it
+    N = more[:, ::2].sum(0)
+    M = N - N // 20
+    of = more[:, ::2]
+    draft = torch.where(of & (torch.cumsum(of, 0) <= M), 0.0, -math.inf)
+    u_next = torch.rand(n_seq, generator=g, device="cuda")
+    ids, starts = torch.full((n_seq,), 7, dtype=torch.int32, device="cuda"), ints(list(range(n_seq + 1)))
+    for low in (64.0, -64.0, 1.0, 3.7e-3):
+        lo = torch.full((V, 2 * n_seq), low, device="cuda")
+        hi = torch.nextafter(lo, torch.full_like(lo, math.inf))
+        x = torch.where(more, hi, lo)
+        for apart in (260.0, 400.0, 520.0, 700.0, 763.0, 990.0, 1020.0, 1500.0):
+            tau = float(hi[0, 0].double() - lo[0, 0].double()) / apart
+            for factor, kept in ((0.999, 1), (1.001, 0)):
+                got = ctx.strp_verify_draft(x, draft, ids, (M / N * factor).float(), u_next, starts, tau)
+                assert got["accepted"].tolist() == [kept] * n_seq, (low, apart, factor)
+                if kept:
+                    for s in range(0, n_seq, 7):
+                        at = of[:, s].nonzero()[:, 0]
+                        place = float(u_next[s]) * len(at)
+                        assert abs(place - round(place)) > 1e-6   # equal weights: the answer's place among them
+                        assert int(got["next_ids"][s]) == int(at[math.floor(place)]), (low, apart, s)

@@ -59,6 +59,21 @@ __device__ __forceinline__ float both_32(float x, bool sum) {
 __device__ __forceinline__ float quads_max(float x) { return both_32(both_16(x, false), false); }
 __device__ __forceinline__ float quads_sum(float x) { return both_32(both_16(x, true), true); }
 
+// Exponents in bf16 are S scale - R with R = m scale, rounded: one instruction from a score S and the row's maximum m.  What that rounding took, m scale - R, is in every exponent by m, so results by
+// different maxima are brought together with it (else a part's weight is off by up to 2^-24 of its score in powers of two, and from scores of 10^9 on beyond what exp2 holds).
+// From R of FAR on differences come first: S is given less m, and R is 0.  In fp32 they always do.
+constexpr float FAR = 1048576.0f;          // 2^20: what is left is 2^-5 at most
+template <bool BF>
+__device__ __forceinline__ float left_over(float m, float scale) {
+  const float r = m * scale;
+  return BF && fabsf(r) < FAR ? __builtin_fmaf(m, scale, -r) : 0.0f;
+}
+// what results by the maximum m are multiplied by to be such by `to`, which is not below it
+template <bool BF>
+__device__ __forceinline__ float between(float m, float to, float scale) {
+  return __builtin_amdgcn_exp2f((m - to) * scale + (left_over<BF>(to, scale) - left_over<BF>(m, scale)));
+}
+
 // a value that all lanes have, in scalar registers
 __device__ __forceinline__ long long uniform(long long x) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));

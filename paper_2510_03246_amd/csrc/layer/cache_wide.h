@@ -300,7 +300,7 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
         for (int t = 0; t < U; ++t) S.u[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_k(from, d, t), qf[d], S.u[t], 0, 0, 0);
     };
     // the running maximum with a tile's scores, what is held rescaled to it; returns what is to be taken from a score in powers of two
-    auto raise = [&](const Scores& S) {
+    auto raise = [&](Scores& S) {
       float mt = m;
 #pragma unroll
       for (int t = 0; t < U; ++t)
@@ -310,7 +310,7 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
       // what a row holds stays as it is until its maximum has grown past 2^8 times: probabilities of up to 256 are as good as those below 1
       const bool grown = !((mt - m) * p.scale_log2e <= 8.0f || mt == -INFINITY);
       if (__builtin_amdgcn_ballot_w64(grown)) {
-        const float fac = grown ? __builtin_amdgcn_exp2f((m - mt) * p.scale_log2e) : 1.0f;
+        const float fac = grown ? between<true>(m, mt, p.scale_log2e) : 1.0f;
         l[0] *= fac;
         if constexpr (!SPLIT || Q4) l[1] *= fac;
         if constexpr (Q4) lowest *= fac;
@@ -320,7 +320,14 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
           for (int e = 0; e < 16; ++e) O[ch][e] *= fac;
         m = grown ? mt : m;
       }
-      return m == -INFINITY ? 0.0f : m * p.scale_log2e;
+      const float ref = m == -INFINITY ? 0.0f : m, ref_log2 = ref * p.scale_log2e;
+      const bool far = !(fabsf(ref_log2) < FAR);
+      if (__builtin_amdgcn_ballot_w64(far))
+#pragma unroll
+        for (int t = 0; t < U; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) S.u[t][e] -= far ? ref : 0.0f;
+      return far ? 0.0f : ref_log2;
     };
     // Probabilities of the quarter k of a tile's keys and, in fp32, their sum.  SPLIT: hi has their upper 16 bits and lo what that leaves, together within 2^-16 of them;
     // else hi is rounded to bf16 and the sum is of what was rounded.
@@ -614,7 +621,7 @@ __device__ __forceinline__ void wide_join(const RowsP& p, int worker, int y) {
       float most = m;
 #pragma unroll
       for (int k = 0; k < UN; ++k) most = i0 + k < parts ? __builtin_elementwise_maximum(most, ml[k].x) : most;
-      const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((of - most) * p.scale_log2e); };
+      const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : between<true>(of, most, p.scale_log2e); };
       const float f = factor(m);
       m = most;
       l *= f;

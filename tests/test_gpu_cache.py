@@ -633,3 +633,44 @@ def test_binding_refusals(ctx):
                       (ValueError, lambda: ctx.strp_cache_attention(Q, 4, 4, cache, table, past, out=torch.empty((256, 8), device="cpu", dtype=BF16)))):
         with pytest.raises(err):
             call()
+
+
+# ---- scores that are large beside what tells them apart ----
+@pytest.mark.parametrize("dts", CASES, ids=IDS)
+@pytest.mark.parametrize("n,past,spare", [(1, 700, 2), (3, 90, 2), (200, 400, 1 << 15), (200, 400, 2)], ids=["1", "3", "200-wide", "200"])
+def test_attention_of_large_scores(ctx, dts, n, past, spare):
+    """Whole scores about 524288, the best of every part of the keys another one: exact in fp32 (numbers of 4 bits enter with up to 255 of their query beside them: below 2^24), so a
+    probability is off by what its exponent is (64 2^-23: differences of up to 32 in powers of two, where it counts, rounded twice, and a scale rounded once), whatever the scale."""
+    heads, dh, page, keys = 2, 64, 16, past + n
+    pages = -(-keys // page)
+    g = torch.Generator(device="cuda").manual_seed(n + spare)
+    whole = torch.randint(0, 16, (pages, 1, page, dh), generator=g, device="cuda")
+    whole[..., 0] = 15
+    v = torch.randint(0, 16, (pages, 1, page, dh), generator=g, device="cuda")
+    if dts[1] == Q4:
+        scales = torch.ones((pages, 1, page, 2), device="cuda")
+        scales[..., 0] = -7.0
+        pack = lambda x: (x[..., ::2] | (x[..., 1::2] << 4)).to(torch.uint8)
+        cache = strp.PagedCache(pack(whole), pack(v), scales, scales.clone())
+    else:
+        cache = strp.PagedCache((whole - 7).to(dts[1]), (v - 7).to(dts[1]))
+    table = torch.full((1, pages + spare), -1, dtype=torch.int32)
+    table[0, :pages] = torch.randperm(pages, generator=torch.Generator().manual_seed(1)).to(torch.int32)
+    table = table.cuda()
+    Q = torch.zeros((heads * dh, ld8(n)), device="cuda")
+    for h in range(heads):
+        Q[h * dh:h * dh + 24] = torch.randint(-1, 2, (24, ld8(n)), generator=g, device="cuda").float()
+        Q[h * dh] = 65536.0
+    Q = Q.to(dts[0])
+    K, V = (x[table[0, :pages].long(), 0].reshape(-1, dh)[:keys] for x in values(cache))
+    seen = torch.ones((n, keys), dtype=torch.bool, device="cuda").tril(past)
+    for scale in (1e-5, 0.03, 0.9, 1.3, 1.6, 40.0, 1e4, 1e9, 1e13, 1e30, 2e38):
+        C = ctx.strp_cache_attention(Q, n, heads, cache, table, ints([past]), scale=scale)
+        scale = float(torch.tensor(scale, dtype=F32))
+        for h in range(heads):
+            s = torch.where(seen, Q[h * dh:(h + 1) * dh, :n].double().t() @ K.t(), -math.inf)
+            p = torch.softmax(scale * (s - s.max(1, keepdim=True).values), 1)
+            o = (p @ V).t()
+            mag = 262.0 if dts[1] == Q4 else 8.0                  # of what is summed for a key: 255 and 7 beside it
+            tol = 2 * (64 + keys + 64) * U * mag + 2.0 ** -16 * 8.0 + H(dts[0]) * o.abs()
+            close(C[h * dh:(h + 1) * dh, :n], o, tol, (scale, h))

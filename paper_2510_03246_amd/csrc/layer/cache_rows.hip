@@ -200,7 +200,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 
   // Units asked for ahead: of 4 bits one is too little to hide the way from memory (eight sequences of 33000 keys, 32 heads of 128 on 8: 84 us instead of 92, before shorter code made it 78).
   constexpr int AHEAD = BF && Q4 && W > 2 ? 2 : 1;
-  const Numbers128 with_128;
+  const Numbers16 with_16;
   struct Tiles {
     TileT t[NT];
     __device__ __forceinline__ TileT& operator[](int i) { return t[i]; }
@@ -379,7 +379,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 
     floatx4 O[W];
     float m, l, lowest;
-    floatx4 weight;                        // of 4 bits: lowest: the sum of p lowest; weight, in each entry: of what the whole numbers were multiplied by, to take 128 off again
+    floatx4 weight;                        // of 4 bits: lowest: the sum of p lowest; weight, in each entry: of what the whole numbers were multiplied by, to take 16 off again
     bool careful = false, odd;
     while (true) {
       odd = false;
@@ -393,7 +393,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
         floatx4 S[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const float from = BF && Q4 ? -128.0f * qsum : 0.0f;
+          const float from = BF && Q4 ? -16.0f * qsum : 0.0f;
           S[t] = floatx4{from, from, from, from};
           if constexpr (BF && !Q4) {
 #pragma unroll
@@ -409,7 +409,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
               const unsigned x = T[t].k[i];
-              const uintx4 k = uintx4{with_128(x), with_128(x >> 4), with_128(x >> 8), with_128(x >> 12)};
+              const uintx4 k = uintx4{with_16(x, 0), with_16(x, 1), with_16(x, 2), with_16(x, 3)};
               S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, qb[i]), S[t], 0, 0, 0);
             }
           } else if constexpr (!Q4) {
@@ -553,7 +553,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
                 v[d] = pick(T[d >> 1].v[2 * (d & 1)][j >> 1], T[d >> 1].v[2 * (d & 1) + 1][j >> 1], j & 1 ? HIGHS : LOWS);
               } else {
                 const unsigned a = T[d >> 1].v[2 * (d & 1)], z = T[d >> 1].v[2 * (d & 1) + 1];
-                v[d] = with_128(pick(a, z, j < 4 ? LOWS : HIGHS) >> (4 * (j & 3)));
+                v[d] = with_16(pick(a, z, j < 4 ? LOWS : HIGHS), j & 3);
               }
             }
             O[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, hi), O[j], 0, 0, 0);
@@ -642,7 +642,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
     l = quads_sum(l);
     if constexpr (Q4) {
       lowest = quads_sum(lowest);
-      if constexpr (BF) lowest -= 128.0f * weight[0];
+      if constexpr (BF) lowest -= 16.0f * weight[0];
 #pragma unroll
       for (int j = 0; j < W; ++j) O[j] += lowest;
     }

@@ -674,3 +674,34 @@ def test_attention_of_large_scores(ctx, dts, n, past, spare):
             mag = 262.0 if dts[1] == Q4 else 8.0                  # of what is summed for a key: 255 and 7 beside it
             tol = 2 * (64 + keys + 64) * U * mag + 2.0 ** -16 * 8.0 + H(dts[0]) * o.abs()
             close(C[h * dh:(h + 1) * dh, :n], o, tol, (scale, h))
+
+
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("of", ["values", "keys"])
+def test_attention_on_4_bits_loses_nothing_beside_the_numbers(ctx, fast, dh, of):
+    """Sums that 24 bits hold with 16 beside every whole number, and not with 128: nothing is rounded, and what cancels leaves nothing.  512 tiles of 16000 keys, 4000 for a wavefront.
+    Values (n - 7.5) 129 / 128 with 15 - n in the next key: up to 31 * 129 / 128 * 4000 = 124969 < 2^17 in steps of 2^-7.
+    Keys n - 7.5 with 15 - n and an equal query in the next channel, queries of 128 to 255 and sixteenths of such: up to 31 * 255 * 64 * 17 / 16 = 537540 < 2^20 in steps of 2^-4 (heads of
+    128; beside 128 about 1.7 10^6)."""
+    kv, page, keys, n_seq = 16, 64, 16000, 32
+    g = torch.Generator(device="cuda").manual_seed(dh)
+    n = torch.randint(0, 16, (keys // page, kv, page, dh), generator=g, device="cuda", dtype=torch.uint8)
+    v, k = n.clone(), n.clone()
+    v[:, :, 1::2] = 15 - v[:, :, ::2]
+    k[..., 1::2] = 15 - k[..., ::2]
+    pack = lambda x: x[..., ::2] | (x[..., 1::2] << 4)
+    def scales(step):
+        s = torch.full((keys // page, kv, page, 2), step, device="cuda")
+        s[..., 0] = -7.5 * step
+        return s
+    cache = strp.PagedCache(pack(k), pack(v), scales(1.0), scales(129 / 128))
+    Q = torch.zeros((kv * dh, n_seq), device="cuda")
+    if of == "keys":
+        q = torch.randint(128, 256, (kv * dh // 4, 2, n_seq), generator=g, device="cuda").float()
+        q[:, 1] /= 16
+        Q = q.reshape(-1, 1, n_seq).expand(-1, 2, n_seq).reshape(kv * dh, n_seq)
+    Q = Q.to(BF16).contiguous()
+    table = torch.arange(keys // page, dtype=torch.int32, device="cuda").repeat(n_seq, 1).contiguous()
+    for c in ctx, fast:
+        C = c.strp_cache_attention(Q, n_seq, kv, cache, table, ints([keys - 1] * n_seq), ints(list(range(n_seq + 1))))
+        assert (C == 0).all(), (float(C.abs().max()), int((C != 0).sum()))

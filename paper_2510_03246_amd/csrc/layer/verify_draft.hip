@@ -460,15 +460,15 @@ __global__ __launch_bounds__(256) void verify_find_kernel(const VerifyP p) {
   if (threadIdx.x == 0) p.next_id[seq] = last;
 }
 
+constexpr int WIDEST = 8;                  // 16-byte columns of a workgroup: a line of 128 bytes
 struct VerifyPlan {
   int ct, groups_t, groups_d, slices, rows, parts, part_rows;
 };
 static VerifyPlan plan_verify(int V, long long T, int n_seq, int dtype) {
   VerifyPlan q;
   const long long vec = dtype == STRP_BF16 ? 8 : 4, chunks_t = (T + n_seq + vec - 1) / vec, chunks_d = (T + vec - 1) / vec;
-  const int widest = 8;                    // a line of 128 bytes
   q.ct = 1;
-  while (q.ct < widest && q.ct < chunks_t) q.ct *= 2;
+  while (q.ct < WIDEST && q.ct < chunks_t) q.ct *= 2;
   q.groups_t = (int)((chunks_t + q.ct - 1) / q.ct);
   q.groups_d = (int)((chunks_d + q.ct - 1) / q.ct);
   // as many workgroups as the chip holds at once, three a CU in bf16 and six in fp32 (verify_256 131 us; 1024 workgroups 134, 2048 138), none below one entry a thread
@@ -508,8 +508,13 @@ extern "C" {
 
 size_t strp_verify_draft_workspace_bytes(int32_t V, int64_t T, int32_t n_seq) {
   if (V <= 0 || V > (1 << 30) || T < 0 || T > (1 << 20) || n_seq <= 0 || n_seq > 65536) return 0;
+  // What plan_verify makes of these sizes or of smaller ones, in either type: more slices than one only where their workgroups, of up to 128 bytes of columns, are no more than 768 (fp32:
+  // 1536) in all.  (256 for every column asked for 9.1 GB at 2^20 drafted tokens of 65536 sequences, which take 0.31.)
+  const size_t columns = 2 * (size_t)T + n_seq, at_once = (size_t)768 * WIDEST * 8, most = (size_t)(V + 256 / WIDEST - 1) / (256 / WIDEST);
+  const size_t each = columns * (most < SLICES ? most : SLICES), all = columns > at_once ? columns : at_once;
+  const size_t parts = (size_t)(V + 255) / 256;
   // (a workspace has 4 KB at least)
-  return 4096 + up256((size_t)(2 * T + n_seq) * SLICES * sizeof(Mass)) + up256((size_t)n_seq * sizeof(Chosen)) + up256((size_t)n_seq * PARTS * 16);
+  return 4096 + up256((each < all ? each : all) * sizeof(Mass)) + up256((size_t)n_seq * sizeof(Chosen)) + up256((size_t)n_seq * (parts < PARTS ? parts : PARTS) * 16);
 }
 
 strp_status strp_verify_draft(strp_ctx* ctx, const strp_verify_draft_in* in) {

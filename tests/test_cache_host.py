@@ -147,6 +147,35 @@ def check_the_current_device_is_left_as_it_was():
             assert fake.hipGetDevice(C.byref(now)) == 0 and now.value == current
 
 
+def check_verify_workspace_is_near_what_a_call_takes():
+    """At most twice what a call takes and 256 KB (slices are whole numbers, and so are the workgroups of few columns), and never less for larger sizes than for smaller ones: a program asks once, for its largest call."""
+    lib = _library()
+    strp = lib.strp
+    need = lib.lib.strp_verify_draft_workspace_bytes
+
+    def least(V, T, n):
+        most = 0
+        for dt in (strp.BF16, strp.F32):
+            ld = (T + n + 7) // 8 * 8
+            call = strp.VerifyDraftIn(target=A[0], draft=A[1], draft_id=A[2], u=A[3], u_next=A[4], draft_start=A[5], accepted=A[6], next_id=A[7], dtype=dt, V=V, n_seq=n, temperature=1.0,
+                                      T=T, ldt=ld, ldd=ld)
+            low, high = 4096, 1 << 34
+            while high - low > 256:
+                mid = (low + high) // 2
+                lib.workspace(mid)
+                st, _ = lib.launches(lambda: lib.lib.strp_verify_draft(lib.h, C.byref(call)))
+                low, high = (low, mid) if st == strp.OK else (mid, high)
+            most = max(most, high)
+        return most
+
+    for V in (300, 5003, 50000, 130001):
+        for T, n in ((0, 1), (0, 64), (4, 1), (40, 9), (300, 70), (1024, 256), (4096, 1024), (8192, 2048), (1 << 20, 65536)):
+            asked, taken = need(V, T, n), least(V, T, n)
+            assert taken <= asked <= 2 * taken + (256 << 10), (V, T, n, asked, taken)
+            for smaller in ((V, T // 2, n), (V, T, (n + 1) // 2), (V // 2, T, n), (V, T - 1 if T else 0, n), (V, T // 3, (n + 2) // 3)):
+                assert need(*smaller) <= asked and least(*smaller) <= asked, (V, T, n, smaller)
+
+
 CHECKS = [check_append, check_attention, check_verify, check_the_current_device_is_left_as_it_was]
 
 
@@ -165,6 +194,10 @@ def test_cache_host(fake_hip, check):
         __graft_entry__.build()
     out = subprocess.run([sys.executable, os.path.abspath(__file__), check], env=dict(os.environ, FAKE_HIP=fake_hip), capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stdout + out.stderr
+
+
+def test_verify_workspace_is_near_what_a_call_takes(fake_hip):
+    test_cache_host(fake_hip, "check_verify_workspace_is_near_what_a_call_takes")
 
 
 def test_binding_structs_mirror_the_header(tmp_path):

@@ -68,10 +68,14 @@ __device__ __forceinline__ float left_over(float m, float scale) {
   const float r = m * scale;
   return BF && fabsf(r) < FAR ? __builtin_fmaf(m, scale, -r) : 0.0f;
 }
-// what results by the maximum m are multiplied by to be such by `to`, which is not below it
+// what results by the maximum m are multiplied by to be such by `to`, which is not below it: as exponents by that are rounded, or, for those who join them, as if they were not
 template <bool BF>
 __device__ __forceinline__ float between(float m, float to, float scale) {
   return __builtin_amdgcn_exp2f((m - to) * scale + (left_over<BF>(to, scale) - left_over<BF>(m, scale)));
+}
+template <bool BF>
+__device__ __forceinline__ float between_exactly(float m, float to, float scale) {
+  return __builtin_amdgcn_exp2f((m - to) * scale - left_over<BF>(m, scale));
 }
 
 // a value that all lanes have, in scalar registers

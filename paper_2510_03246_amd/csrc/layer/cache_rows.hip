@@ -666,7 +666,7 @@ __device__ __forceinline__ void rows_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const float mw = sM[w][row];
-        f[w] = mw == -INFINITY ? 0.0f : between<BF>(mw, M, p.scale_log2e);      // a wavefront that saw no key has zeros
+        f[w] = mw == -INFINITY ? 0.0f : between_exactly<BF>(mw, M, p.scale_log2e);      // a wavefront that saw no key has zeros
         L += f[w] * sL[w][row];
       }
       const bool whole_row = b0 == 0 && b1 == g.units;
@@ -734,7 +734,6 @@ __global__ __launch_bounds__(256, 2) void cache_wide_kernel(const RowsP p) {
 // the parts, a lane two channels.
 template <typename E>
 __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
-  constexpr bool BF = sizeof(E) == 2;
   __shared__ float sO[4][128];
   __shared__ float sM[4], sL[4];
   // a tile's workgroups are on different XCDs: what one reads for itself comes an eighth as fast (105 tokens, 6 heads, on 31000 keys of 4 bits: join 34 us on one, 26 on all)
@@ -763,7 +762,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
     float most = m;
 #pragma unroll
     for (int k = 0; k < UN; ++k) most = __builtin_elementwise_maximum(most, ml[k].x);
-    const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : between<BF>(of, most, p.scale_log2e); };
+    const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((of - most) * p.scale_log2e); };
     const float f = factor(m);
     m = most;
     l *= f;
@@ -791,7 +790,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(const RowsP p) {
   for (int w = 1; w < 4; ++w) most = __builtin_elementwise_maximum(most, sM[w]);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const float f = sM[w] == -INFINITY ? 0.0f : between<BF>(sM[w], most, p.scale_log2e);
+    const float f = sM[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((sM[w] - most) * p.scale_log2e);
     L += f * sL[w];
     sum += f * sO[w][threadIdx.x];
   }

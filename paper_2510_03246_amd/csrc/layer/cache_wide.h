@@ -575,6 +575,7 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
           }
     } else {
       const int slot = worker * 2 + (b0 == 0 ? 1 : 0);
+      const float by = __builtin_amdgcn_exp2f(-left_over<true>(m, p.scale_log2e));      // parts are joined as if exponents were not rounded
       float* part = p.wide_part + (long long)slot * width * WIDE + r;
       if (wave * 32 < rows)
 #pragma unroll
@@ -582,11 +583,11 @@ __device__ __forceinline__ void wide_share(const RowsP& p, const Heads& heads, u
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int x = 32 * ch + 8 * (e >> 2) + 4 * half + (e & 3);
-            if (x < width) part[x * WIDE] = O[ch][e];
+            if (x < width) part[x * WIDE] = O[ch][e] * by;
             __builtin_amdgcn_sched_barrier(0);
           }
       if (h == 0) {
-        p.wide_ml[slot * WIDE + r] = float2{m, sum};
+        p.wide_ml[slot * WIDE + r] = float2{m, sum * by};
         p.wide_off[slot * WIDE + r] = out;
       }
       // the workgroups from this one to that with the tile's last unit
@@ -621,7 +622,7 @@ __device__ __forceinline__ void wide_join(const RowsP& p, int worker, int y) {
       float most = m;
 #pragma unroll
       for (int k = 0; k < UN; ++k) most = i0 + k < parts ? __builtin_elementwise_maximum(most, ml[k].x) : most;
-      const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : between<true>(of, most, p.scale_log2e); };
+      const auto factor = [&](float of) { return of == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((of - most) * p.scale_log2e); };
       const float f = factor(m);
       m = most;
       l *= f;

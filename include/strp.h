@@ -434,8 +434,9 @@ strp_status strp_cache_append(strp_ctx* ctx, const strp_cache_append_in* in);
  * token does not see has no part in its result, whatever it holds, infinities and NaN included.
  * bf16: products of bf16 with fp32 sums; probabilities meet V as the context's precision says, as in strp_attention; whole numbers of 4 bits
  * enter the products exactly (few rows: 16 beside each of them, taken off behind the sums), lowest and step in fp32.  fp32: products of fp32.  The division by the sum of the probabilities comes last.
- * A call repeated on the same inputs gives the same bits; how the keys are split depends on all sequences of the call, so the
- * last bits of a sequence's results may depend on the lengths of the others.
+ * A call repeated on the same inputs gives the same bits; how the keys are split depends on all sequences of the call and on ld_table * page, so the
+ * last bits of a sequence's results may depend on the lengths of the others and on the table's width.  Chunks of tens of tokens are the faster for tables no
+ * wider than the longest sequence needs.
  * Errors: STRP_EINVAL (as strp_cache_append; heads * T above 2^30; scale not positive or above 2e38; kv_heads that does not divide heads without kv_of_head),
  * STRP_ENOMEM (strp_cache_attention_workspace_bytes).
  */

@@ -859,7 +859,9 @@ strp_status strp_cache_attention(strp_ctx* ctx, const strp_cache_attention_in* i
   if (p.group == 0) p.group = 1;
   // a tile has no more rows than the heads that one key-value head can have times the tokens
   const long long rows = (in->kv_of_head ? in->heads : p.group) * in->T;
-  // 128 rows at a time pay from about 2^23 pairs of a row and a key on, as far as the host knows them: what a call has beyond a token a sequence, and keys that a table holds.  Below, a
+  // 128 rows at a time pay from about 2^23 pairs of a row and a key on, as far as the host knows them: what a call has beyond a token a sequence, and keys that a table has room for.  That is
+  // more than there are where tables are wide (64 tokens of one sequence on 2000 keys 31 us with a table for those, 47 with one for 32768; the drafts below 114 and 118, the second launch
+  // finding nothing), and fewer rows where sequences have no tokens; the kernels know better, but not before they are launched.  Below, a
   // second launch and the join of large parts cost more than reading keys again for every 16 rows (32 heads of 128 on 2000 keys each: 64 tokens of one sequence 32 us by 16, 45 by 128,
   // 5 drafts of each of 16 sequences 103 and 108, 128 tokens 46 and 49; 200 tokens 62 and 54, 33 of each of 8 sequences 141 and 79, 100 on 30000 keys 456 and 155).
   const long long beyond = rows / in->T > WIDE_FROM ? in->T : in->T - c.n_seq;

@@ -4,7 +4,7 @@
 // with p and q the softmax of two columns of logits [V x tokens].  What is asked is an index into 10^5 sums, of which some lie within 10^-7 of each other:
 // 32 bits would answer beside it once in a few hundred times, so exponentials and sums are of 64.
 //
-// Four kernels: sums of exponentials over slices of every column (all that is read once; 256 sequences of 4 tokens, 50000 entries of bf16: 81 of 130 us, the vector unit busy 85 % of
+// Four kernels: sums of exponentials over slices of every column (all that is read once; 256 sequences of 4 tokens, 50000 entries of bf16: 87 of 132 us, the vector unit busy 83 % of
 // them where memory needs 45); the first token of every sequence that is not kept;
 // the sums of r over parts of the vocabulary; the part that holds the answer, entry by entry.
 #include "layer_ops.h"
@@ -17,7 +17,7 @@ constexpr int SLICES = 256, PARTS = 256;   // at most: a lane has four of either
 
 // e^y to 2^-43 of itself, for y from -705 to 600, in units of ln 2 / 32: y = 32 k + j + r with |r| <= 1/2, so that e^y = 2^k 2^(j/32) 2^(r/32): a table of 32 in LDS, which 64 banks
 // give to any lanes at once, and a polynomial of the fourth degree (the series to r^5 with that power taken for the nearest lower ones on the interval, a Chebyshev polynomial less).
-// 10 instructions in 64 bits, 18 an entry in all (verify_256 131 us; without the table and to r^12 22 instructions, and 445 us before the other steps too).
+// 10 instructions in 64 bits, 18 an entry in all (verify_256 132 us; without the table and to r^12 22 instructions, and 445 us before the other steps too).
 constexpr double LN2 = 0.69314718055994530942, UNITS = 32.0 / LN2;      // of ln 2 / 32 in one
 constexpr double LOWEST = -700.0 * UNITS;
 struct ExpTable { double of[32]; };
@@ -87,7 +87,7 @@ struct VerifyP {
 };
 
 // An exponent is x scale - from with from = ref scale, rounded: one instruction, but what that rounding took stays in every exponent, ref's own among them, and grows with ref / temperature.
-// It is one number a reference, so the sum by it is put right at its end (otherwise 10^-9 of it at logits of 20 and a temperature of 10^-6, 10^-3 at 10^-12, and anything at 10^-16).
+// It is one number a reference, so the sum by it is put right at its end (otherwise 10^-9 of it at logits of 20 and a temperature of 10^-6, 10^-3 at 10^-12, and anything at 10^-16; the correction costs verify_64 1.3 us of 55, verify_256 1.6 of 132).
 // From references of FAR units on differences come first: what is left would outgrow the exponents, and neighbouring logits are 2^21 units apart.
 constexpr double FAR = 35184372088832.0;   // 2^45
 __device__ __forceinline__ double left_over(float ref, double from, double scale) { return fabs(from) < FAR ? __builtin_fma((double)ref, scale, -from) : 0.0; }

@@ -639,7 +639,7 @@ def test_binding_refusals(ctx):
 @pytest.mark.parametrize("dts", CASES, ids=IDS)
 @pytest.mark.parametrize("n,past,spare", [(1, 700, 2), (3, 90, 2), (200, 400, 1 << 15), (200, 400, 2)], ids=["1", "3", "200-wide", "200"])
 def test_attention_of_large_scores(ctx, dts, n, past, spare):
-    """Whole scores about 524288, the best of every part of the keys another one: exact in fp32 (numbers of 4 bits enter with up to 255 of their query beside them: below 2^24), so a
+    """Whole scores about 524288, the best of every part of the keys another one: exact in fp32 (numbers of 4 bits enter as up to 31: below 2^22), so a
     probability is off by what its exponent is (64 2^-23: differences of up to 32 in powers of two, where it counts, rounded twice, and a scale rounded once), whatever the scale."""
     heads, dh, page, keys = 2, 64, 16, past + n
     pages = -(-keys // page)
@@ -671,7 +671,7 @@ def test_attention_of_large_scores(ctx, dts, n, past, spare):
             s = torch.where(seen, Q[h * dh:(h + 1) * dh, :n].double().t() @ K.t(), -math.inf)
             p = torch.softmax(scale * (s - s.max(1, keepdim=True).values), 1)
             o = (p @ V).t()
-            mag = 262.0 if dts[1] == Q4 else 8.0                  # of what is summed for a key: 255 and 7 beside it
+            mag = 54.0 if dts[1] == Q4 else 8.0                   # of what is summed for a key: 31, 16 taken off, and 7
             tol = 2 * (64 + keys + 64) * U * mag + 2.0 ** -16 * 8.0 + H(dts[0]) * o.abs()
             close(C[h * dh:(h + 1) * dh, :n], o, tol, (scale, h))
 

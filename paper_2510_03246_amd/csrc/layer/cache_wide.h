@@ -4,7 +4,7 @@
 // at a time (of 4 bits 32); their rows of K and of V lie in LDS as in their pages, the chunks of 16 bytes of a row in an order that depends on the row, so that what is read at
 // once lies in different banks.  A row is a lane's: S has the keys 8 (e / 4) + 4 (lane / 32) + e % 4 in its registers e, and where the fragments of V, read turned,
 // have the keys in that order too, eight registers of P are a second operand of V^T P as they are.  The scores of the next keys are multiplied beside the softmax of these.
-// Bound by the vector unit and the matrix cores, either busy half of the time: 1024 tokens of 32 heads of 128 (8 of keys) on 30000 keys 670-705 TFLOP/s by box, on 6000 560-570; 4 bits 357-375.
+// Bound by the vector unit and the matrix cores, either busy half of the time: 1024 tokens of 32 heads of 128 (8 of keys) on 30000 keys 670-705 TFLOP/s, on 6000 560-570; 4 bits 357-375.
 //
 // Work is counted in units of so many keys of one tile, and every workgroup has as many as any other.  Tile i of e sees about as many keys as it leaves to tile e - 1 - i: tiles
 // are taken in such pairs, which are all given the same number of units, so that nobody has to add up the tiles before his own.
